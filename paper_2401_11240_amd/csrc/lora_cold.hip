@@ -11,6 +11,7 @@
 #include "lora_coldstart.h"
 #include "lora_device.h"
 #include "lora_internal.h"
+#include "lora_stream.h"
 
 namespace lora {
 int set_error(int code, const std::string& msg);
@@ -43,25 +44,6 @@ __global__ void __launch_bounds__(kAddThreads) lora_add_delta_kernel(const float
     const float y2 = Fmt::to_f32(v.y & 0xffffu) + d.z, y3 = Fmt::to_f32(v.y >> 16) + d.w;
     *yp = uint2{Fmt::pack2(y0, y1), Fmt::pack2(y2, y3)};
 }
-
-// The device a stream belongs to current for the launch.
-struct StreamDevice {
-    int prev = -1;
-    bool ok = false;
-    explicit StreamDevice(hipStream_t s) {
-        int dev = -1;
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        if (s) {
-            if (hipStreamGetDevice(s, &dev) != hipSuccess) return;
-        } else {
-            dev = prev;
-        }
-        ok = dev == prev || hipSetDevice(dev) == hipSuccess;
-    }
-    ~StreamDevice() {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
 
 int enqueue_signal(uint32_t* flag, uint32_t value, hipStream_t s) {
     hipLaunchKernelGGL(lora_signal_kernel, dim3(1), dim3(64), 0, s, flag, value);

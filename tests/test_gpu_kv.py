@@ -1,0 +1,619 @@
+"""Paged key-value cache on the GPU: attention of single tokens and of prompt
+segments against a plain 64-bit form, rows into pages and the page book against
+Python lists, bit for bit."""
+import itertools
+import random
+import sys
+
+import numpy as np
+import pytest
+
+import kv_reference as R
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():   # collected on CPU-only hosts, never run there
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2401_11240_amd import kv as KV  # noqa: E402
+from paper_2401_11240_amd import lora as L  # noqa: E402
+
+DEV = torch.device("cuda:0")
+DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def stream():
+    return torch.cuda.current_stream(DEV)
+
+
+@pytest.fixture(scope="module")
+def attn():
+    a = KV.lora_attn_create(0, stream())
+    yield a
+    torch.cuda.synchronize()
+    KV.lora_attn_destroy(a)
+
+
+class Case:
+    """A cache with random pages, every row that no token occupies NaN, and
+    queries of the last rows of each sequence."""
+
+    def __init__(self, dtype, heads, kv_heads, dim, page_rows, lens, rows, *, order="head", layers=1, seed=0, pad=0,
+                 spare=3, q_scale=1.5, drop=()):
+        gen = torch.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        self.dtype, self.heads, self.kv_heads, self.dim, self.pr = dtype, heads, kv_heads, dim, page_rows
+        self.lens, self.rows = list(lens), list(rows)
+        held = [-(-n // page_rows) for n in lens]
+        ld = max(held + [1]) + 1
+        n_pages = sum(held) + spare
+        ids = rng.permutation(n_pages)
+        self.table = np.full((len(lens), ld), -1, np.int32)
+        at = 0
+        shape = (n_pages, page_rows, kv_heads, dim) if order == "row" else (n_pages, kv_heads, page_rows, dim)
+        td = DTYPES[dtype]
+        nan = float("nan")
+        k, v = (torch.randn(shape, generator=gen).to(td) for _ in range(2))
+        if order == "row":
+            k, v = k.transpose(1, 2), v.transpose(1, 2)
+        used = torch.zeros(n_pages, page_rows, dtype=torch.bool)
+        for s, n in enumerate(lens):
+            self.table[s, :held[s]] = ids[at:at + held[s]]
+            at += held[s]
+            for e in range(held[s]):
+                used[self.table[s, e], :max(0, min(page_rows, n - e * page_rows))] = True
+        mask = ~used[:, None, :, None]
+        k, v = k.masked_fill(mask, nan), v.masked_fill(mask, nan)
+        for s, e in drop:                        # visible tokens without a page
+            self.table[s, e] = -1 if e % 2 else n_pages + 7
+        self.n_pages = n_pages
+        self.k, self.v = k.double().numpy(), v.double().numpy()
+        # [layers, ...] on the device, other layers NaN
+        def dev(t):
+            if order == "row":
+                t = t.transpose(1, 2)
+            full = torch.full((layers,) + tuple(t.shape), nan, dtype=td, device=DEV)
+            full[layers - 1] = t.to(DEV)
+            return full.transpose(2, 3) if order == "row" else full
+        self.layer = layers - 1
+        self.kd, self.vd = dev(k), dev(v)
+        self.cache = KV.Cache(self.kd, self.vd)
+        n_rows = sum(rows)
+        w = heads * dim
+        q = (torch.randn((n_rows, w + pad), generator=gen) * q_scale).to(td)
+        self.q = q[:, :w].double().numpy().reshape(n_rows, heads, dim)
+        self.qd = q.to(DEV)
+        self.out = torch.full((n_rows, w + pad), 7.0, dtype=td, device=DEV)
+        self.ld = w + pad
+        self.tables = torch.from_numpy(self.table).to(DEV)
+        self.lens_d = torch.tensor(self.lens, dtype=torch.int32, device=DEV)
+        self.off = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+        self.off_d = torch.from_numpy(self.off).to(DEV)
+        self.seqs = KV.Seqs(self.tables, self.lens_d, max(self.lens + [0]))
+        self.scale = dim ** -0.5
+
+    def decode(self, attn, window=0, sinks=0, st=None):
+        KV.lora_attn_decode(attn, self.cache, self.layer, self.seqs, self.heads, self.qd, self.ld, self.out, self.ld,
+                            self.scale, window, sinks, st or stream())
+
+    def prompt(self, attn, window=0, sinks=0, st=None):
+        KV.lora_attn_prompt(attn, self.cache, self.layer, self.seqs, self.off_d, int(self.off[-1]), self.heads,
+                            self.qd, self.ld, self.out, self.ld, self.scale, window, sinks, st or stream())
+
+    def got(self):
+        w = self.heads * self.dim
+        o = self.out.double().cpu().numpy()
+        assert (o[:, w:] == 7.0).all()           # nothing behind a row's heads is written
+        return o[:, :w].reshape(-1, self.heads, self.dim)
+
+    def want(self, window=0, sinks=0, seqs=None):
+        ref = np.zeros_like(self.q)
+        tol = np.zeros_like(self.q)
+        for s, (n, r) in enumerate(zip(self.lens, self.rows)):
+            lo, hi = int(self.off[s]), int(self.off[s + 1])
+            o, m, reach = R.attention(self.q[lo:hi], self.k, self.v, self.table[s], n, n - r, self.scale, window, sinks)
+            ref[lo:hi] = o
+            tol[lo:hi] = R.allowance(o, m, reach, self.dim, max(1, n), self.dtype == "bf16")
+        return ref, tol
+
+    def check(self, window=0, sinks=0, what=""):
+        got = self.got()
+        ref, tol = self.want(window, sinks)
+        err = np.abs(got - ref)
+        assert np.isfinite(got).all(), what
+        worst = float((err / tol).max()) if err.size else 0.0
+        rel = float(np.linalg.norm(got - ref) / max(1e-30, np.linalg.norm(ref)))
+        say(f"{what}: rel {rel:.2e}, worst {worst:.2f} of the allowance")
+        assert worst <= 1.0, what
+
+
+HEADS = [(4, 4, 128), (8, 1, 128), (6, 2, 64), (16, 2, 256), (3, 1, 80), (20, 1, 96), (34, 2, 128), (5, 5, 8),
+         (2, 1, 200), (7, 7, 16)]
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_decode_heads(attn, dtype, heads, kv_heads, dim):
+    lens = [1, 0, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 255, 300, 513, 1000]
+    c = Case(dtype, heads, kv_heads, dim, 16, lens, [1] * len(lens), seed=heads * dim, pad=8)
+    c.decode(attn)
+    c.check(what=f"decode {dtype} {heads}/{kv_heads} x {dim}")
+
+
+@pytest.mark.parametrize("page_rows,order,layers", [(16, "row", 2), (32, "head", 1), (64, "row", 1), (128, "head", 3),
+                                                    (1024, "head", 1)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (17, 0), (100, 3), (128, 128), (64, 500), (4000, 4)])
+def test_decode_pages_and_windows(attn, page_rows, order, layers, window, sinks):
+    lens = [700, 1, 0, 129, 1300, 64, 31, 2500]
+    c = Case("bf16", 8, 2, 128, page_rows, lens, [1] * 8, order=order, layers=layers, seed=page_rows + window)
+    c.decode(attn, window, sinks)
+    c.check(window, sinks, f"decode pages of {page_rows} {order}, window {window}, sinks {sinks}")
+
+
+@pytest.mark.parametrize("lens,heads,kv_heads,dim", [([20000], 8, 2, 128), ([5000, 3, 9000], 2, 1, 64),
+                                                     ([4097], 16, 16, 128), ([3001, 17000], 4, 1, 256),
+                                                     ([2000] * 40, 4, 4, 128), ([9] * 700, 3, 3, 64)])
+def test_decode_split_over_the_cache(attn, lens, heads, kv_heads, dim):
+    c = Case("f16", heads, kv_heads, dim, 32, lens, [1] * len(lens), seed=len(lens))
+    for rep in range(3):                         # the counters are ready for the next launch
+        c.out.fill_(7.0)
+        c.decode(attn)
+        if rep == 0:
+            first = c.out.clone()
+    assert torch.equal(first, c.out)
+    c.check(what=f"decode {lens[:3]} x {len(lens)}")
+
+
+PROMPTS = [
+    # lens, rows
+    ([1], [1]), ([5], [5]), ([64], [64]), ([129], [129]), ([200, 1, 77], [200, 1, 77]),
+    ([300, 300, 90], [17, 300, 1]), ([1000], [100]), ([40, 0, 256], [40, 0, 0]), ([700, 33], [500, 33]),
+]
+
+
+@pytest.mark.parametrize("lens,rows", PROMPTS)
+@pytest.mark.parametrize("heads,kv_heads,dim,dtype", [(4, 4, 128, "bf16"), (8, 1, 128, "f16"), (6, 2, 64, "bf16"),
+                                                      (4, 2, 256, "f16"), (3, 1, 80, "bf16"), (5, 5, 8, "f16"),
+                                                      (20, 1, 96, "bf16")])
+def test_prompt_shapes(attn, lens, rows, heads, kv_heads, dim, dtype):
+    c = Case(dtype, heads, kv_heads, dim, 16, lens, rows, seed=len(lens) + dim, pad=16)
+    c.prompt(attn)
+    c.check(what=f"prompt {lens} rows {rows} {dtype} {heads}/{kv_heads} x {dim}")
+
+
+@pytest.mark.parametrize("page_rows,order", [(16, "row"), (64, "head"), (256, "row")])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (17, 2), (64, 64), (100, 130), (333, 1), (5000, 4)])
+def test_prompt_pages_and_windows(attn, page_rows, order, window, sinks):
+    c = Case("f16", 4, 2, 128, page_rows, [600, 130, 257], [431, 130, 50], order=order, layers=2, seed=window)
+    c.prompt(attn, window, sinks)
+    c.check(window, sinks, f"prompt pages of {page_rows} {order}, window {window}, sinks {sinks}")
+
+
+@pytest.mark.parametrize("lens,rows,heads,kv_heads,dim", [([9000], [40], 8, 2, 128), ([5000, 7000], [3, 130], 4, 1, 64),
+                                                          ([6001], [9], 4, 4, 256)])
+def test_prompt_split_over_the_cache(attn, lens, rows, heads, kv_heads, dim):
+    c = Case("bf16", heads, kv_heads, dim, 64, lens, rows, seed=lens[0])
+    for rep in range(3):
+        c.out.fill_(7.0)
+        c.prompt(attn)
+        if rep == 0:
+            first = c.out.clone()
+    assert torch.equal(first, c.out)
+    c.check(what=f"prompt {lens} rows {rows}")
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_cases(attn, seed):
+    rng = random.Random(seed)
+    dim = 8 * rng.randint(1, 32)
+    kv_heads, group = rng.choice([(1, 1), (1, 5), (2, 8), (3, 3), (1, 17), (4, 1)])
+    n = rng.randint(1, 9)
+    lens = [rng.choice([rng.randint(0, 70), rng.randint(0, 900)]) for _ in range(n)]
+    rows = [rng.randint(0, x) for x in lens]
+    window = rng.choice([0, rng.randint(1, 400)])
+    sinks = rng.choice([0, rng.randint(0, 90)])
+    page_rows = rng.choice([16, 32, 64, 512])
+    args = dict(order=rng.choice(["head", "row"]), seed=seed, pad=rng.choice([0, 8]))
+    dtype = rng.choice(["f16", "bf16"])
+    what = f"seed {seed}: {dtype} {kv_heads * group}/{kv_heads} x {dim} pages {page_rows} lens {lens} rows {rows} window {window} sinks {sinks}"
+    say(what)
+    if sum(rows):
+        c = Case(dtype, kv_heads * group, kv_heads, dim, page_rows, lens, rows, **args)
+        c.prompt(attn, window, sinks)
+        c.check(window, sinks, "prompt " + what)
+    c = Case(dtype, kv_heads * group, kv_heads, dim, page_rows, lens, [1] * n, **args)
+    c.decode(attn, window, sinks)
+    c.check(window, sinks, "decode " + what)
+
+
+def test_more_rows_than_tokens(attn):
+    # rows at negative positions see nothing: zeros
+    c = Case("bf16", 4, 2, 64, 16, [3, 40], [10, 40], seed=1)
+    c.prompt(attn)
+    c.check(what="rows before the first token")
+    assert (c.got()[:7] == 0).all()
+
+
+def test_tokens_without_a_page_are_left_out(attn):
+    lens, rows = [200, 64, 33, 1500], [1, 1, 1, 1]
+    drop = [(0, 0), (0, 5), (1, 0), (1, 1), (1, 2), (1, 3), (2, 2), (3, 40)]
+    c = Case("bf16", 4, 2, 128, 16, lens, rows, seed=2, drop=drop)
+    c.decode(attn)
+    c.check(what="decode with missing pages")
+    assert (c.got()[1] == 0).all()
+    c = Case("f16", 4, 2, 128, 16, lens, [150, 64, 33, 20], seed=3, drop=drop)
+    c.prompt(attn)
+    c.check(what="prompt with missing pages")
+
+
+def test_released_pages_behind_a_window_are_not_read(attn):
+    window, sinks = 70, 5
+    lens = [500, 90, 1100]
+    drop = [(s, e) for s, n in enumerate(lens) for e in range(1, 40) if (e + 1) * 16 - 1 <= n - window and e * 16 >= sinks]
+    c = Case("bf16", 8, 2, 128, 16, lens, [1] * 3, seed=4, drop=drop)
+    c.decode(attn, window, sinks)
+    c.check(window, sinks, "decode behind a trimmed window")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_hidden_values_do_not_reach_rows_that_do_not_see_them(attn, dtype, bad, dim):
+    # token 90 of a 130-row prompt is not finite: rows before it are as without it
+    c = Case(dtype, 4, 2, dim, 16, [130], [130], seed=5)
+    c.prompt(attn)
+    clean = c.got()
+    page, row = int(c.table[0, 90 // 16]), 90 % 16
+    c.vd[c.layer][page, :, row] = bad
+    c.prompt(attn)
+    o = c.got()
+    assert np.array_equal(o[:90], clean[:90])
+    assert not np.isfinite(o[90:]).any()
+    c.kd[c.layer][page, :, row] = bad
+    c.prompt(attn)
+    o = c.got()
+    assert np.array_equal(o[:90], clean[:90])
+    # and with a window of 20, rows from 110 on do not see it either
+    c.prompt(attn, 20, 0)
+    o = c.got()
+    c.k[page, :, row] = 0
+    c.v[page, :, row] = 0
+    ref, tol = c.want(20, 0)
+    hidden = [r for r in range(130) if r < 90 or r >= 110]
+    assert (np.abs(o - ref)[hidden] <= tol[hidden]).all()
+
+
+def test_large_and_small_scores(attn):
+    # one token holds all the weight; scores of some thousands; equal scores
+    for q_scale in (0.0, 30.0, 600.0):
+        c = Case("bf16", 4, 2, 128, 16, [300, 1, 77], [1, 1, 1], seed=6, q_scale=q_scale)
+        c.decode(attn)
+        c.check(what=f"decode, queries times {q_scale}")
+        c = Case("f16", 4, 2, 128, 16, [300, 1, 77], [128, 1, 77], seed=6, q_scale=min(q_scale, 300.0))
+        c.prompt(attn)
+        c.check(what=f"prompt, queries times {q_scale}")
+
+
+def test_rising_scores(attn):
+    # the maximum grows with every token: the running maximum moves in every tile
+    c = Case("bf16", 2, 1, 64, 16, [900], [1], seed=8)
+    k = torch.zeros(c.kd[0].shape, dtype=torch.float32)
+    for j in range(900):
+        k[c.table[0, j // 16], :, j % 16] = j / 100.0
+    c.kd[0].copy_(k)
+    c.k = k.to(DTYPES["bf16"]).double().numpy()
+    c.qd.fill_(1.0)
+    c.q[:] = 1.0
+    c.decode(attn)
+    c.check(what="rising scores, decode")
+    p = Case("bf16", 2, 1, 64, 16, [900], [300], seed=8)
+    p.kd[0].copy_(k)
+    p.k = c.k
+    p.qd.fill_(1.0)
+    p.q[:] = 1.0
+    p.prompt(attn)
+    p.check(what="rising scores, prompt")
+
+
+def test_offsets_past_32_bits(attn):
+    dim, pr, gap = 64, 16, (1 << 31) + 4096      # elements between pages: 4 GiB and some
+    lens = [40, 21]
+    store = [torch.empty(gap * 4 + 2 * pr * dim, dtype=torch.float16, device=DEV) for _ in range(2)]
+    views = [t.as_strided((1, 5, 2, pr, dim), (0, gap, pr * dim, dim, 1)) for t in store]
+    c = Case("f16", 4, 2, dim, pr, lens, [1, 1], seed=9, spare=0)
+    for view, src in zip(views, (c.kd, c.vd)):
+        view[0, :c.n_pages] = src[0]
+    c.cache = KV.Cache(*views)
+    c.decode(attn)
+    c.check(what="decode, pages 4 GiB apart")
+    p = Case("f16", 4, 2, dim, pr, lens, [33, 21], seed=9, spare=0)
+    p.cache = c.cache
+    for view, src in zip(views, (p.kd, p.vd)):
+        view[0, :p.n_pages] = src[0]
+    p.prompt(attn)
+    p.check(what="prompt, pages 4 GiB apart")
+    new = torch.randn((2, 2 * dim), device=DEV).half()
+    KV.lora_kv_append(c.cache, 0, c.seqs, None, 2, new, 2 * dim, -new, 2 * dim, stream())
+    for s, n in enumerate(lens):
+        page = int(c.table[s, (n - 1) // pr])
+        assert torch.equal(views[0][0, page, :, (n - 1) % pr].reshape(-1), new[s])
+        assert torch.equal(views[1][0, page, :, (n - 1) % pr].reshape(-1), -new[s])
+
+
+def test_garbage_lengths_and_tables_stay_inside(attn):
+    # lengths above max_len and below zero, page ids of every kind, offsets out of order
+    c = Case("bf16", 4, 2, 128, 16, [100, 100, 100], [1, 1, 1], seed=10)
+    c.lens_d.copy_(torch.tensor([1 << 30, -5, 100], dtype=torch.int32))
+    c.decode(attn)
+    got = c.got()
+    c.lens[1] = 0
+    ref, tol = c.want()
+    assert (np.abs(got - ref) <= tol).all()      # the first is read as max_len = 100
+    c.tables.fill_(1 << 30)
+    c.decode(attn)
+    assert (c.got() == 0).all()
+    p = Case("bf16", 4, 2, 128, 16, [100, 100], [60, 40], seed=11)
+    p.tables.fill_(-(1 << 31))
+    p.prompt(attn)
+    assert (p.got() == 0).all()
+    for off in ([0, 1 << 30, -7], [-3, 50, 40], [90, 20, 100], [1 << 30, 1 << 30, 1 << 30]):
+        say("offsets", off)
+        p.off_d.copy_(torch.tensor(off, dtype=torch.int32))
+        p.prompt(attn)
+        KV.lora_kv_append(p.cache, 0, p.seqs, p.off_d, 100, p.qd, p.ld, p.qd, p.ld, stream())
+        torch.cuda.synchronize()
+
+
+def test_other_stream_and_graph(attn):
+    """A decode loop recorded once: grow, append, attention; every replay against the reference."""
+    heads, kvh, dim, pr, n = 8, 2, 128, 16, 3
+    lens0 = [14, 100, 31]
+    c = Case("bf16", heads, kvh, dim, pr, lens0, [1] * n, seed=12, spare=12)
+    n_pages = c.n_pages
+    tables = torch.full((n, 12), -1, dtype=torch.int32)
+    tables[:, :c.table.shape[1]] = torch.from_numpy(c.table)
+    ref_book = R.Book(tables.tolist(), lens0, n_pages, pr)
+    tables = tables.to(DEV)
+    refs = torch.tensor(ref_book.refs, dtype=torch.int32, device=DEV)
+    book = KV.Book(tables, c.lens_d, refs, pr)
+    seqs = KV.Seqs(tables, c.lens_d, 12 * pr)
+    add = torch.ones(n, dtype=torch.int32, device=DEV)
+    info = torch.zeros(2, dtype=torch.int32, device=DEV)
+    nb = KV.lora_kv_workspace_bytes(book)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    w = kvh * dim
+    kn, vn = (torch.zeros((n, w), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+
+    def step(st):
+        KV.lora_kv_grow(book, add, info, ws, nb, st)
+        KV.lora_kv_append(c.cache, 0, seqs, None, n, kn, w, vn, w, st)
+        KV.lora_attn_decode(attn, c.cache, 0, seqs, heads, c.qd, c.ld, c.out, c.ld, c.scale, 0, 0, st)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(torch.cuda.current_stream())
+    gen = torch.Generator().manual_seed(3)
+    for rep in range(20):
+        knh, vnh = (torch.randn((n, w), generator=gen).bfloat16() for _ in range(2))
+        qh = torch.randn((n, heads * dim), generator=gen).bfloat16()
+        kn.copy_(knh), vn.copy_(vnh), c.qd.copy_(qh)
+        if rep % 3 == 2:
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                step(side)
+            torch.cuda.synchronize()
+        else:
+            graph.replay()
+        assert ref_book.grow([1] * n) == info.tolist()
+        assert tables.tolist() == ref_book.t and refs.tolist() == ref_book.refs
+        c.lens = list(ref_book.lens)
+        assert c.lens_d.tolist() == c.lens
+        c.table = np.array(ref_book.t)
+        c.q = qh.double().numpy().reshape(n, heads, dim)
+        for s in range(n):
+            j = c.lens[s] - 1
+            c.k[c.table[s, j // pr], :, j % pr] = knh[s].double().numpy().reshape(kvh, dim)
+            c.v[c.table[s, j // pr], :, j % pr] = vnh[s].double().numpy().reshape(kvh, dim)
+        c.check(what=f"token {rep}")
+
+
+# ---------------------------------------------------------------------------
+# rows into pages, and the book
+# ---------------------------------------------------------------------------
+
+def bits(t):
+    return t.view(torch.int16)
+
+
+@pytest.mark.parametrize("order", ["head", "row"])
+@pytest.mark.parametrize("kv_heads,dim,page_rows", [(1, 8, 16), (8, 128, 16), (3, 80, 64), (40, 128, 32), (2, 256, 128)])
+def test_append(order, kv_heads, dim, page_rows):
+    lens, rows = [50, 1, 0, 300, 17, 64, 5], [50, 1, 0, 37, 3, 64, 9]
+    c = Case("f16", kv_heads, kv_heads, dim, page_rows, lens, rows, order=order, layers=2, seed=dim)
+    c.table[3, 0] = -1
+    c.tables.copy_(torch.from_numpy(c.table))
+    w = kv_heads * dim
+    n = sum(rows)
+    kn = torch.randn((n, w + 8), device=DEV).half()
+    vn = torch.randn((n, w + 16), device=DEV).half()
+    wk, wv = c.kd.clone(), c.vd.clone()
+    for s in range(len(lens)):
+        for i in range(rows[s]):
+            j = lens[s] - rows[s] + i
+            if j < 0 or c.table[s, j // page_rows] < 0:
+                continue
+            page, r = int(c.table[s, j // page_rows]), j % page_rows
+            wk[1, page, :, r] = kn[c.off[s] + i, :w].view(kv_heads, dim)
+            wv[1, page, :, r] = vn[c.off[s] + i, :w].view(kv_heads, dim)
+    KV.lora_kv_append(c.cache, 1, c.seqs, c.off_d, n, kn, w + 8, vn, w + 16, stream())
+    assert torch.equal(bits(c.kd), bits(wk)) and torch.equal(bits(c.vd), bits(wv))
+    # one row per sequence
+    kn, vn = (torch.randn((len(lens), w), device=DEV).half() for _ in range(2))
+    for s in range(len(lens)):
+        j = lens[s] - 1
+        if j >= 0 and c.table[s, j // page_rows] >= 0:
+            wk[0, int(c.table[s, j // page_rows]), :, j % page_rows] = kn[s].view(kv_heads, dim)
+            wv[0, int(c.table[s, j // page_rows]), :, j % page_rows] = vn[s].view(kv_heads, dim)
+    KV.lora_kv_append(c.cache, 0, c.seqs, None, len(lens), kn, w, vn, w, stream())
+    assert torch.equal(bits(c.kd), bits(wk)) and torch.equal(bits(c.vd), bits(wv))
+
+
+class Pages:
+    """A book on the device beside its reference, and a small cache."""
+
+    def __init__(self, n_seqs, ld, n_pages, page_rows, lens, seed=0, layers=2, kv_heads=2, dim=16, order="head"):
+        rng = random.Random(seed)
+        free = list(range(n_pages))
+        rng.shuffle(free)
+        tables = [[-1] * ld for _ in range(n_seqs)]
+        for s, n in enumerate(lens):
+            for e in range(-(-n // page_rows)):
+                tables[s][e] = free.pop()
+        lens = list(lens) + [0] * (n_seqs - len(lens))
+        self.ref = R.Book(tables, lens, n_pages, page_rows)
+        i32 = dict(dtype=torch.int32, device=DEV)
+        self.tables, self.lens = torch.tensor(tables, **i32), torch.tensor(lens, **i32)
+        self.refs = torch.tensor(self.ref.refs, **i32)
+        self.book = KV.Book(self.tables, self.lens, self.refs, page_rows)
+        self.nb = KV.lora_kv_workspace_bytes(self.book)
+        self.ws = torch.full((self.nb,), 0xff, dtype=torch.uint8, device=DEV)
+        self.info = torch.full((2,), -9, **i32)
+        shape = (layers, n_pages, page_rows, kv_heads, dim) if order == "row" else (layers, n_pages, kv_heads, page_rows, dim)
+        self.k, self.v = (torch.randint(-32768, 32767, shape, dtype=torch.int16, device=DEV).view(torch.bfloat16)
+                          for _ in range(2))
+        if order == "row":
+            self.k, self.v = self.k.transpose(2, 3), self.v.transpose(2, 3)
+        self.cache = KV.Cache(self.k, self.v)
+
+    def same(self):
+        assert self.lens.tolist() == self.ref.lens
+        assert self.refs.tolist() == self.ref.refs
+        held = [self.ref.t[s][:self.ref.held(s)] for s in range(len(self.ref.lens))]
+        assert [row[:len(h)] for row, h in zip(self.tables.tolist(), held)] == held
+
+
+@pytest.mark.parametrize("n_pages", [5, 40, 9000, 20001])
+def test_grow(n_pages):
+    p = Pages(1300, 6, n_pages, 16, [20, 0, 33], seed=n_pages)
+    rng = random.Random(n_pages)
+    for rep in range(4):
+        add = [rng.choice([0, 0, 1, 1, 5, 16, 40, -3, 200]) for _ in range(1300)]
+        KV.lora_kv_grow(p.book, torch.tensor(add, dtype=torch.int32, device=DEV), p.info, p.ws, p.nb, stream())
+        assert p.info.tolist() == p.ref.grow(add), rep
+        p.same()
+    KV.lora_kv_grow(p.book, torch.ones(1300, dtype=torch.int32, device=DEV), None, p.ws, p.nb, stream())
+    p.ref.grow([1] * 1300)
+    p.same()
+
+
+@pytest.mark.parametrize("order", ["head", "row"])
+@pytest.mark.parametrize("n_pages,seqs", [(60, 20), (4000, 700), (9, 20)])
+def test_fork_free_trim_compact(n_pages, seqs, order):
+    rng = random.Random(n_pages)
+    lens, room = [], n_pages
+    for _ in range(seqs // 2):
+        n = rng.choice([0, 1, 16, 17, 40, 64, 95])
+        if room < -(-n // 16):
+            break
+        room -= -(-n // 16)
+        lens.append(n)
+    p = Pages(seqs, 6, n_pages, 16, lens, seed=1, order=order)
+    n_par = len(lens)
+    for rep in range(6):
+        kids = rng.sample(range(n_par, seqs), rng.randint(0, min(300, seqs - n_par)))
+        pars = [rng.randrange(n_par) for _ in kids]
+        wk, wv = p.k.clone(), p.v.clone()
+        KV.lora_kv_fork(p.cache, p.book, pars, kids, p.info, p.ws, p.nb, stream())
+        info, copies = p.ref.fork(pars, kids)
+        assert p.info.tolist() == info
+        p.same()
+        for src, dst, rows in copies:
+            for w, t in ((wk, p.k), (wv, p.v)):
+                w[:, dst, :, :rows] = w[:, src, :, :rows].clone()
+        assert torch.equal(bits(p.k), bits(wk)) and torch.equal(bits(p.v), bits(wv))
+        if rep == 2:
+            KV.lora_kv_trim(p.book, 30, 4, stream())
+            p.ref.trim(30, 4)
+            p.same()
+        gone = rng.sample(range(n_par, seqs), (seqs - n_par) // 3)
+        KV.lora_kv_free(p.book, gone, stream())
+        p.ref.free(gone)
+        p.same()
+        if rep % 2:
+            out = (p.tables, p.refs)             # in place
+            if rep == 3:
+                out = (torch.full_like(p.tables, -5), torch.full_like(p.refs, -5))
+                before = (p.tables.clone(), p.refs.clone())
+            wk, wv = p.k.clone(), p.v.clone()
+            KV.lora_kv_compact(p.cache, p.book, out[0], out[1], p.info, p.ws, p.nb, stream())
+            info, moves = p.ref.compact()
+            assert p.info.tolist() == info
+            for src, dst in moves:
+                wk[:, dst], wv[:, dst] = wk[:, src].clone(), wv[:, src].clone()
+            assert torch.equal(bits(p.k), bits(wk)) and torch.equal(bits(p.v), bits(wv))
+            if rep == 3:
+                assert torch.equal(p.tables, before[0]) and torch.equal(p.refs, before[1])
+                p.tables.copy_(out[0]), p.refs.copy_(out[1])
+            assert p.tables.tolist() == p.ref.t
+            p.same()
+
+
+@pytest.mark.parametrize("layers,kv_heads,dim,page_rows,order", [(1, 1, 8, 16, "head"), (3, 5, 80, 64, "row"),
+                                                                 (2, 8, 128, 32, "head"), (1, 2, 256, 1024, "row")])
+def test_copy(layers, kv_heads, dim, page_rows, order):
+    n = 600
+    if page_rows > 64:
+        n = 40
+    p = Pages(1, 1, n, page_rows, [1], layers=layers, kv_heads=kv_heads, dim=dim, order=order)
+    ids = list(range(n))
+    random.Random(dim).shuffle(ids)
+    half = n // 2
+    src, dst = [random.Random(i).choice(ids[:half]) for i in range(half)], ids[half:half + half]
+    wk, wv = p.k.clone(), p.v.clone()
+    wk[:, dst], wv[:, dst] = wk[:, src], wv[:, src]
+    KV.lora_kv_copy(p.cache, src, dst, stream())
+    assert torch.equal(bits(p.k), bits(wk)) and torch.equal(bits(p.v), bits(wv))
+    KV.lora_kv_copy(p.cache, [], [], stream())
+
+
+def test_nothing_to_do(attn):
+    e = torch.empty((0, 1), dtype=torch.int32, device=DEV)
+    c = Case("bf16", 4, 2, 64, 16, [10], [10])
+    seqs = KV.Seqs(e, torch.empty(0, dtype=torch.int32, device=DEV), 0)
+    KV.lora_attn_decode(attn, c.cache, 0, seqs, 4, None, 256, None, 256, 1.0, 0, 0, stream())
+    KV.lora_attn_prompt(attn, c.cache, 0, seqs, c.off_d, 0, 4, None, 256, None, 256, 1.0, 0, 0, stream())
+    KV.lora_kv_append(c.cache, 0, seqs, None, 0, None, 128, None, 128, stream())
+    book = KV.Book(e, torch.empty(0, dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), 16)
+    ws = torch.empty(64, dtype=torch.uint8, device=DEV)
+    info = torch.full((2,), 5, dtype=torch.int32, device=DEV)
+    KV.lora_kv_grow(book, None, info, ws, 64, stream())
+    assert info.tolist() == [0, 0]
+    KV.lora_kv_free(book, [], stream())
+    KV.lora_kv_trim(book, 1, 0, stream())
+
+
+def test_capture_refused_and_memory_unchanged(attn):
+    graph = torch.cuda.CUDAGraph()
+    x = torch.zeros(4, device=DEV)
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(L.LoraError) as e:
+            KV.lora_attn_create(0, torch.cuda.current_stream())
+    assert e.value.code == L.LORA_E_CAPTURE
+    c = Case("bf16", 8, 2, 128, 16, [700, 30], [1, 1])
+    c.decode(attn)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    for _ in range(5):
+        c.decode(attn)
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == free
