@@ -1,4 +1,31 @@
 // gfx950 kernels of attention over the paged key-value cache (include/lora_kv.h).
+//
+// Decode: one new token per sequence.  Per visible token and key-value head
+// 4 head_dim bytes are read and 4 group head_dim operations done on them (group: the q
+// heads that share the head), far below what the chip computes per byte read:
+// the launch is bound by HBM, so what counts is that every compute unit reads
+// all the time and that nothing is read twice.
+//
+//   Work: the visible tokens of every (sequence, key-value head) are cut into
+//   tiles of kTile tokens; all tiles of the launch lie in one line, and
+//   workgroup w takes tiles [w R, (w + 1) R), R from the lengths as they are on
+//   the device.  So the load is even whatever the lengths, one long sequence
+//   fills the chip, and a recorded launch serves every later token.
+//
+//   Tile: four waves of 32 tokens.  S^T = K Q^T on v_mfma_f32_16x16x32 with the
+//   tokens as rows, so that a lane's four results are four tokens of one head;
+//   in the product O^T = V^T P^T the 32 tokens may stand in any order, and the one
+//   taken is that of the lanes that hold their weights: P goes from one product
+//   into the other without leaving its lane.  V^T comes from 8 tokens x
+//   head_dim / 16 elements per lane, transposed in registers (one v_perm per
+//   word).  No LDS in the loop, each byte of K and V is loaded once, 16 bytes
+//   per lane.  The group's heads are the 16 columns; most of the arithmetic is
+//   on empty columns when few heads share keys, and free beside the reads.
+//
+//   Join: a head's partial results (float32 sums with their maximum) of the
+//   four waves meet in LDS, those of several workgroups in device memory: the
+//   last one to arrive, counted by an atomic, adds them up in the order of the
+//   tokens, so the result does not depend on timing.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -8,9 +35,17 @@
 
 using namespace lora;
 
+namespace {
+// Workgroups of the decode kernel per compute unit: registers for a tile's K and V
+// in flight beside the output.
+constexpr int decode_per_cu(int dp) { return dp == 256 ? 1 : dp == 128 ? 3 : 4; }
+}
+
 struct lora_attn_s {
     int device = 0;
     int n_cu = 0;
+    uint32_t* counters = nullptr;          // one per workgroup of a decode launch: partial results that have arrived; 0 between launches
+    float* slots = nullptr;                // two partial results per workgroup
 };
 
 namespace {
@@ -26,6 +61,410 @@ struct AttnArgs {
     int32_t window, n_sinks;
     float scale;
 };
+
+constexpr int kTile = 128;                 // tokens per tile: 32 per wave
+constexpr int kWaveTokens = 32;
+constexpr int kHeads = 16;                 // q heads per group tile (columns of the MFMA)
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// One partial result in device memory: kHeads rows of the unnormalised output, then the
+// maxima and the sums.
+constexpr int slot_floats(int dp) { return kHeads * dp + 2 * kHeads; }
+
+// The visible tokens of a decode row: [0, sinks) and [first, len), in tiles
+// [0, sink_tiles) and [win_tile, ..).  At least one tile, so that a row that
+// sees nothing is written as well.
+struct Span {
+    int len, first, sinks, sink_tiles, win_tile, n;
+};
+__device__ __forceinline__ Span decode_span(const AttnArgs& a, int s) {
+    Span p;
+    p.len = kv_len(a.lens, s, a.max_len);
+    p.first = a.window ? max(0, p.len - a.window) : 0;
+    p.sinks = min(a.n_sinks, p.first);
+    p.sink_tiles = (p.sinks + kTile - 1) / kTile;
+    p.win_tile = max(p.first / kTile, p.sink_tiles);
+    p.n = max(1, p.sink_tiles + (p.len + kTile - 1) / kTile - p.win_tile);
+    return p;
+}
+__device__ __forceinline__ int tile_token(const Span& p, int i) {
+    return (i < p.sink_tiles ? i : p.win_tile + i - p.sink_tiles) * kTile;
+}
+
+struct DecodeArgs {
+    AttnArgs a;
+    uint32_t* counters;
+    float* slots;
+    int32_t heads_per_seq;                 // kv heads times group tiles
+    int32_t group_tiles;
+};
+
+// The largest of v over the four lanes l % 16 + 16 i, in each of them.
+__device__ __forceinline__ float max_over_quarters(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_over_quarters(float v) {
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+template <class Fmt, int DP>
+struct DecodeWave {
+    static constexpr int NS = DP / 32;     // MFMA steps of a score
+    static constexpr int NV = DP / 16;     // elements of V per lane and token
+    static constexpr int VW = NV / 2;      // the same in words
+    const AttnArgs& a;
+    const int l, w;
+    u32x4 q[NS];
+    u32x4 kf[2][NS];
+    uint32_t vf[8][VW];
+    f32x4 o[NV];
+    float m, sum;
+    uint32_t koff[NS], voff[(NV + 7) / 8];
+    uint32_t page_bytes, row_bytes;
+    int pages;                             // lane i: page of subtile i of the next 32 tiles
+    int pages_at;                          // the first of those tiles
+    bool has_page[2];                      // of the tile in kf, for its two subtiles
+    __device__ __forceinline__ DecodeWave(const AttnArgs& args)
+        : a(args), l(threadIdx.x & 63), w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {
+        row_bytes = (uint32_t)a.row_stride * 2u;
+        page_bytes = ((1u << a.page_shift) - 1) * row_bytes + (uint32_t)a.head_dim * 2u;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) koff[i] = 32 * i + 8 * (l >> 4) < a.head_dim ? 64u * i + 16u * (l >> 4) : (uint32_t)kOut;
+#pragma unroll
+        for (int i = 0; i < (NV + 7) / 8; ++i)
+            voff[i] = (l & 15) * NV + 8 * i < a.head_dim ? (l & 15) * NV * 2u + 16u * i : (uint32_t)kOut;
+    }
+
+    // Pages of the subtiles of tiles [i, i + 32): lane 2 t + u that of tile i + t's tokens 32 w + 16 u on, -1 where none is seen.
+    __device__ __forceinline__ void load_pages(const Span& p, int s, int i, int end) {
+        const int t = i + (l >> 1);
+        const int token = tile_token(p, t) + kWaveTokens * w + 16 * (l & 1);
+        const bool seen = t < end && token < p.len && (token < p.sinks || token + 15 >= p.first);
+        int page = -1;
+        if (seen) page = a.tables[(int64_t)s * a.ld_table + (token >> a.page_shift)];
+        pages = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+        pages_at = i;
+    }
+    __device__ __forceinline__ rsrc_t page_rsrc(const uint16_t* base, int page, int kh) const {
+        const int64_t at = max(page, 0) * a.page_stride + kh * a.head_stride;
+        return make_rsrc(base + at, page < 0 ? 0u : page_bytes);
+    }
+    __device__ __forceinline__ void load_k(const Span& p, int kh, int i) {
+        const int base = tile_token(p, i) + kWaveTokens * w;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int page = __builtin_amdgcn_readlane(pages, 2 * (i - pages_at) + u);
+            has_page[u] = page >= 0;
+            const rsrc_t r = page_rsrc(a.k, page, kh);
+            const uint32_t row = (uint32_t)(((base + 16 * u) & ((1 << a.page_shift) - 1)) + (l & 15)) * row_bytes;
+#pragma unroll
+            for (int x = 0; x < NS; ++x) kf[u][x] = bload16(r, (int)(row + koff[x]));
+        }
+    }
+    // Which tokens of a tile this lane sees: x stands for token x + 4 (l / 16) of the wave's 32.
+    struct Seen {
+        int sinks, first, end;
+        __device__ __forceinline__ Seen(const Span& p, int base, int l)
+            : sinks(p.sinks - base - 4 * (l >> 4)), first(p.first - base - 4 * (l >> 4)), end(p.len - base - 4 * (l >> 4)) {}
+        __device__ __forceinline__ bool operator()(int x) const { return (x < sinks) | ((x >= first) & (x < end)); }
+    };
+    __device__ __forceinline__ void load_v(const Span& p, int kh, int i) {
+        const int base = tile_token(p, i) + kWaveTokens * w;
+        const Seen seen(p, base, l);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const rsrc_t r = page_rsrc(a.v, __builtin_amdgcn_readlane(pages, 2 * (i - pages_at) + u), kh);
+            const uint32_t row = (uint32_t)(((base + 16 * u) & ((1 << a.page_shift) - 1)) + 4 * (l >> 4)) * row_bytes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // values of tokens that are not seen are not read: their weight is
+                // zero, but zero times an infinity or a NaN is not
+                const uint32_t at = seen(16 * u + j) ? row : (uint32_t)kOut;
+                const int so = j * (int)row_bytes;
+                if constexpr (NV == 4) {
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)(at + voff[0]), so, 0));
+                    vf[4 * u + j][0] = x[0];
+                    vf[4 * u + j][1] = x[1];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < NV / 8; ++x) {
+                        const u32x4 y = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(at + voff[x]), so, 0));
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) vf[4 * u + j][4 * x + z] = y[z];
+                    }
+                }
+            }
+        }
+    }
+    // Scores of the tile from kf, weights, and the statistics; returns the weights as the B operand of the product with V.
+    __device__ __forceinline__ u32x4 weights(const Span& p, int i) {
+        const int base = tile_token(p, i) + kWaveTokens * w;
+        f32x4 sc[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < NS; ++x) c = Fmt::mma32(kf[u][x], q[x], c);
+            sc[u] = c;
+        }
+        const float c = a.scale * kLog2e;
+        const Seen seen(p, base, l);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[u][j] = (seen(16 * u + j) & has_page[u]) ? sc[u][j] * c : -INFINITY;
+        float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                          fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+        top = max_over_quarters(top);
+        const float mn = fmaxf(m, top);
+        const float ref = mn == -INFINITY ? 0.f : mn;
+        const float f = __builtin_amdgcn_exp2f(m - ref);
+        m = mn;
+        u32x4 pw;
+        float add = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(sc[u][2 * h] - ref),
+                                              __builtin_amdgcn_exp2f(sc[u][2 * h + 1] - ref));
+                pw[2 * u + h] = x;
+                add += Fmt::to_f32(lo16(x)) + Fmt::to_f32(hi16(x));
+            }
+        sum = sum * f + add;
+#pragma unroll
+        for (int t = 0; t < NV; ++t) o[t] *= f;
+        return pw;
+    }
+    __device__ __forceinline__ void add_v(const u32x4& pw) {
+#pragma unroll
+        for (int t = 0; t < NV; ++t) {
+            u32x4 x;
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+                x[z] = (t & 1) ? pack_hi(vf[2 * z][t >> 1], vf[2 * z + 1][t >> 1])
+                               : pack_lo(vf[2 * z][t >> 1], vf[2 * z + 1][t >> 1]);
+            o[t] = Fmt::mma32(x, pw, o[t]);
+        }
+    }
+    // Tiles [i0, i1) of sequence s, key-value head kh, group tile g.
+    __device__ __forceinline__ void run(const Span& p, int s, int kh, int g, int i0, int i1) {
+        const int head = g * kHeads + (l & 15);
+        const uint16_t* qr = a.q + s * a.ldq + (int64_t)(kh * a.group) * a.head_dim;
+        const rsrc_t r = make_rsrc(qr, (uint32_t)a.group * a.head_dim * 2u);
+        load_pages(p, s, i0, i1);
+        load_k(p, kh, i0);
+        load_v(p, kh, i0);
+#pragma unroll
+        for (int x = 0; x < NS; ++x)
+            q[x] = bload16(r, head < a.group ? (int)((uint32_t)head * a.head_dim * 2u + koff[x]) : kOut);
+        m = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < NV; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = i0; i < i1; ++i) {
+            const u32x4 pw = weights(p, i);
+            // kf and vf are refilled as soon as they have been used, and not before:
+            // a second set of registers would cost more waves than it brings.
+            // (tile i1 has no pages: its loads return zeros and read nothing)
+            if (i + 1 - pages_at == 32) load_pages(p, s, i + 1, i1);
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(p, kh, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            add_v(pw);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(p, kh, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum = sum_over_quarters(sum);
+    }
+};
+
+template <class Fmt, int DP>
+__global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kernel(DecodeArgs d) {
+    constexpr int NV = DP / 16;
+    constexpr int LD = DP + 4;
+    __shared__ float lo[4][kHeads][LD];
+    __shared__ float lm[4][kHeads], ls[4][kHeads];
+    __shared__ int wave_n[4], wave_max[4], at_seq, at_before, last;
+    const AttnArgs& a = d.a;
+    const int t = threadIdx.x, l = t & 63, w = t >> 6;
+    // the line of all tiles: tiles of the sequences before each
+    const int per = (a.n_seqs + 255) / 256;
+    int mine = 0, longest = 0;
+    for (int s = t * per; s < min(t * per + per, a.n_seqs); ++s) {
+        const int n = decode_span(a, s).n;
+        mine += n;
+        longest = max(longest, n);
+    }
+    int before = mine;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+        const int o = __shfl_up(before, i, 64);
+        if (l >= i) before += o;
+        longest = max(longest, __shfl_xor(longest, i, 64));
+    }
+    if (l == 63) {
+        wave_n[w] = before;
+        wave_max[w] = longest;
+    }
+    __syncthreads();
+    int tiles = 0;
+    longest = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        before += i < w ? wave_n[i] : 0;
+        tiles += wave_n[i];
+        longest = max(longest, wave_max[i]);
+    }
+    before -= mine;
+    const int64_t total = (int64_t)tiles * d.heads_per_seq;
+    int64_t R = (total + gridDim.x - 1) / gridDim.x;
+    const int64_t start = blockIdx.x * R;
+    if (start >= total) return;
+    const int at = (int)(start / d.heads_per_seq);
+    if (at >= before && at < before + mine) {
+        int s = t * per, b = before;
+        for (;;) {
+            const int n = decode_span(a, s).n;
+            if (at < b + n) break;
+            b += n;
+            ++s;
+        }
+        at_seq = s;
+        at_before = b;
+    }
+    __syncthreads();
+    int s = __builtin_amdgcn_readfirstlane(at_seq);
+    int seq_before = __builtin_amdgcn_readfirstlane(at_before);
+    Span p = decode_span(a, s);
+    int hs, i0;
+    {
+        const int64_t in = start - (int64_t)seq_before * d.heads_per_seq;
+        hs = (int)(in / p.n);
+        i0 = (int)(in - (int64_t)hs * p.n);
+    }
+    int64_t left = min(R, total - start);
+    DecodeWave<Fmt, DP> wave(a);
+    while (true) {
+        const int take = (int)min(left, (int64_t)(p.n - i0));
+        const int kh = hs / d.group_tiles, g = hs - kh * d.group_tiles;
+        wave.run(p, s, kh, g, i0, i0 + take);
+        // the waves' results meet in LDS
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < NV; x += 4)
+                *(f32x4*)&lo[w][l & 15][(4 * (l >> 4) + i) * NV + x] =
+                    f32x4{wave.o[x][i], wave.o[x + 1][i], wave.o[x + 2][i], wave.o[x + 3][i]};
+        if (l < 16) {
+            lm[w][l] = wave.m;
+            ls[w][l] = wave.sum;
+        }
+        __syncthreads();
+        // thread t: elements NV (t % 16) .. of head t / 16
+        const int h = t >> 4, e0 = (t & 15) * NV;
+        const int head = g * kHeads + h;
+        float M = fmaxf(fmaxf(lm[0][h], lm[1][h]), fmaxf(lm[2][h], lm[3][h]));
+        float S = 0.f;
+        f32x4 acc[NV / 4];
+#pragma unroll
+        for (int x = 0; x < NV / 4; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        {
+            const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = __builtin_amdgcn_exp2f(lm[i][h] - ref);
+                S += ls[i][h] * f;
+#pragma unroll
+                for (int x = 0; x < NV / 4; ++x) acc[x] += *(const f32x4*)&lo[i][h][e0 + 4 * x] * f;
+            }
+        }
+        bool store = true;
+        if (take != p.n) {
+            // a part of the head's tokens: to device memory, and on only if all parts are there
+            const int64_t first = (int64_t)seq_before * d.heads_per_seq + (int64_t)hs * p.n;
+            const int w0 = (int)(first / R), w1 = (int)((first + p.n - 1) / R);
+            constexpr int SF = slot_floats(DP);
+            const int slot = 2 * (int)blockIdx.x + (i0 == 0);
+            const rsrc_t r = make_rsrc(d.slots + (int64_t)slot * SF, SF * 4u);
+            if (head < a.group) {
+#pragma unroll
+                for (int x = 0; x < NV / 4; ++x) bstore16<kCoherent>(as_u4(acc[x]), r, (h * DP + e0 + 4 * x) * 4);
+                if ((t & 15) == 0)
+                    bstore8<kCoherent>(u32x2{__float_as_uint(M), __float_as_uint(S)}, r, (kHeads * DP + 2 * h) * 4);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            if (t == 0)
+                last = __hip_atomic_fetch_add(d.counters + w0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                       (uint32_t)(w1 - w0);
+            __syncthreads();
+            store = last;
+            if (store) {
+                if (t == 0) __hip_atomic_store(d.counters + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                M = -INFINITY;
+                S = 0.f;
+#pragma unroll
+                for (int x = 0; x < NV / 4; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (head < a.group)
+                    for (int v = w0; v <= w1; ++v) {
+                        const rsrc_t r2 = make_rsrc(d.slots + (int64_t)(2 * v + (v == w0)) * SF, SF * 4u);
+                        const u32x2 ms = bload8<kCoherent>(r2, (kHeads * DP + 2 * h) * 4);
+                        const float m1 = __uint_as_float(ms[0]), mn = fmaxf(M, m1), ref = mn == -INFINITY ? 0.f : mn;
+                        const float f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
+                        M = mn;
+                        S = S * f0 + __uint_as_float(ms[1]) * f1;
+#pragma unroll
+                        for (int x = 0; x < NV / 4; ++x)
+                            acc[x] = acc[x] * f0 + as_f4(bload16<kCoherent>(r2, (h * DP + e0 + 4 * x) * 4)) * f1;
+                    }
+            }
+        }
+        if (store && head < a.group) {
+            const float f = S != 0.f ? 1.f / S : 0.f;
+            uint16_t* dst = a.out + s * a.ldo + (int64_t)(kh * a.group + head) * a.head_dim + e0;
+#pragma unroll
+            for (int x = 0; x < NV / 4; x += NV == 4 ? 1 : 2) {
+                if (e0 + 4 * x >= a.head_dim) continue;
+                const f32x4 y = acc[x] * f;
+                if constexpr (NV == 4) {
+                    *(u32x2*)dst = u32x2{Fmt::pack2(y[0], y[1]), Fmt::pack2(y[2], y[3])};
+                } else {
+                    const f32x4 z = acc[x + 1] * f;
+                    *(u32x4*)(dst + 4 * x) = u32x4{Fmt::pack2(y[0], y[1]), Fmt::pack2(y[2], y[3]),
+                                                   Fmt::pack2(z[0], z[1]), Fmt::pack2(z[2], z[3])};
+                }
+            }
+        }
+        left -= take;
+        if (left == 0) return;
+        // the next head, or the next sequence's first
+        i0 = 0;
+        if (++hs == d.heads_per_seq) {
+            seq_before += p.n;
+            hs = 0;
+            p = decode_span(a, ++s);
+        }
+        __syncthreads();                   // lo, lm, ls have been read
+    }
+}
+
+template <int DP>
+void launch_decode(const DecodeArgs& d, int dtype, int blocks, hipStream_t st) {
+    if (dtype == LORA_F16)
+        hipLaunchKernelGGL((lora_attn_decode_kernel<FmtF16, DP>), dim3(blocks), dim3(256), 0, st, d);
+    else
+        hipLaunchKernelGGL((lora_attn_decode_kernel<FmtBF16, DP>), dim3(blocks), dim3(256), 0, st, d);
+}
+
+__global__ void __launch_bounds__(256) lora_attn_clear_kernel(uint32_t* p, int n) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) p[i] = 0u;
+}
 
 // One wave per row and head: 4 elements of the head per lane, one token at a time.
 template <class Fmt>
@@ -166,12 +605,38 @@ int lora_attn_create(lora_attn_t* out, int device, void* stream) {
     auto* h = new (std::nothrow) lora_attn_s();
     if (!h) return set_error(LORA_E_NOMEM, "handle allocation failed");
     h->device = device;
+    int n_cu = 0;
+    if (hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n_cu < 1) n_cu = 256;
+    h->n_cu = n_cu;
+    const size_t n_counters = (size_t)n_cu * decode_per_cu(64);
+    size_t n_floats = 0;
+    for (int dp = 64; dp <= 256; dp *= 2)
+        n_floats = std::max(n_floats, (size_t)n_cu * decode_per_cu(dp) * 2 * slot_floats(dp));
+    hipError_t e = hipMalloc((void**)&h->counters, n_counters * 4);
+    if (e == hipSuccess) e = hipMalloc((void**)&h->slots, n_floats * 4);
+    if (e != hipSuccess) {
+        lora_attn_destroy(h);
+        return set_error(LORA_E_NOMEM, std::string("hipMalloc of the attention handle: ") + hipGetErrorString(e));
+    }
+    hipLaunchKernelGGL(lora_attn_clear_kernel, dim3((unsigned)((n_counters + 255) / 256)), dim3(256), 0,
+                       (hipStream_t)stream, h->counters, (int)n_counters);
+    e = hipGetLastError();
+    if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
+    if (e != hipSuccess) {
+        lora_attn_destroy(h);
+        return set_error(LORA_E_HIP, std::string("lora_attn_create: ") + hipGetErrorString(e));
+    }
     *out = h;
     return LORA_OK;
 }
 
 int lora_attn_destroy(lora_attn_t a) {
     if (!a) return set_error(LORA_E_ARG, "attention handle is NULL");
+    {
+        HandleDevice g(a->device);
+        (void)hipFree(a->counters);
+        (void)hipFree(a->slots);
+    }
     delete a;
     return LORA_OK;
 }
@@ -184,10 +649,20 @@ int lora_attn_decode(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     HandleDevice g(h->device);
     if (!g.ok) return set_error(LORA_E_HIP, "lora_attn_decode: cannot select the device");
     const AttnArgs a = attn_args(c, layer, s, nullptr, s->n_seqs, n_heads, q, ldq, out, ldo, scale, window, n_sinks);
-    if (c->dtype == LORA_F16)
-        hipLaunchKernelGGL(lora_attn_row_kernel<FmtF16>, dim3(a.n_rows, n_heads), dim3(64), 0, (hipStream_t)stream, a);
-    else
-        hipLaunchKernelGGL(lora_attn_row_kernel<FmtBF16>, dim3(a.n_rows, n_heads), dim3(64), 0, (hipStream_t)stream, a);
+    DecodeArgs d;
+    d.a = a;
+    d.counters = h->counters;
+    d.slots = h->slots;
+    d.group_tiles = (a.group + kHeads - 1) / kHeads;
+    d.heads_per_seq = c->n_kv_heads * d.group_tiles;
+    const int64_t tiles = std::max(1, (s->max_len + kTile - 1) / kTile + 1);   // of a sequence, at most
+    if (tiles * s->n_seqs > 0x7fffffff || tiles * d.heads_per_seq > 0x7fffffff)
+        return set_error(LORA_E_SHAPE, "lora_attn_decode: more than 2^31 tiles of 128 tokens");
+    const int dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    const int blocks = (int)std::min<int64_t>((int64_t)h->n_cu * decode_per_cu(dp), tiles * s->n_seqs * d.heads_per_seq);
+    if (dp == 64) launch_decode<64>(d, c->dtype, blocks, (hipStream_t)stream);
+    else if (dp == 128) launch_decode<128>(d, c->dtype, blocks, (hipStream_t)stream);
+    else launch_decode<256>(d, c->dtype, blocks, (hipStream_t)stream);
     return check_launch("lora_attn_decode");
 }
 
