@@ -175,14 +175,17 @@ struct DecodeWave {
         const Seen seen(p, base, l);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const rsrc_t r = page_rsrc(a.v, __builtin_amdgcn_readlane(pages, 2 * (i - pages_at) + u), kh);
+            const int page = __builtin_amdgcn_readlane(pages, 2 * (i - pages_at) + u);
+            const rsrc_t r = page_rsrc(a.v, page, kh);
+            // (an empty buffer with no scalar offset, so that every offset is out of its range)
+            const int step = page < 0 ? 0 : (int)row_bytes;
             const uint32_t row = (uint32_t)(((base + 16 * u) & ((1 << a.page_shift) - 1)) + 4 * (l >> 4)) * row_bytes;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 // values of tokens that are not seen are not read: their weight is
                 // zero, but zero times an infinity or a NaN is not
                 const uint32_t at = seen(16 * u + j) ? row : (uint32_t)kOut;
-                const int so = j * (int)row_bytes;
+                const int so = j * step;
                 if constexpr (NV == 4) {
                     const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)(at + voff[0]), so, 0));
                     vf[4 * u + j][0] = x[0];
@@ -466,53 +469,489 @@ __global__ void __launch_bounds__(256) lora_attn_clear_kernel(uint32_t* p, int n
     if (i < n) p[i] = 0u;
 }
 
-// One wave per row and head: 4 elements of the head per lane, one token at a time.
+// ---------------------------------------------------------------------------
+// prompt
+// ---------------------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kCols = 128;                 // columns (row, head) of a workgroup: 32 per wave
+constexpr int kKeys = 64;                  // tokens per step
+constexpr float kSlack = 8.f;              // how far (in powers of two) a maximum may rise before the sums are rescaled
+
+struct PromptArgs {
+    AttnArgs a;
+    uint32_t* counters;
+    float* slots;
+    int32_t kv_heads;
+    int32_t parts;                         // workgroups that share a tile's tokens
+};
+
+// Floats of a partial result: the outputs, then maximum and sum of every column.
+constexpr int part_floats(int dp) { return kCols * dp + 2 * kCols; }
+
 template <class Fmt>
-__global__ void __launch_bounds__(64) lora_attn_row_kernel(AttnArgs a) {
-    const int l = threadIdx.x, row = blockIdx.x, h = blockIdx.y;
-    int s = row, n = 1, i = 0;
-    if (a.seg_offset) {
-        int lo = 0, hi = a.n_seqs;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (a.seg_offset[mid + 1] > row) hi = mid;
-            else lo = mid + 1;
+__device__ __forceinline__ f32x16 mma32x32(const u32x4& a, const u32x4& b, f32x16 c);
+template <>
+__device__ __forceinline__ f32x16 mma32x32<FmtF16>(const u32x4& a, const u32x4& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x16 mma32x32<FmtBF16>(const u32x4& a, const u32x4& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// s + the two 16-bit values of x.
+template <class Fmt>
+__device__ __forceinline__ float add_pair(uint32_t x, float s);
+template <>
+__device__ __forceinline__ float add_pair<FmtF16>(uint32_t x, float s) {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2v, x), __builtin_bit_cast(f16x2v, 0x3c003c00u), s, false);
+}
+template <>
+__device__ __forceinline__ float add_pair<FmtBF16>(uint32_t x, float s) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v, x), __builtin_bit_cast(bf16x2v, 0x3f803f80u), s, false);
+}
+
+// 16 bytes per lane from buffer r at byte offset off + so (zeros when out of
+// range) into LDS at lds + 16 * lane; lds, so and r are the same in every lane.
+// Inline assembly without an output: for the builtin the compiler waits for
+// every such load in flight before each LDS read.  A wait and a barrier order the
+// reads after it.  The wait state after the write of m0 is here, those of the
+// resource in uniform_rsrc().
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is reserved: nothing to preserve, the clobber is what is said
+__device__ __forceinline__ void lds_load16(const u32x4& r, uint32_t lds, uint32_t off, uint32_t so) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(lds), "v"(off), "s"(r), "s"(so) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// The resource of make_rsrc() as four scalar words, five wait states after the
+// vector instructions that may write them.
+__device__ __forceinline__ u32x4 uniform_rsrc(const void* base, uint32_t bytes) {
+    const uint64_t b = (uint64_t)base;
+    u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xffffu,
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), (uint32_t)kRsrcWord3};
+    asm volatile("s_nop 4" : "+s"(r));
+    return r;
+}
+
+// Transposing read: lane j of each 16 lanes gets element j % 4 of the 8-byte
+// values that lanes j / 4, 4 + j / 4, 8 + j / 4 and 12 + j / 4 address.
+__device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds_u8*)p));
+}
+
+// The larger of v in lane l and lane l ^ 32, in both; their sum.
+__device__ __forceinline__ float max_over_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_over_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A workgroup's tile: 128 columns of one segment and key-value head, and the
+// tokens that some row of it sees, [0, sinks) and [first, last], in steps of 64.
+struct PromptTile {
+    int seq, row0, n;                      // segment, its first row, its rows
+    int col0;                              // the tile's first column: row col0 / group, head col0 % group
+    int pos0;                              // position of the segment's first row
+    int lowest, last;                      // positions of the tile's first and last row
+    int first, sinks, sink_steps, win_step, steps;
+};
+
+template <class Fmt, int DP>
+struct PromptBlock {
+    static constexpr int CH = DP / 8;      // 16-byte chunks of a token
+    static constexpr int NS = DP / 16;     // MFMA steps of a score
+    static constexpr int ND = DP / 32;     // 32-row blocks of the output
+    static constexpr int NL = CH / 4;      // loads of K (and of V) per wave and step
+    static constexpr int kStage = kKeys * CH * 16;   // bytes of K (or V) of a step
+    const PromptArgs& pa;
+    const AttnArgs& a;
+    const PromptTile& p;
+    unsigned char* lds;
+    const int kh, l, w;
+    const int pos;                         // of this lane's column, -1 for none
+    u32x4 q[NS];
+    f32x16 o[ND];
+    float m, sum;
+    uint32_t ko[NL], vo[NL];               // byte offsets of this lane's chunks in its 16 tokens; kOut past the head
+    uint32_t row_bytes, page_bytes, lbase;
+    int pages, next_pages;                 // lane 4 t + g: page of tokens 16 g on of step t of 16, -1 for none seen
+    uint64_t has_pages;                    // which of pages there are
+
+    __device__ __forceinline__ PromptBlock(const PromptArgs& args, const PromptTile& tile, unsigned char* smem, int kv_head,
+                                           int position)
+        : pa(args), a(args.a), p(tile), lds(smem), kh(kv_head), l(threadIdx.x & 63),
+          w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), pos(position) {
+        lbase = (uint32_t)(uintptr_t)(lds_u8*)smem;
+        row_bytes = (uint32_t)a.row_stride * 2u;
+        page_bytes = ((1u << a.page_shift) - 1) * row_bytes + (uint32_t)a.head_dim * 2u;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int at = i * 64 + l, r = at / CH;
+            const int kc = (at % CH) ^ k_key(r), vc = (at % CH) ^ v_key(r);
+            ko[i] = 8 * kc < a.head_dim ? r * row_bytes + 16u * kc : (uint32_t)kOut;
+            vo[i] = 8 * vc < a.head_dim ? r * row_bytes + 16u * vc : (uint32_t)kOut;
         }
-        s = lo;
-        if (s >= a.n_seqs) return;
-        const int first = a.seg_offset[s];
-        n = min(a.seg_offset[s + 1], a.n_rows) - first;
-        i = row - first;
-        if (first < 0 || i < 0) return;
     }
-    const int len = kv_len(a.lens, s, a.max_len);
-    const int p = len - n + i;
-    const int d = 4 * l;
-    const bool in = d < a.head_dim;
-    float q[4] = {0, 0, 0, 0}, o[4] = {0, 0, 0, 0}, m = -INFINITY, sum = 0.f;
-    if (in)
-        for (int e = 0; e < 4; ++e) q[e] = Fmt::to_f32(a.q[row * a.ldq + (int64_t)h * a.head_dim + d + e]);
-    for (int j = 0; j <= p; ++j) {
-        if (a.window && j <= p - a.window && j >= a.n_sinks) continue;
-        const int page = a.tables[(int64_t)s * a.ld_table + (j >> a.page_shift)];
-        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-        const int64_t at = page * a.page_stride + (h / a.group) * a.head_stride +
-                           (j & ((1 << a.page_shift) - 1)) * a.row_stride + d;
-        float x = 0.f;
-        if (in)
-            for (int e = 0; e < 4; ++e) x += q[e] * Fmt::to_f32(a.k[at + e]);
-        for (int b = 1; b < 64; b <<= 1) x += __shfl_xor(x, b, 64);
-        x *= a.scale;
-        const float mn = fmaxf(m, x), f = m == -INFINITY ? 0.f : expf(m - mn), w = mn == -INFINITY ? 0.f : expf(x - mn);
-        m = mn;
-        sum = sum * f + w;
-        if (in)
-            for (int e = 0; e < 4; ++e) o[e] = o[e] * f + w * Fmt::to_f32(a.v[at + e]);
+    // Chunk c of token r stands in slot c ^ key(r) of its row.  K: the 16 rows
+    // that a quarter wave reads one chunk of lie in 16 bank groups.  V: the four
+    // rows that a transposing read takes 64 bytes of lie in four.
+    static __device__ __forceinline__ int k_key(int r) { return CH >= 16 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ int v_key(int r) { return CH >= 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
+
+    __device__ __forceinline__ int step_token(int i) const {
+        return (i < p.sink_steps ? i : p.win_step + i - p.sink_steps) * kKeys;
     }
-    if (!in) return;
-    const float r = sum != 0.f ? 1.f / sum : 0.f;
-    for (int e = 0; e < 4; e += 2)
-        *(uint32_t*)(a.out + row * a.ldo + (int64_t)h * a.head_dim + d + e) = Fmt::pack2(o[e] * r, o[e + 1] * r);
+    __device__ __forceinline__ void fetch_pages(int i, int end) {
+        const int t = i + (l >> 2), token = step_token(t) + 16 * (l & 3);
+        const bool seen = t < end && token <= p.last && (token < p.sinks || token + 15 >= p.first);
+        int page = -1;
+        if (seen) page = a.tables[(int64_t)p.seq * a.ld_table + (token >> a.page_shift)];
+        next_pages = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+    }
+    // K and V of step i (of pages' 16 from step `at` on) into buffer b: wave w the tokens 16 w .. + 15.
+    __device__ __forceinline__ void load(int i, int at, int b) {
+        const int token = step_token(i) + 16 * w;
+        const int page = __builtin_amdgcn_readlane(pages, 4 * (i - at) + w);
+        const int64_t off = max(page, 0) * a.page_stride + kh * a.head_stride;
+        const uint32_t bytes = page < 0 ? 0u : page_bytes;
+        const u32x4 kr = uniform_rsrc(a.k + off, bytes), vr = uniform_rsrc(a.v + off, bytes);
+        // (an empty buffer with no scalar offset, so that every offset is out of its range)
+        const uint32_t so = page < 0 ? 0u : (uint32_t)(token & ((1 << a.page_shift) - 1)) * row_bytes;
+        const uint32_t to = lbase + (uint32_t)(b * 2 * kStage + w * 16 * CH * 16);
+        if ((token + 15 <= p.last) & ((token >= p.first) | (token + 15 < p.sinks))) {
+#pragma unroll
+            for (int j = 0; j < NL; ++j) lds_load16(kr, to + j * 1024u, ko[j], so);
+#pragma unroll
+            for (int j = 0; j < NL; ++j) lds_load16(vr, to + kStage + j * 1024u, vo[j], so);
+        } else {
+            // tokens that no row of the tile sees are not read: zeros
+#pragma unroll
+            for (int j = 0; j < NL; ++j) {
+                const int x = token + (j * 64 + l) / CH;
+                const bool in = (x <= p.last) & ((x >= p.first) | (x < p.sinks));
+                lds_load16(kr, to + j * 1024u, in ? ko[j] : (uint32_t)kOut, so);
+                lds_load16(vr, to + kStage + j * 1024u, in ? vo[j] : (uint32_t)kOut, so);
+            }
+        }
+    }
+    __device__ __forceinline__ bool visible(int token) const {
+        return (token <= pos) & ((a.window == 0) | (token > pos - a.window) | (token < a.n_sinks));
+    }
+
+    // The two 16-bit values of x, infinities and NaN replaced by zero.
+    static constexpr uint32_t kExponent = Fmt::kNarrowRange ? 0x7c00u : 0x7f80u;
+    static __device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
+        const uint32_t lo = (x & kExponent) == kExponent ? 0u : lo16(x);
+        return (x >> 16 & kExponent) == kExponent ? lo : lo | (x & 0xffff0000u);
+    }
+
+    // Steps [i0, i1) into o, m and sum.  A token that a column does not see has
+    // weight zero, which is as good as leaving it out unless its value is an infinity
+    // or NaN.  careful: such values of steps that only some columns see are kept out
+    // of the product and added to the columns that see them.
+    template <bool kCareful>
+    __device__ __forceinline__ void run(int i0, int i1) {
+        const float c = a.scale * kLog2e;
+        const int h = l >> 5;
+        m = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+        fetch_pages(i0, i1);
+        pages = next_pages;
+        has_pages = __ballot(pages >= 0);
+        int at = i0;
+        load(i0, at, 0);
+        fetch_pages(i0 + 16, i1);
+        int b = 0;
+        for (int i = i0; i < i1; ++i) {
+            const uint32_t has = (uint32_t)(has_pages >> (4 * (i - at))) & 15u;
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0070);          // this wave's loads of the step have landed
+            __builtin_amdgcn_s_barrier();                // every wave's have, and the other buffer has been read
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 - at == 16) {
+                pages = next_pages;
+                has_pages = __ballot(pages >= 0);
+                at = i + 1;
+                fetch_pages(at + 16, i1);
+            }
+            if (i + 1 < i1) load(i + 1, at, b ^ 1);
+            const unsigned char* kb = lds + b * 2 * kStage;
+            const unsigned char* vb = kb + kStage;
+            const int base = step_token(i);
+            f32x16 s[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
+                const int row = 32 * kt + (l & 31);
+#pragma unroll
+                for (int x = 0; x < NS; ++x)
+                    s[kt] = mma32x32<Fmt>(*(const u32x4*)(kb + (row * CH + ((2 * x + h) ^ k_key(row))) * 16), q[x], s[kt]);
+            }
+            const bool edge = !((base + kKeys - 1 <= p.lowest) & (has == 15u) &
+                                ((a.window == 0) | (base > p.last - a.window) | (base + kKeys <= a.n_sinks)));
+            if (edge) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int x = 32 * kt + 8 * (r >> 2) + (r & 3);
+                        const bool in = visible(base + x + 4 * h) & ((has >> (x >> 4)) & 1u);
+                        s[kt][r] = in ? s[kt][r] : -INFINITY;
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kt][r]);
+            top = max_over_halves(top) * c;
+            // (a column's maximum does not depend on the others': no value that it does not see reaches it)
+            const bool rise = top > m + kSlack;
+            if (__any(rise)) {
+                const float f = rise ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+                m = rise ? top : m;
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[d] *= f;
+            }
+            const float ref = m == -INFINITY ? 0.f : m;
+            u32x4 pw[4];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) {
+                    const uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r], c, -ref)),
+                                                  __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r + 1], c, -ref)));
+                    pw[2 * kt + (r >> 3)][(r >> 1) & 3] = x;
+                    sum = add_pair<Fmt>(x, sum);
+                }
+            {
+                // lane l reads 4 elements of token r, which the 16 lanes exchange
+                const int r = 4 * h + ((l & 15) >> 2);
+                const int e = (l & 16) + 4 * (l & 3);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        u32x4 x;
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int row = 16 * t + 8 * z + r;
+                            const u32x2 y = lds_read_tr16(vb + (row * CH + ((4 * d + (e >> 3)) ^ v_key(row))) * 16 + 2 * (e & 7));
+                            x[2 * z] = y[0];
+                            x[2 * z + 1] = y[1];
+                        }
+                        if (kCareful && edge) {
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) x[z] = finite_pair(x[z]);
+                        }
+                        o[d] = mma32x32<Fmt>(x, pw[t], o[d]);
+                    }
+            }
+            if (kCareful && edge) {
+                // the values left out above, into the columns that see them
+                for (int j = 0; j < kKeys; ++j) {
+                    // token j's weight: word 2 (j / 8) + (j % 4) / 2 of the lanes of half (j / 4) % 2
+                    const int word = 2 * (j >> 3) + ((j & 3) >> 1);
+                    uint32_t x = pw[0][0];
+#pragma unroll
+                    for (int e = 1; e < 16; ++e) x = word == e ? pw[e >> 2][e & 3] : x;
+                    x = (uint32_t)__shfl((int)x, (l & 31) + 8 * (j & 4), 64);
+                    const float pj = Fmt::to_f32(j & 1 ? hi16(x) : lo16(x));
+                    const bool in = visible(base + j) & ((has >> (j >> 4)) & 1u);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const u32x2 y = *(const u32x2*)(vb + (j * CH + ((4 * d + e) ^ v_key(j))) * 16 + 8 * h);
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const uint32_t v = z & 1 ? hi16(y[z >> 1]) : lo16(y[z >> 1]);
+                                const bool add = in & ((v & kExponent) == kExponent);
+                                o[d][4 * e + z] = add ? __builtin_fmaf(pj, Fmt::to_f32(v), o[d][4 * e + z]) : o[d][4 * e + z];
+                            }
+                        }
+                }
+            }
+            b ^= 1;
+        }
+        sum = sum_over_halves(sum);
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_barrier();                    // the buffers have been read
+    }
+};
+
+template <class Fmt, int DP>
+__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) lora_attn_prompt_kernel(PromptArgs pa) {
+    using Block = PromptBlock<Fmt, DP>;
+    constexpr int ND = DP / 32;
+    __shared__ __align__(16) unsigned char smem[4 * Block::kStage];
+    __shared__ int wave_n[4], at_seq, at_before, last_part, bad;
+    const AttnArgs& a = pa.a;
+    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int kh = blockIdx.x % pa.kv_heads;
+    const int rest = blockIdx.x / pa.kv_heads;
+    const int part = rest % pa.parts;
+    // row tiles of every segment in one line, the last (which see the most) first
+    auto rows_of = [&](int s, int& row0) {
+        row0 = min(max(a.seg_offset[s], 0), a.n_rows);
+        return max(min(a.seg_offset[s + 1], a.n_rows) - row0, 0);
+    };
+    auto tiles_of = [&](int s) {
+        int row0;
+        return (int)(((int64_t)rows_of(s, row0) * a.group + kCols - 1) / kCols);
+    };
+    const int per = (a.n_seqs + 255) / 256;
+    int mine = 0;
+    for (int s = t * per; s < min(t * per + per, a.n_seqs); ++s) mine += tiles_of(s);
+    int before = mine;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+        const int o = __shfl_up(before, i, 64);
+        if (l >= i) before += o;
+    }
+    if (l == 63) wave_n[w] = before;
+    if (t == 0) bad = 0;
+    __syncthreads();
+    int tiles = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        before += i < w ? wave_n[i] : 0;
+        tiles += wave_n[i];
+    }
+    before -= mine;
+    const int tile = tiles - 1 - rest / pa.parts;
+    if (tile < 0) return;
+    if (tile >= before && tile < before + mine) {
+        int s = t * per, b = before;
+        for (;;) {
+            const int n = tiles_of(s);
+            if (tile < b + n) break;
+            b += n;
+            ++s;
+        }
+        at_seq = s;
+        at_before = b;
+    }
+    __syncthreads();
+    PromptTile p;
+    p.seq = __builtin_amdgcn_readfirstlane(at_seq);
+    p.n = __builtin_amdgcn_readfirstlane(rows_of(p.seq, p.row0));
+    p.row0 = __builtin_amdgcn_readfirstlane(p.row0);
+    p.col0 = (tile - __builtin_amdgcn_readfirstlane(at_before)) * kCols;
+    p.pos0 = __builtin_amdgcn_readfirstlane(kv_len(a.lens, p.seq, a.max_len)) - p.n;
+    p.lowest = p.pos0 + p.col0 / a.group;
+    p.last = p.pos0 + min((p.col0 + kCols - 1) / a.group, p.n - 1);
+    p.first = a.window ? max(0, p.lowest - a.window + 1) : 0;
+    p.sinks = min(a.n_sinks, p.first);
+    p.sink_steps = (p.sinks + kKeys - 1) / kKeys;
+    p.win_step = max(p.first / kKeys, p.sink_steps);
+    p.steps = p.last < 0 ? 0 : max(0, p.sink_steps + p.last / kKeys + 1 - p.win_step);
+    const int col = p.col0 + 32 * w + (l & 31);
+    const int row = col / a.group, head = kh * a.group + col - row * a.group;
+    const bool real = row < p.n;
+    Block blk(pa, p, smem, kh, real ? p.pos0 + row : -1);
+    {
+        const uint16_t* qr = a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim;
+#pragma unroll
+        for (int x = 0; x < Block::NS; ++x) {
+            const int d = 16 * x + 8 * (l >> 5);
+            blk.q[x] = u32x4{0u, 0u, 0u, 0u};
+            if (real && d < a.head_dim) blk.q[x] = *(const u32x4*)(qr + d);
+        }
+    }
+    const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
+    blk.template run<false>(i0, i1);
+    // a value that is not finite: it may come from a token that the column does not see
+    float worst = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) worst += blk.o[d][r] * 0.f;
+    if (!(worst == 0.f)) bad = 1;
+    __syncthreads();
+    if (bad) blk.template run<true>(i0, i1);
+    if (pa.parts > 1) {
+        constexpr int PF = part_floats(DP);
+        const int64_t slot = (int64_t)(kh + pa.kv_heads * (rest / pa.parts)) * pa.parts;
+        const rsrc_t r = make_rsrc(pa.slots + (slot + part) * PF, PF * 4u);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                bstore16<kCoherent>(u32x4{__float_as_uint(blk.o[d][4 * e]), __float_as_uint(blk.o[d][4 * e + 1]),
+                                          __float_as_uint(blk.o[d][4 * e + 2]), __float_as_uint(blk.o[d][4 * e + 3])},
+                                    r, ((4 * d + e) * 256 + t) * 16);
+        if (l < 32) bstore8<kCoherent>(u32x2{__float_as_uint(blk.m), __float_as_uint(blk.sum)}, r,
+                                       (kCols * DP + 2 * (32 * w + l)) * 4);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        uint32_t* counter = pa.counters + kh + pa.kv_heads * (rest / pa.parts);
+        if (t == 0)
+            last_part = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                        (uint32_t)(pa.parts - 1);
+        __syncthreads();
+        if (!last_part) return;
+        if (t == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        blk.m = -INFINITY;
+        blk.sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) blk.o[d][x] = 0.f;
+        for (int z = 0; z < pa.parts; ++z) {
+            const rsrc_t r2 = make_rsrc(pa.slots + (slot + z) * PF, PF * 4u);
+            const u32x2 ms = bload8<kCoherent>(r2, (kCols * DP + 2 * (32 * w + (l & 31))) * 4);
+            const float m1 = __uint_as_float(ms[0]), mn = fmaxf(blk.m, m1), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = __builtin_amdgcn_exp2f(blk.m - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
+            blk.m = mn;
+            blk.sum = blk.sum * f0 + __uint_as_float(ms[1]) * f1;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 y = as_f4(bload16<kCoherent>(r2, ((4 * d + e) * 256 + t) * 16));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) blk.o[d][4 * e + x] = blk.o[d][4 * e + x] * f0 + y[x] * f1;
+                }
+        }
+    }
+    if (!real) return;
+    const float f = blk.sum != 0.f ? 1.f / blk.sum : 0.f;
+    uint16_t* dst = a.out + (p.row0 + row) * a.ldo + (int64_t)head * a.head_dim + 4 * (l >> 5);
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int x = 32 * d + 8 * e;
+            if (x < a.head_dim)
+                *(u32x2*)(dst + x) = u32x2{Fmt::pack2(blk.o[d][4 * e] * f, blk.o[d][4 * e + 1] * f),
+                                           Fmt::pack2(blk.o[d][4 * e + 2] * f, blk.o[d][4 * e + 3] * f)};
+        }
+}
+
+template <int DP>
+void launch_prompt(const PromptArgs& p, int dtype, unsigned blocks, hipStream_t st) {
+    if (dtype == LORA_F16)
+        hipLaunchKernelGGL((lora_attn_prompt_kernel<FmtF16, DP>), dim3(blocks), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((lora_attn_prompt_kernel<FmtBF16, DP>), dim3(blocks), dim3(256), 0, st, p);
 }
 
 // ---------------------------------------------------------------------------
@@ -576,6 +1015,14 @@ AttnArgs attn_args(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     return a;
 }
 
+// Parts that a row tile's tokens are cut into, so that `tiles` of them fill the
+// chip: at least 4 steps each, and no more than there are slots.
+int prompt_parts(const lora_attn_s* h, int64_t tiles, int32_t max_len) {
+    const int64_t fill = 2 * (int64_t)h->n_cu / std::max<int64_t>(1, tiles);
+    const int64_t most = (max_len + 4 * kKeys - 1) / (4 * kKeys);
+    return (int)std::max<int64_t>(1, std::min(fill, most));
+}
+
 struct HandleDevice {
     int prev = -1;
     bool ok = false;
@@ -611,7 +1058,8 @@ int lora_attn_create(lora_attn_t* out, int device, void* stream) {
     const size_t n_counters = (size_t)n_cu * decode_per_cu(64);
     size_t n_floats = 0;
     for (int dp = 64; dp <= 256; dp *= 2)
-        n_floats = std::max(n_floats, (size_t)n_cu * decode_per_cu(dp) * 2 * slot_floats(dp));
+        n_floats = std::max({n_floats, (size_t)n_cu * decode_per_cu(dp) * 2 * slot_floats(dp),
+                             (size_t)n_cu * 2 * part_floats(dp)});
     hipError_t e = hipMalloc((void**)&h->counters, n_counters * 4);
     if (e == hipSuccess) e = hipMalloc((void**)&h->slots, n_floats * 4);
     if (e != hipSuccess) {
@@ -676,10 +1124,20 @@ int lora_attn_prompt(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     HandleDevice g(h->device);
     if (!g.ok) return set_error(LORA_E_HIP, "lora_attn_prompt: cannot select the device");
     const AttnArgs a = attn_args(c, layer, s, seg_offset, n_rows, n_heads, q, ldq, out, ldo, scale, window, n_sinks);
-    if (c->dtype == LORA_F16)
-        hipLaunchKernelGGL(lora_attn_row_kernel<FmtF16>, dim3(n_rows, n_heads), dim3(64), 0, (hipStream_t)stream, a);
-    else
-        hipLaunchKernelGGL(lora_attn_row_kernel<FmtBF16>, dim3(n_rows, n_heads), dim3(64), 0, (hipStream_t)stream, a);
+    PromptArgs pa;
+    pa.a = a;
+    pa.counters = h->counters;
+    pa.slots = h->slots;
+    pa.kv_heads = c->n_kv_heads;
+    // row tiles: every segment's last may be partly filled
+    const int64_t cols = (int64_t)n_rows * a.group;
+    const int64_t tiles = std::min((cols + (int64_t)s->n_seqs * (kCols - 1)) / kCols, cols);
+    pa.parts = prompt_parts(h, tiles * pa.kv_heads, s->max_len);
+    const int64_t blocks = tiles * pa.kv_heads * pa.parts;
+    if (blocks > 0x7fffff) return set_error(LORA_E_SHAPE, "lora_attn_prompt: too many rows");
+    if (c->head_dim <= 64) launch_prompt<64>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
+    else if (c->head_dim <= 128) launch_prompt<128>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
+    else launch_prompt<256>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
     return check_launch("lora_attn_prompt");
 }
 
