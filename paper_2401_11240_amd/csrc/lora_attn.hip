@@ -77,9 +77,9 @@ constexpr int slot_floats(int dp) { return kHeads * dp + 2 * kHeads; }
 struct Span {
     int len, first, sinks, sink_tiles, win_tile, n;
 };
-__device__ __forceinline__ Span decode_span(const AttnArgs& a, int s) {
+__device__ __forceinline__ Span decode_span(const AttnArgs& a, int len) {
     Span p;
-    p.len = kv_len(a.lens, s, a.max_len);
+    p.len = len;
     p.first = a.window ? max(0, p.len - a.window) : 0;
     p.sinks = min(a.n_sinks, p.first);
     p.sink_tiles = (p.sinks + kTile - 1) / kTile;
@@ -291,58 +291,37 @@ __global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kerne
     constexpr int LD = DP + 4;
     __shared__ float lo[4][kHeads][LD];
     __shared__ float lm[4][kHeads], ls[4][kHeads];
-    __shared__ int wave_n[4], wave_max[4], at_seq, at_before, last;
+    __shared__ int last;
     const AttnArgs& a = d.a;
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    // the line of all tiles: tiles of the sequences before each
-    const int per = (a.n_seqs + 255) / 256;
-    int mine = 0, longest = 0;
-    for (int s = t * per; s < min(t * per + per, a.n_seqs); ++s) {
-        const int n = decode_span(a, s).n;
-        mine += n;
-        longest = max(longest, n);
+    // the line of all tiles; each wave finds its own way: lane l has sequences per l on
+    const int per = (a.n_seqs + 63) / 64;
+    int s = l * per, len = 0, mine = 0;
+    if (s < a.n_seqs) {
+        len = kv_len(a.lens, s, a.max_len);
+        mine = decode_span(a, len).n;
     }
-    int before = mine;
+    for (int x = s + 1; x < min(s + per, a.n_seqs); ++x) mine += decode_span(a, kv_len(a.lens, x, a.max_len)).n;
+    int seq_before = mine;                 // tiles of the sequences before
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
-        const int o = __shfl_up(before, i, 64);
-        if (l >= i) before += o;
-        longest = max(longest, __shfl_xor(longest, i, 64));
+        const int o = __shfl_up(seq_before, i, 64);
+        if (l >= i) seq_before += o;
     }
-    if (l == 63) {
-        wave_n[w] = before;
-        wave_max[w] = longest;
-    }
-    __syncthreads();
-    int tiles = 0;
-    longest = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        before += i < w ? wave_n[i] : 0;
-        tiles += wave_n[i];
-        longest = max(longest, wave_max[i]);
-    }
-    before -= mine;
-    const int64_t total = (int64_t)tiles * d.heads_per_seq;
-    int64_t R = (total + gridDim.x - 1) / gridDim.x;
+    const int64_t total = (int64_t)__builtin_amdgcn_readlane(seq_before, 63) * d.heads_per_seq;
+    const int64_t R = (total + gridDim.x - 1) / gridDim.x;
     const int64_t start = blockIdx.x * R;
     if (start >= total) return;
     const int at = (int)(start / d.heads_per_seq);
-    if (at >= before && at < before + mine) {
-        int s = t * per, b = before;
-        for (;;) {
-            const int n = decode_span(a, s).n;
-            if (at < b + n) break;
-            b += n;
-            ++s;
-        }
-        at_seq = s;
-        at_before = b;
+    seq_before -= mine;
+    const int lane = __builtin_ctzll(__ballot(at >= seq_before && at < seq_before + mine));
+    seq_before = __builtin_amdgcn_readlane(seq_before, lane);
+    s = __builtin_amdgcn_readlane(s, lane);
+    Span p = decode_span(a, __builtin_amdgcn_readlane(len, lane));
+    while (at >= seq_before + p.n) {       // one of the lane's others
+        seq_before += p.n;
+        p = decode_span(a, __builtin_amdgcn_readfirstlane(kv_len(a.lens, ++s, a.max_len)));
     }
-    __syncthreads();
-    int s = __builtin_amdgcn_readfirstlane(at_seq);
-    int seq_before = __builtin_amdgcn_readfirstlane(at_before);
-    Span p = decode_span(a, s);
     int hs, i0;
     {
         const int64_t in = start - (int64_t)seq_before * d.heads_per_seq;
@@ -450,7 +429,7 @@ __global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kerne
         if (++hs == d.heads_per_seq) {
             seq_before += p.n;
             hs = 0;
-            p = decode_span(a, ++s);
+            p = decode_span(a, __builtin_amdgcn_readfirstlane(kv_len(a.lens, ++s, a.max_len)));
         }
         __syncthreads();                   // lo, lm, ls have been read
     }
@@ -489,6 +468,8 @@ struct PromptArgs {
     int32_t parts;                         // workgroups that share a tile's tokens
 };
 
+// Workgroups per compute unit: what the registers allow.
+constexpr int prompt_per_cu(int dp) { return dp == 256 ? 1 : dp == 128 ? 2 : 3; }
 // Floats of a partial result: the outputs, then maximum and sum of every column.
 constexpr int part_floats(int dp) { return kCols * dp + 2 * kCols; }
 
@@ -539,11 +520,19 @@ __device__ __forceinline__ u32x4 uniform_rsrc(const void* base, uint32_t bytes) 
     return r;
 }
 
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // Transposing read: lane j of each 16 lanes gets element j % 4 of the 8-byte
 // values that lanes j / 4, 4 + j / 4, 8 + j / 4 and 12 + j / 4 address.
-__device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds_u8*)p));
+__device__ __forceinline__ u32x2 lds_read_tr16(uint32_t at) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at));
+}
+
+// s_waitcnt vmcnt(N), the other counters left free.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+    static_assert(N >= 0 && N < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
 // The larger of v in lane l and lane l ^ 32, in both; their sum.
@@ -571,7 +560,10 @@ struct PromptBlock {
     static constexpr int CH = DP / 8;      // 16-byte chunks of a token
     static constexpr int NS = DP / 16;     // MFMA steps of a score
     static constexpr int ND = DP / 32;     // 32-row blocks of the output
+    static constexpr int KD = 2;           // MFMA steps of a score read ahead from LDS
+    static constexpr int VD = 4;           // products with V read ahead from LDS
     static constexpr int NL = CH / 4;      // loads of K (and of V) per wave and step
+    static constexpr int NVO = CH == 32 ? 2 : 1;     // see vo
     static constexpr int kStage = kKeys * CH * 16;   // bytes of K (or V) of a step
     const PromptArgs& pa;
     const AttnArgs& a;
@@ -582,10 +574,17 @@ struct PromptBlock {
     u32x4 q[NS];
     f32x16 o[ND];
     float m, sum;
-    uint32_t ko[NL], vo[NL];               // byte offsets of this lane's chunks in its 16 tokens; kOut past the head
-    uint32_t row_bytes, page_bytes, lbase;
+    // byte offsets of this lane's chunks in its 16 tokens, kOut past the head; of V only
+    // those that differ by more than whole tokens
+    uint32_t ko[NL], vo[NVO];
+    uint32_t row_bytes, lbase;
+    uint32_t ka, va[ND];                   // see set_reads()
     int pages, next_pages;                 // lane 4 t + g: page of tokens 16 g on of step t of 16, -1 for none seen
     uint64_t has_pages;                    // which of pages there are
+    int pages_at, pages_end;               // the first step of pages; the end of this run's
+    int k_page;                            // this wave's page of the step whose K was loaded last
+    uint32_t has_load;                     // which pages there are of the four of the step whose K came last
+    float c, top;                          // scale in powers of two; the step's largest score
 
     __device__ __forceinline__ PromptBlock(const PromptArgs& args, const PromptTile& tile, unsigned char* smem, int kv_head,
                                            int position)
@@ -593,13 +592,12 @@ struct PromptBlock {
           w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), pos(position) {
         lbase = (uint32_t)(uintptr_t)(lds_u8*)smem;
         row_bytes = (uint32_t)a.row_stride * 2u;
-        page_bytes = ((1u << a.page_shift) - 1) * row_bytes + (uint32_t)a.head_dim * 2u;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int at = i * 64 + l, r = at / CH;
             const int kc = (at % CH) ^ k_key(r), vc = (at % CH) ^ v_key(r);
             ko[i] = 8 * kc < a.head_dim ? r * row_bytes + 16u * kc : (uint32_t)kOut;
-            vo[i] = 8 * vc < a.head_dim ? r * row_bytes + 16u * vc : (uint32_t)kOut;
+            if (i < NVO) vo[i] = 8 * vc < a.head_dim ? r * row_bytes + 16u * vc : (uint32_t)kOut;
         }
     }
     // Chunk c of token r stands in slot c ^ key(r) of its row.  K: the 16 rows
@@ -611,38 +609,76 @@ struct PromptBlock {
     __device__ __forceinline__ int step_token(int i) const {
         return (i < p.sink_steps ? i : p.win_step + i - p.sink_steps) * kKeys;
     }
-    __device__ __forceinline__ void fetch_pages(int i, int end) {
+    __device__ __forceinline__ void fetch_pages(int i) {
         const int t = i + (l >> 2), token = step_token(t) + 16 * (l & 3);
-        const bool seen = t < end && token <= p.last && (token < p.sinks || token + 15 >= p.first);
-        int page = -1;
-        if (seen) page = a.tables[(int64_t)p.seq * a.ld_table + (token >> a.page_shift)];
-        next_pages = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+        const bool seen = t < pages_end && token <= p.last && (token < p.sinks || token + 15 >= p.first);
+        next_pages = -1;
+        if (seen) next_pages = a.tables[(int64_t)p.seq * a.ld_table + (token >> a.page_shift)];
     }
-    // K and V of step i (of pages' 16 from step `at` on) into buffer b: wave w the tokens 16 w .. + 15.
-    __device__ __forceinline__ void load(int i, int at, int b) {
-        const int token = step_token(i) + 16 * w;
-        const int page = __builtin_amdgcn_readlane(pages, 4 * (i - at) + w);
-        const int64_t off = max(page, 0) * a.page_stride + kh * a.head_stride;
-        const uint32_t bytes = page < 0 ? 0u : page_bytes;
-        const u32x4 kr = uniform_rsrc(a.k + off, bytes), vr = uniform_rsrc(a.v + off, bytes);
+    __device__ __forceinline__ void turn_pages(int i) {
+        pages = (uint32_t)next_pages < (uint32_t)a.n_pages ? next_pages : -1;
+        has_pages = __ballot(pages >= 0);
+        pages_at = i;
+        fetch_pages(i + 16);
+    }
+    // 16 tokens of a step's K or V on their way to LDS: wave w takes tokens 16 w .. + 15.
+    struct Source {
+        u32x4 r;
+        uint32_t so, step, to;
+    };
+    // K or V of step i into buffer b of its kind.  Tokens past the last one that
+    // the tile sees are past the end of the resource: zeros.  (Those it does not see
+    // before a window are read, and kept out as hidden values.)
+    template <bool kV>
+    __device__ __forceinline__ Source source(int i, int page, int b) const {
+        const int token = step_token(i) + 16 * w, row = token & ((1 << a.page_shift) - 1);
+        const int rows = min((1 << a.page_shift) - 1, p.last - token + row);      // the last row of the page to read
+        Source s;
+        s.r = uniform_rsrc((kV ? a.v : a.k) + max(page, 0) * a.page_stride + kh * a.head_stride,
+                           page < 0 ? 0u : (uint32_t)rows * row_bytes + (uint32_t)a.head_dim * 2u);
         // (an empty buffer with no scalar offset, so that every offset is out of its range)
-        const uint32_t so = page < 0 ? 0u : (uint32_t)(token & ((1 << a.page_shift) - 1)) * row_bytes;
-        const uint32_t to = lbase + (uint32_t)(b * 2 * kStage + w * 16 * CH * 16);
-        if ((token + 15 <= p.last) & ((token >= p.first) | (token + 15 < p.sinks))) {
+        s.step = page < 0 ? 0u : row_bytes;
+        s.so = (uint32_t)row * s.step;
+        s.to = lbase + (uint32_t)(((kV ? 2 : 0) + b) * kStage + w * 16 * CH * 16);
+        return s;
+    }
+    template <bool kV>
+    __device__ __forceinline__ void issue(const Source& s, int j) const {
+        lds_load16(s.r, s.to + j * 1024u, kV ? vo[j % NVO] : ko[j], kV ? s.so + (j - j % NVO) * (64 / CH) * s.step : s.so);
+    }
+    // K of step i into buffer b (steps in order); V of the step whose K came last.
+    __device__ __forceinline__ Source next_k(int i, int b) {
+        if (i - pages_at == 16) turn_pages(i);
+        k_page = __builtin_amdgcn_readlane(pages, 4 * (i - pages_at) + w);
+        has_load = (uint32_t)(has_pages >> (4 * (i - pages_at))) & 15u;
+        return source<false>(i, k_page, b);
+    }
+    __device__ __forceinline__ Source next_v(int i, int b) const { return source<true>(i, k_page, b); }
+    template <bool kV>
+    __device__ __forceinline__ void issue_all(const Source& s) const {
 #pragma unroll
-            for (int j = 0; j < NL; ++j) lds_load16(kr, to + j * 1024u, ko[j], so);
+        for (int j = 0; j < NL; ++j) issue<kV>(s, j);
+    }
+
+    // LDS addresses of this lane's reads in the first buffers: K chunk l / 32 of token
+    // l % 32 (chunk 2 x + l / 32 is 2 x in the chunk's bits away); 4 elements of V's block d of token 4 (l / 32) + (l % 16) / 4, which
+    // the 16 lanes exchange.  Other tokens of the step are constants away.
+    __device__ __forceinline__ void set_reads() {
+        const int h = l >> 5, row = l & 31;
+        ka = lbase + (row * CH + (h ^ k_key(row))) * 16;
+        const int r = 4 * h + ((l & 15) >> 2), e = (l & 16) + 4 * (l & 3);
 #pragma unroll
-            for (int j = 0; j < NL; ++j) lds_load16(vr, to + kStage + j * 1024u, vo[j], so);
-        } else {
-            // tokens that no row of the tile sees are not read: zeros
+        for (int d = 0; d < ND; ++d) va[d] = lbase + 2 * kStage + (r * CH + ((4 * d + (e >> 3)) ^ v_key(r))) * 16 + 2 * (e & 7);
+    }
+    __device__ __forceinline__ void read_k(u32x4 (&f)[2], int x, int b) const {
 #pragma unroll
-            for (int j = 0; j < NL; ++j) {
-                const int x = token + (j * 64 + l) / CH;
-                const bool in = (x <= p.last) & ((x >= p.first) | (x < p.sinks));
-                lds_load16(kr, to + j * 1024u, in ? ko[j] : (uint32_t)kOut, so);
-                lds_load16(vr, to + kStage + j * 1024u, in ? vo[j] : (uint32_t)kOut, so);
-            }
-        }
+        for (int kt = 0; kt < 2; ++kt) f[kt] = *(const lds_u32x4*)(uintptr_t)((ka ^ (32u * x)) + b * kStage + kt * 32 * CH * 16);
+    }
+    // V of product f: 16 tokens f / ND, output block f % ND.
+    __device__ __forceinline__ u32x4 read_v(int f, int b) const {
+        const uint32_t at = va[f % ND] + b * kStage + 16 * (f / ND) * CH * 16;
+        const u32x2 x = lds_read_tr16(at), y = lds_read_tr16(at + 8 * CH * 16);
+        return u32x4{x[0], x[1], y[0], y[1]};
     }
     __device__ __forceinline__ bool visible(int token) const {
         return (token <= pos) & ((a.window == 0) | (token > pos - a.window) | (token < a.n_sinks));
@@ -655,116 +691,197 @@ struct PromptBlock {
         return (x >> 16 & kExponent) == kExponent ? lo : lo | (x & 0xffff0000u);
     }
 
-    // Steps [i0, i1) into o, m and sum.  A token that a column does not see has
-    // weight zero, which is as good as leaving it out unless its value is an infinity
-    // or NaN.  careful: such values of steps that only some columns see are kept out
-    // of the product and added to the columns that see them.
-    template <bool kCareful>
-    __device__ __forceinline__ void run(int i0, int i1) {
-        const float c = a.scale * kLog2e;
-        const int h = l >> 5;
+    // Do all columns see all tokens of step i?
+    __device__ __forceinline__ bool all_see(int i, uint32_t has) const {
+        const int base = step_token(i);
+        return (base + kKeys - 1 <= p.lowest) & (has == 15u) &
+               ((a.window == 0) | (base > p.last - a.window) | (base + kKeys <= a.n_sinks));
+    }
+    __device__ __forceinline__ void hide(f32x16 (&s)[2], int i, uint32_t has) const {
+        const int base = step_token(i) + 4 * (l >> 5);
+        const int first = a.window ? pos - a.window + 1 : 0;              // seen: first .. pos, and the sinks
+        const uint32_t span = (uint32_t)(pos - max(first, 0)), from = (uint32_t)(base - max(first, 0));
+        const bool simple = (has == 15u) & (step_token(i) >= a.n_sinks) & (pos >= 0);
+        if (__all(simple)) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[kt][r] = from + (uint32_t)(32 * kt + 8 * (r >> 2) + (r & 3)) <= span ? s[kt][r] : -INFINITY;
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int x = 32 * kt + 8 * (r >> 2) + (r & 3);
+                    s[kt][r] = (visible(base + x) & ((has >> (x >> 4)) & 1u)) ? s[kt][r] : -INFINITY;
+                }
+        }
+    }
+    // Scores of the step whose K is in buffer b; filler(x) after the products of dimensions 16 x on.
+    template <class F>
+    __device__ __forceinline__ void score(f32x16 (&s)[2], int b, F filler) {
+        u32x4 kf[KD][2];
+#pragma unroll
+        for (int x = 0; x < KD; ++x) read_k(kf[x], x, b);
+        __builtin_amdgcn_sched_barrier(0);
+        filler(-1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < NS; ++x) {
+            const f32x16 zero = {};
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) s[kt] = mma32x32<Fmt>(kf[x % KD][kt], q[x], x ? s[kt] : zero);
+            if (x + KD < NS) read_k(kf[x % KD], x + KD, b);
+            filler(x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __device__ __forceinline__ void rescale() {
+        // (a column's maximum does not depend on the others': no value that it does not see reaches it)
+        const bool rise = top > m + kSlack;
+        if (__any(rise)) {
+            const float f = rise ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+            m = rise ? top : m;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) o[d] *= f;
+        }
+    }
+    // Weights of pair z of this lane's 32 tokens: pw[t] is the B operand of tokens 16 t on.
+    __device__ __forceinline__ void weigh_pair(const f32x16 (&s)[2], u32x4 (&pw)[4], int z, float ref) {
+        const int kt = z >> 3, r = 2 * (z & 7);
+        uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r], c, -ref)),
+                                __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r + 1], c, -ref)));
+        asm volatile("" : "+v"(x));                      // here, and not where the compiler would rather have it
+        pw[z >> 2][z & 3] = x;
+        sum = add_pair<Fmt>(x, sum);
+    }
+
+    // Step i, its K and V in buffers B; the next step's go into the other ones.
+    template <int B>
+    __device__ __forceinline__ void step(int i) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070);              // this wave's loads have landed, its reads are done;
+        __builtin_amdgcn_s_barrier();                    // every wave's
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t has = has_load;
+        const Source sk = next_k(i + 1, B ^ 1), sv = next_v(i + 1, B ^ 1);   // (past the end: zeros)
+        f32x16 s[2];
+        // the next step's loads behind the products, one at a time: each takes 16 cycles
+        // of the path into LDS, and all at once they held every wave up for 800 of
+        // a step's 3600 cycles
+        score(s, B, [&](int x) {
+#pragma unroll
+            for (int j = 2 * NL * x / NS; x >= 0 && j < 2 * NL * (x + 1) / NS; ++j) {
+                if (j < NL) issue<false>(sk, j);
+                else issue<true>(sv, j - NL);
+            }
+        });
+        u32x4 vf[VD];
+#pragma unroll
+        for (int f = 0; f < VD; ++f) vf[f] = read_v(f, B);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!all_see(i, has)) hide(s, i, has);
+        top = highest(s);
+        rescale();
+        const float ref = m == -INFINITY ? 0.f : m;
+        u32x4 pw[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) weigh_pair(s, pw, z, ref);
+        __builtin_amdgcn_sched_barrier(0);
+        // the weights of 16 tokens behind the products of the 16 before
+#pragma unroll
+        for (int f = 0; f < 4 * ND; ++f) {
+            o[f % ND] = mma32x32<Fmt>(vf[f % VD], pw[f / ND], o[f % ND]);
+            if (f + VD < 4 * ND) vf[f % VD] = read_v(f + VD, B);
+            if (f < 3 * ND) {
+#pragma unroll
+                for (int z = 4 + 4 * f / ND; z < 4 + 4 * (f + 1) / ND; ++z) weigh_pair(s, pw, z, ref);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    __device__ __forceinline__ void start(int i0, int i1) {
+        c = a.scale * kLog2e;
         m = -INFINITY;
         sum = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-        fetch_pages(i0, i1);
-        pages = next_pages;
-        has_pages = __ballot(pages >= 0);
-        int at = i0;
-        load(i0, at, 0);
-        fetch_pages(i0 + 16, i1);
-        int b = 0;
+        set_reads();
+        pages_end = i1;
+        fetch_pages(i0);
+        turn_pages(i0);
+    }
+    __device__ __forceinline__ float highest(const f32x16 (&s)[2]) const {
+        float high = s[0][0];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) high = fmaxf(high, s[kt][r]);
+        return max_over_halves(high) * c;
+    }
+    __device__ __forceinline__ void finish() {
+        sum = sum_over_halves(sum);
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_barrier();                    // the buffers have been read
+    }
+
+    // Steps [i0, i1) into o, m and sum.
+    __device__ __forceinline__ void run(int i0, int i1) {
+        start(i0, i1);
+        if (i0 < i1) {
+            issue_all<false>(next_k(i0, 0));
+            issue_all<true>(next_v(i0, 0));
+            for (int i = i0;;) {
+                step<0>(i);
+                if (++i == i1) break;
+                step<1>(i);
+                if (++i == i1) break;
+            }
+        }
+        finish();
+    }
+
+    // The same with infinities and NaN among the values.  A token that a column
+    // does not see has weight zero, which is as good as leaving it out unless its
+    // value is one of those.  Here such values, in steps that only some columns see,
+    // are kept out of the product and added to the columns that see them; the
+    // other columns' sums are made in run()'s order, to the same bits.  One step at a time.
+    __device__ __forceinline__ void run_careful(int i0, int i1) {
+        start(i0, i1);
+        const int h = l >> 5;
         for (int i = i0; i < i1; ++i) {
-            const uint32_t has = (uint32_t)(has_pages >> (4 * (i - at))) & 15u;
+            issue_all<false>(next_k(i, 0));
+            issue_all<true>(next_v(i, 0));
+            wait_vm<0>();
+            __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(0x0070);          // this wave's loads of the step have landed
-            __builtin_amdgcn_s_barrier();                // every wave's have, and the other buffer has been read
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + 1 - at == 16) {
-                pages = next_pages;
-                has_pages = __ballot(pages >= 0);
-                at = i + 1;
-                fetch_pages(at + 16, i1);
-            }
-            if (i + 1 < i1) load(i + 1, at, b ^ 1);
-            const unsigned char* kb = lds + b * 2 * kStage;
-            const unsigned char* vb = kb + kStage;
-            const int base = step_token(i);
             f32x16 s[2];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kt][r] = 0.f;
-                const int row = 32 * kt + (l & 31);
-#pragma unroll
-                for (int x = 0; x < NS; ++x)
-                    s[kt] = mma32x32<Fmt>(*(const u32x4*)(kb + (row * CH + ((2 * x + h) ^ k_key(row))) * 16), q[x], s[kt]);
-            }
-            const bool edge = !((base + kKeys - 1 <= p.lowest) & (has == 15u) &
-                                ((a.window == 0) | (base > p.last - a.window) | (base + kKeys <= a.n_sinks)));
-            if (edge) {
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int x = 32 * kt + 8 * (r >> 2) + (r & 3);
-                        const bool in = visible(base + x + 4 * h) & ((has >> (x >> 4)) & 1u);
-                        s[kt][r] = in ? s[kt][r] : -INFINITY;
-                    }
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kt][r]);
-            top = max_over_halves(top) * c;
-            // (a column's maximum does not depend on the others': no value that it does not see reaches it)
-            const bool rise = top > m + kSlack;
-            if (__any(rise)) {
-                const float f = rise ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-                m = rise ? top : m;
-                sum *= f;
-#pragma unroll
-                for (int d = 0; d < ND; ++d) o[d] *= f;
-            }
+            score(s, 0, [](int) {});
+            const bool edge = !all_see(i, has_load);
+            if (edge) hide(s, i, has_load);
+            top = highest(s);
+            rescale();
             const float ref = m == -INFINITY ? 0.f : m;
             u32x4 pw[4];
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int z = 0; z < 16; ++z) weigh_pair(s, pw, z, ref);
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) {
-                    const uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r], c, -ref)),
-                                                  __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r + 1], c, -ref)));
-                    pw[2 * kt + (r >> 3)][(r >> 1) & 3] = x;
-                    sum = add_pair<Fmt>(x, sum);
+            for (int f = 0; f < 4 * ND; ++f) {
+                u32x4 x = read_v(f, 0);
+                if (edge) {
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) x[z] = finite_pair(x[z]);
                 }
-            {
-                // lane l reads 4 elements of token r, which the 16 lanes exchange
-                const int r = 4 * h + ((l & 15) >> 2);
-                const int e = (l & 16) + 4 * (l & 3);
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        u32x4 x;
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int row = 16 * t + 8 * z + r;
-                            const u32x2 y = lds_read_tr16(vb + (row * CH + ((4 * d + (e >> 3)) ^ v_key(row))) * 16 + 2 * (e & 7));
-                            x[2 * z] = y[0];
-                            x[2 * z + 1] = y[1];
-                        }
-                        if (kCareful && edge) {
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) x[z] = finite_pair(x[z]);
-                        }
-                        o[d] = mma32x32<Fmt>(x, pw[t], o[d]);
-                    }
+                o[f % ND] = mma32x32<Fmt>(x, pw[f / ND], o[f % ND]);
             }
-            if (kCareful && edge) {
-                // the values left out above, into the columns that see them
+            if (edge) {
+                const int base = step_token(i);
+                const unsigned char* vb = lds + 2 * kStage;
                 for (int j = 0; j < kKeys; ++j) {
                     // token j's weight: word 2 (j / 8) + (j % 4) / 2 of the lanes of half (j / 4) % 2
                     const int word = 2 * (j >> 3) + ((j & 3) >> 1);
@@ -773,7 +890,7 @@ struct PromptBlock {
                     for (int e = 1; e < 16; ++e) x = word == e ? pw[e >> 2][e & 3] : x;
                     x = (uint32_t)__shfl((int)x, (l & 31) + 8 * (j & 4), 64);
                     const float pj = Fmt::to_f32(j & 1 ? hi16(x) : lo16(x));
-                    const bool in = visible(base + j) & ((has >> (j >> 4)) & 1u);
+                    const bool in = visible(base + j) & ((has_load >> (j >> 4)) & 1u);
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -788,73 +905,75 @@ struct PromptBlock {
                         }
                 }
             }
-            b ^= 1;
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0070);          // the buffer has been read
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
         }
-        sum = sum_over_halves(sum);
-        __builtin_amdgcn_s_waitcnt(0);
-        __builtin_amdgcn_s_barrier();                    // the buffers have been read
+        finish();
     }
 };
 
 template <class Fmt, int DP>
-__global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) lora_attn_prompt_kernel(PromptArgs pa) {
+__global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kernel(PromptArgs pa) {
     using Block = PromptBlock<Fmt, DP>;
     constexpr int ND = DP / 32;
-    __shared__ __align__(16) unsigned char smem[4 * Block::kStage];
-    __shared__ int wave_n[4], at_seq, at_before, last_part, bad;
+    __shared__ __align__(1024) unsigned char smem[4 * Block::kStage];   // (rows of 512 bytes whose chunks are told apart by XOR)
+    __shared__ int last_part, bad;
     const AttnArgs& a = pa.a;
     const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
     const int kh = blockIdx.x % pa.kv_heads;
     const int rest = blockIdx.x / pa.kv_heads;
     const int part = rest % pa.parts;
-    // row tiles of every segment in one line, the last (which see the most) first
+    if (t == 0) bad = 0;                   // (run() has barriers)
+    // row tiles of every segment in one line, the last (which see the most) first;
+    // each wave finds its own way: lane l has segments per l on
+    const int per = (a.n_seqs + 63) / 64;
     auto rows_of = [&](int s, int& row0) {
-        row0 = min(max(a.seg_offset[s], 0), a.n_rows);
-        return max(min(a.seg_offset[s + 1], a.n_rows) - row0, 0);
+        const int lo = a.seg_offset[s], hi = a.seg_offset[s + 1];
+        row0 = min(max(lo, 0), a.n_rows);
+        return max(min(hi, a.n_rows) - row0, 0);
     };
-    auto tiles_of = [&](int s) {
-        int row0;
-        return (int)(((int64_t)rows_of(s, row0) * a.group + kCols - 1) / kCols);
-    };
-    const int per = (a.n_seqs + 255) / 256;
-    int mine = 0;
-    for (int s = t * per; s < min(t * per + per, a.n_seqs); ++s) mine += tiles_of(s);
+    auto tiles_of = [&](int n) { return (int)(((int64_t)n * a.group + kCols - 1) / kCols); };
+    PromptTile p;
+    int seq = l * per, row0 = 0, n = 0, len = 0, mine = 0;     // the lane's first segment, or the one found
+    if (seq < a.n_seqs) {
+        n = rows_of(seq, row0);
+        len = kv_len(a.lens, seq, a.max_len);
+        mine = tiles_of(n);
+    }
+    for (int s = seq + 1; s < min(seq + per, a.n_seqs); ++s) {
+        int r;
+        mine += tiles_of(rows_of(s, r));
+    }
     int before = mine;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
         const int o = __shfl_up(before, i, 64);
         if (l >= i) before += o;
     }
-    if (l == 63) wave_n[w] = before;
-    if (t == 0) bad = 0;
-    __syncthreads();
-    int tiles = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        before += i < w ? wave_n[i] : 0;
-        tiles += wave_n[i];
-    }
-    before -= mine;
-    const int tile = tiles - 1 - rest / pa.parts;
+    const int tile = __builtin_amdgcn_readlane(before, 63) - 1 - rest / pa.parts;
     if (tile < 0) return;
-    if (tile >= before && tile < before + mine) {
-        int s = t * per, b = before;
-        for (;;) {
-            const int n = tiles_of(s);
-            if (tile < b + n) break;
-            b += n;
-            ++s;
-        }
-        at_seq = s;
-        at_before = b;
+    before -= mine;
+    const uint64_t here = __ballot(tile >= before && tile < before + mine);
+    const int lane = __builtin_ctzll(here);
+    before = __builtin_amdgcn_readlane(before, lane);
+    p.seq = __builtin_amdgcn_readlane(seq, lane);
+    p.row0 = __builtin_amdgcn_readlane(row0, lane);
+    p.n = __builtin_amdgcn_readlane(n, lane);
+    len = __builtin_amdgcn_readlane(len, lane);
+    if (per > 1 && tile >= before + tiles_of(p.n)) {           // one of the lane's others
+        do {
+            before += tiles_of(p.n);
+            p.n = rows_of(++p.seq, p.row0);
+        } while (tile >= before + tiles_of(p.n));
+        len = kv_len(a.lens, p.seq, a.max_len);
+        p.n = __builtin_amdgcn_readfirstlane(p.n);
+        p.row0 = __builtin_amdgcn_readfirstlane(p.row0);
+        len = __builtin_amdgcn_readfirstlane(len);
     }
-    __syncthreads();
-    PromptTile p;
-    p.seq = __builtin_amdgcn_readfirstlane(at_seq);
-    p.n = __builtin_amdgcn_readfirstlane(rows_of(p.seq, p.row0));
-    p.row0 = __builtin_amdgcn_readfirstlane(p.row0);
-    p.col0 = (tile - __builtin_amdgcn_readfirstlane(at_before)) * kCols;
-    p.pos0 = __builtin_amdgcn_readfirstlane(kv_len(a.lens, p.seq, a.max_len)) - p.n;
+    p.col0 = (tile - before) * kCols;
+    p.pos0 = len - p.n;
     p.lowest = p.pos0 + p.col0 / a.group;
     p.last = p.pos0 + min((p.col0 + kCols - 1) / a.group, p.n - 1);
     p.first = a.window ? max(0, p.lowest - a.window + 1) : 0;
@@ -876,7 +995,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) lora_attn_prompt_kerne
         }
     }
     const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
-    blk.template run<false>(i0, i1);
+    blk.run(i0, i1);
     // a value that is not finite: it may come from a token that the column does not see
     float worst = 0.f;
 #pragma unroll
@@ -885,7 +1004,7 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) lora_attn_prompt_kerne
         for (int r = 0; r < 16; ++r) worst += blk.o[d][r] * 0.f;
     if (!(worst == 0.f)) bad = 1;
     __syncthreads();
-    if (bad) blk.template run<true>(i0, i1);
+    if (bad) blk.run_careful(i0, i1);
     if (pa.parts > 1) {
         constexpr int PF = part_floats(DP);
         const int64_t slot = (int64_t)(kh + pa.kv_heads * (rest / pa.parts)) * pa.parts;
@@ -932,18 +1051,29 @@ __global__ void __launch_bounds__(256, DP == 256 ? 1 : 2) lora_attn_prompt_kerne
                 }
         }
     }
-    if (!real) return;
+    // Out through LDS, whole rows of a head at a time: a lane holds 8 bytes here and
+    // there of its column, and storing those took 2 us of a workgroup's time.  Each
+    // wave has its own part; chunk c of column j is in slot c ^ j % 16 (or % 8).
+    constexpr int CH = Block::CH;
     const float f = blk.sum != 0.f ? 1.f / blk.sum : 0.f;
-    uint16_t* dst = a.out + (p.row0 + row) * a.ldo + (int64_t)head * a.head_dim + 4 * (l >> 5);
+    unsigned char* part_lds = smem + w * 32 * CH * 16;
+    constexpr int kMask = CH < 16 ? 7 : 15;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int x = 32 * d + 8 * e;
-            if (x < a.head_dim)
-                *(u32x2*)(dst + x) = u32x2{Fmt::pack2(blk.o[d][4 * e] * f, blk.o[d][4 * e + 1] * f),
-                                           Fmt::pack2(blk.o[d][4 * e + 2] * f, blk.o[d][4 * e + 3] * f)};
-        }
+        for (int e = 0; e < 4; ++e)
+            *(u32x2*)(part_lds + ((l & 31) * CH + ((4 * d + e) ^ (l & kMask))) * 16 + 8 * (l >> 5)) =
+                u32x2{Fmt::pack2(blk.o[d][4 * e] * f, blk.o[d][4 * e + 1] * f),
+                      Fmt::pack2(blk.o[d][4 * e + 2] * f, blk.o[d][4 * e + 3] * f)};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    const int64_t to = real ? (p.row0 + row) * a.ldo + (int64_t)head * a.head_dim : -1;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+        const int j = i * (64 / CH) + l / CH, ch = l % CH;     // column, chunk
+        const int64_t at = (int64_t)(uint32_t)__shfl((int)(uint32_t)to, j, 64) | (int64_t)__shfl((int)(to >> 32), j, 64) << 32;
+        const u32x4 y = *(const u32x4*)(part_lds + (j * CH + (ch ^ (j & kMask))) * 16);
+        if (at >= 0 && 8 * ch < a.head_dim) *(u32x4*)(a.out + at + 8 * ch) = y;
+    }
 }
 
 template <int DP>
