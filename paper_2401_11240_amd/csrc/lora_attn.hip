@@ -24,8 +24,8 @@
 //
 //   Join: a head's partial results (float32 sums with their maximum) of the
 //   four waves meet in LDS, those of several workgroups in device memory: the
-//   last one to arrive, counted by an atomic, adds them up in the order of the
-//   tokens, so the result does not depend on timing.
+//   last one to arrive, counted by an atomic, adds them up, in an order that
+//   does not depend on which one that is.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -44,7 +44,7 @@ constexpr int decode_per_cu(int dp) { return dp == 256 ? 1 : dp == 128 ? 3 : 4; 
 struct lora_attn_s {
     int device = 0;
     int n_cu = 0;
-    uint32_t* counters = nullptr;          // one per workgroup of a decode launch: partial results that have arrived; 0 between launches
+    uint32_t* counters = nullptr;          // a cache line each: partial results that have arrived; 0 between launches
     float* slots = nullptr;                // two partial results per workgroup
 };
 
@@ -66,6 +66,13 @@ constexpr int kTile = 128;                 // tokens per tile: 32 per wave
 constexpr int kWaveTokens = 32;
 constexpr int kHeads = 16;                 // q heads per group tile (columns of the MFMA)
 constexpr float kLog2e = 1.44269504088896340736f;
+
+constexpr int kCounters = 3;               // per workgroup: see arrive()
+
+// The join gives a tile's q heads 16 threads each, of 256; what they leave goes to parts.
+__host__ __device__ constexpr int head_slots(int heads) { return heads > 8 ? 16 : heads > 4 ? 8 : heads > 2 ? 4 : heads; }
+// Parts that one workgroup joins: four for each group of threads at once, or 16.
+__host__ __device__ constexpr int join_width(int heads) { return heads > 2 ? 16 : 64 / head_slots(heads); }
 
 // One partial result in device memory: kHeads rows of the unnormalised output, then the
 // maxima and the sums.
@@ -269,9 +276,10 @@ struct DecodeWave {
         for (int t = 0; t < NV; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int i = i0; i < i1; ++i) {
             const u32x4 pw = weights(p, i);
-            // kf and vf are refilled as soon as they have been used, and not before:
-            // a second set of registers would cost more waves than it brings.
-            // (tile i1 has no pages: its loads return zeros and read nothing)
+            // kf and vf are refilled as soon as they have been used, and not before: a
+            // second set of registers costs more waves than it brings (128 sequences
+            // x 40 heads 249 against 185 us).  (tile i1 has no pages: its loads
+            // return zeros and read nothing)
             if (i + 1 - pages_at == 32) load_pages(p, s, i + 1, i1);
             __builtin_amdgcn_sched_barrier(0);
             load_k(p, kh, i + 1);
@@ -291,7 +299,7 @@ __global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kerne
     constexpr int LD = DP + 4;
     __shared__ float lo[4][kHeads][LD];
     __shared__ float lm[4][kHeads], ls[4][kHeads];
-    __shared__ int last;
+    __shared__ int last[2];
     const AttnArgs& a = d.a;
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
     // the line of all tiles; each wave finds its own way: lane l has sequences per l on
@@ -301,15 +309,26 @@ __global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kerne
         len = kv_len(a.lens, s, a.max_len);
         mine = decode_span(a, len).n;
     }
-    for (int x = s + 1; x < min(s + per, a.n_seqs); ++x) mine += decode_span(a, kv_len(a.lens, x, a.max_len)).n;
+    int longest = mine;
+    for (int x = s + 1; x < min(s + per, a.n_seqs); ++x) {
+        const int n = decode_span(a, kv_len(a.lens, x, a.max_len)).n;
+        mine += n;
+        longest = max(longest, n);
+    }
     int seq_before = mine;                 // tiles of the sequences before
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) {
         const int o = __shfl_up(seq_before, i, 64);
         if (l >= i) seq_before += o;
+        longest = max(longest, __shfl_xor(longest, i, 64));
     }
+    longest = __builtin_amdgcn_readfirstlane(longest);
     const int64_t total = (int64_t)__builtin_amdgcn_readlane(seq_before, 63) * d.heads_per_seq;
-    const int64_t R = (total + gridDim.x - 1) / gridDim.x;
+    // Tiles per workgroup: an even share, but up to 4 where that keeps a head's parts to
+    // what one workgroup joins (8 x 33 tiles of 2 heads: 18.3 us with 3 tiles each, 22.2
+    // with one).
+    const int64_t R = max((total + gridDim.x - 1) / gridDim.x,
+                          (int64_t)min(4, (longest + join_width(a.group) - 1) / join_width(a.group)));
     const int64_t start = blockIdx.x * R;
     if (start >= total) return;
     const int at = (int)(start / d.heads_per_seq);
@@ -366,44 +385,101 @@ __global__ void __launch_bounds__(256, decode_per_cu(DP)) lora_attn_decode_kerne
         }
         bool store = true;
         if (take != p.n) {
-            // a part of the head's tokens: to device memory, and on only if all parts are there
+            // a part of the head's tokens: to device memory, and on only with all parts there.
+            // Many parts are joined 16 or more at a time first, by as many workgroups: a single
+            // one took a microsecond for every few of them.
             const int64_t first = (int64_t)seq_before * d.heads_per_seq + (int64_t)hs * p.n;
-            const int w0 = (int)(first / R), w1 = (int)((first + p.n - 1) / R);
+            const int w0 = (int)(first / R), w1 = (int)((first + p.n - 1) / R);   // the head's workgroups
             constexpr int SF = slot_floats(DP);
-            const int slot = 2 * (int)blockIdx.x + (i0 == 0);
-            const rsrc_t r = make_rsrc(d.slots + (int64_t)slot * SF, SF * 4u);
-            if (head < a.group) {
+            const rsrc_t all = make_rsrc(d.slots, gridDim.x * 2u * SF * 4u);
+            // this thread's place in the partial result of workgroup w: its first part if w is w0, its last
+            auto place = [&](int x, int hh) { return ((2 * x + (x == w0)) * SF + hh * DP + e0) * 4; };
+            auto place_ms = [&](int x, int hh) { return ((2 * x + (x == w0)) * SF + kHeads * DP + 2 * hh) * 4; };
+            auto put = [&](int x) {
+                if (head < a.group) {
 #pragma unroll
-                for (int x = 0; x < NV / 4; ++x) bstore16<kCoherent>(as_u4(acc[x]), r, (h * DP + e0 + 4 * x) * 4);
-                if ((t & 15) == 0)
-                    bstore8<kCoherent>(u32x2{__float_as_uint(M), __float_as_uint(S)}, r, (kHeads * DP + 2 * h) * 4);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-            if (t == 0)
-                last = __hip_atomic_fetch_add(d.counters + w0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                       (uint32_t)(w1 - w0);
-            __syncthreads();
-            store = last;
-            if (store) {
-                if (t == 0) __hip_atomic_store(d.counters + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    for (int y = 0; y < NV / 4; ++y) bstore16<kCoherent>(as_u4(acc[y]), all, place(x, h) + 16 * y);
+                    if ((t & 15) == 0)
+                        bstore8<kCoherent>(u32x2{__float_as_uint(M), __float_as_uint(S)}, all, place_ms(x, h));
+                }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+                __builtin_amdgcn_s_waitcnt(0);           // every thread's stores have reached the device
+                __syncthreads();
+            };
+            // Is this the last of n workgroups to come here?
+            auto arrive = [&](int kind, int x, int n) {
+                if (t == 0) {
+                    uint32_t* c = d.counters + (kind * (int)gridDim.x + x) * kSyncStride;
+                    const bool r = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(n - 1);
+                    if (r) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    last[kind >> 1] = r;
+                }
+                __syncthreads();
+                return last[kind >> 1] != 0;
+            };
+            // The partial results of workgroups x0, x0 + step, .. up to x1 into M, S and acc
+            // of the threads that hold them.  Threads of heads that the tile does not have take
+            // parts as well: group k of the ng takes parts k, k + ng, .., four at a
+            // time in flight, and the groups' sums meet in LDS.
+            const int gp = head_slots(min(kHeads, a.group - g * kHeads));
+            const int ng = kHeads / gp, k = h / gp, hk = h - k * gp;
+            auto join = [&](int x0, int x1, int step) {
                 M = -INFINITY;
                 S = 0.f;
 #pragma unroll
                 for (int x = 0; x < NV / 4; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (head < a.group)
-                    for (int v = w0; v <= w1; ++v) {
-                        const rsrc_t r2 = make_rsrc(d.slots + (int64_t)(2 * v + (v == w0)) * SF, SF * 4u);
-                        const u32x2 ms = bload8<kCoherent>(r2, (kHeads * DP + 2 * h) * 4);
-                        const float m1 = __uint_as_float(ms[0]), mn = fmaxf(M, m1), ref = mn == -INFINITY ? 0.f : mn;
-                        const float f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
-                        M = mn;
-                        S = S * f0 + __uint_as_float(ms[1]) * f1;
+                auto add = [&](float m1, float s1, const f32x4 (&y)[NV / 4]) {
+                    const float mn = fmaxf(M, m1), ref = mn == -INFINITY ? 0.f : mn;
+                    const float f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
+                    M = mn;
+                    S = S * f0 + s1 * f1;
+#pragma unroll
+                    for (int x = 0; x < NV / 4; ++x) acc[x] = acc[x] * f0 + y[x] * f1;
+                };
+                for (int v = x0 + k * step; v <= x1; v += 4 * ng * step) {
+                    u32x2 ms[4];
+                    f32x4 y[4][NV / 4];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int u = v + b * ng * step;
+                        ms[b] = bload8<kCoherent>(all, u <= x1 ? place_ms(u, hk) : kOut);
 #pragma unroll
                         for (int x = 0; x < NV / 4; ++x)
-                            acc[x] = acc[x] * f0 + as_f4(bload16<kCoherent>(r2, (h * DP + e0 + 4 * x) * 4)) * f1;
+                            y[b][x] = as_f4(bload16<kCoherent>(all, u <= x1 ? place(u, hk) + 16 * x : kOut));
                     }
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        add(v + b * ng * step <= x1 ? __uint_as_float(ms[b][0]) : -INFINITY, __uint_as_float(ms[b][1]), y[b]);
+                }
+                if (ng > 1) {
+#pragma unroll
+                    for (int x = 0; x < NV / 4; ++x) *(f32x4*)&lo[0][h][e0 + 4 * x] = acc[x];
+                    if ((t & 15) == 0) {
+                        lm[0][h] = M;
+                        ls[0][h] = S;
+                    }
+                    __syncthreads();
+                    const int used = min(ng, (x1 - x0) / step + 1);
+                    for (int o = 1; o < used && k == 0; ++o) {
+                        f32x4 y[NV / 4];
+#pragma unroll
+                        for (int x = 0; x < NV / 4; ++x) y[x] = *(const f32x4*)&lo[0][o * gp + hk][e0 + 4 * x];
+                        add(lm[0][o * gp + hk], ls[0][o * gp + hk], y);
+                    }
+                }
+            };
+            const int kJoin = join_width(a.group - g * kHeads);
+            const int n = w1 - w0 + 1;
+            const int x0 = w0 + ((int)blockIdx.x - w0) / kJoin * kJoin, x1 = min(x0 + kJoin - 1, w1);
+            put(blockIdx.x);
+            store = arrive(x0 != w0, x0, x1 - x0 + 1);
+            if (store) {
+                join(x0, x1, 1);
+                if (n > kJoin) {
+                    put(x0);                             // (a barrier: what join() left in LDS has been read)
+                    store = arrive(2, w0, (n + kJoin - 1) / kJoin);
+                    if (store) join(w0, w1, kJoin);
+                }
             }
         }
         if (store && head < a.group) {
@@ -1021,7 +1097,7 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        uint32_t* counter = pa.counters + kh + pa.kv_heads * (rest / pa.parts);
+        uint32_t* counter = pa.counters + (kh + pa.kv_heads * (rest / pa.parts)) * kSyncStride;
         if (t == 0)
             last_part = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                         (uint32_t)(pa.parts - 1);
@@ -1185,7 +1261,7 @@ int lora_attn_create(lora_attn_t* out, int device, void* stream) {
     int n_cu = 0;
     if (hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n_cu < 1) n_cu = 256;
     h->n_cu = n_cu;
-    const size_t n_counters = (size_t)n_cu * decode_per_cu(64);
+    const size_t n_counters = (size_t)n_cu * decode_per_cu(64) * kCounters * kSyncStride;
     size_t n_floats = 0;
     for (int dp = 64; dp <= 256; dp *= 2)
         n_floats = std::max({n_floats, (size_t)n_cu * decode_per_cu(dp) * 2 * slot_floats(dp),
