@@ -604,6 +604,8 @@ __device__ __forceinline__ u32x2 lds_read_tr16(uint32_t at) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at));
 }
 
+// s_waitcnt lgkmcnt(0), vmcnt and expcnt left free.
+__device__ __forceinline__ void wait_lgkm0() { __builtin_amdgcn_s_waitcnt(0xC07F); }
 // s_waitcnt vmcnt(N), the other counters left free.
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -631,7 +633,10 @@ struct PromptTile {
     int first, sinks, sink_steps, win_step, steps;
 };
 
-template <class Fmt, int DP>
+// KS 1: the four waves have 32 columns each and share the tokens of a step.
+// KS 4 (launches of few columns): all have the same 32 columns, and each its own 64
+// tokens of a step of 256, which no other wave touches.
+template <class Fmt, int DP, int KS>
 struct PromptBlock {
     static constexpr int CH = DP / 8;      // 16-byte chunks of a token
     static constexpr int NS = DP / 16;     // MFMA steps of a score
@@ -640,8 +645,10 @@ struct PromptBlock {
     static constexpr int VD = 4;           // products with V read ahead from LDS
     static constexpr int NL = CH / 4;      // loads of K (and of V) per wave and step
     static constexpr int NVO = CH == 32 ? 2 : 1;     // see vo
-    static constexpr int kStage = kKeys * CH * 16;   // bytes of K (or V) of a step
-    const PromptArgs& pa;
+    static constexpr int kStage = kKeys * CH * 16;   // bytes of K (or V) of 64 tokens
+    static constexpr int kV = KS == 1 ? 2 * kStage : kStage;       // V in LDS: behind two buffers of K, or one
+    static constexpr int kLds = 4 * kStage * (KS == 1 ? 1 : 2);
+    static constexpr int kGroups = 4 * KS;           // 16-token groups of a step
     const AttnArgs& a;
     const PromptTile& p;
     unsigned char* lds;
@@ -655,18 +662,19 @@ struct PromptBlock {
     uint32_t ko[NL], vo[NVO];
     uint32_t row_bytes, lbase;
     uint32_t ka, va[ND];                   // see set_reads()
-    int pages, next_pages;                 // lane 4 t + g: page of tokens 16 g on of step t of 16, -1 for none seen
+    int pages, next_pages;                 // lane kGroups t + g: page of tokens 16 g on of step t, -1 for none seen
     uint64_t has_pages;                    // which of pages there are
     int pages_at, pages_end;               // the first step of pages; the end of this run's
     int k_page;                            // this wave's page of the step whose K was loaded last
     uint32_t has_load;                     // which pages there are of the four of the step whose K came last
     float c, top;                          // scale in powers of two; the step's largest score
 
-    __device__ __forceinline__ PromptBlock(const PromptArgs& args, const PromptTile& tile, unsigned char* smem, int kv_head,
+    __device__ __forceinline__ PromptBlock(const AttnArgs& args, const PromptTile& tile, unsigned char* smem, int kv_head,
                                            int position)
-        : pa(args), a(args.a), p(tile), lds(smem), kh(kv_head), l(threadIdx.x & 63),
+        : a(args), p(tile), lds(smem), kh(kv_head), l(threadIdx.x & 63),
           w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), pos(position) {
-        lbase = (uint32_t)(uintptr_t)(lds_u8*)smem;
+        if (KS > 1) lds += w * 2 * kStage;
+        lbase = (uint32_t)(uintptr_t)(lds_u8*)lds;
         row_bytes = (uint32_t)a.row_stride * 2u;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -682,11 +690,13 @@ struct PromptBlock {
     static __device__ __forceinline__ int k_key(int r) { return CH >= 16 ? r & 15 : (r >> 1) & 7; }
     static __device__ __forceinline__ int v_key(int r) { return CH >= 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
 
-    __device__ __forceinline__ int step_token(int i) const {
-        return (i < p.sink_steps ? i : p.win_step + i - p.sink_steps) * kKeys;
+    // The first token of step i; of this wave's 64 of it.
+    __device__ __forceinline__ int first_token(int i) const {
+        return (i < p.sink_steps ? i : p.win_step + i - p.sink_steps) * (kKeys * KS);
     }
+    __device__ __forceinline__ int step_token(int i) const { return first_token(i) + (KS == 1 ? 0 : kKeys * w); }
     __device__ __forceinline__ void fetch_pages(int i) {
-        const int t = i + (l >> 2), token = step_token(t) + 16 * (l & 3);
+        const int t = i + l / kGroups, token = first_token(t) + 16 * (l % kGroups);
         const bool seen = t < pages_end && token <= p.last && (token < p.sinks || token + 15 >= p.first);
         next_pages = -1;
         if (seen) next_pages = a.tables[(int64_t)p.seq * a.ld_table + (token >> a.page_shift)];
@@ -695,45 +705,59 @@ struct PromptBlock {
         pages = (uint32_t)next_pages < (uint32_t)a.n_pages ? next_pages : -1;
         has_pages = __ballot(pages >= 0);
         pages_at = i;
-        fetch_pages(i + 16);
+        fetch_pages(i + 64 / kGroups);
     }
-    // 16 tokens of a step's K or V on their way to LDS: wave w takes tokens 16 w .. + 15.
+    // 16 tokens of K or V, `token` on, on their way from their page to `to` in LDS.
+    // Tokens past the last one that the tile sees are past the end of the resource:
+    // zeros.  (Those it does not see before a window are read, and kept out as hidden
+    // values.)
     struct Source {
         u32x4 r;
         uint32_t so, step, to;
     };
-    // K or V of step i into buffer b of its kind.  Tokens past the last one that
-    // the tile sees are past the end of the resource: zeros.  (Those it does not see
-    // before a window are read, and kept out as hidden values.)
-    template <bool kV>
-    __device__ __forceinline__ Source source(int i, int page, int b) const {
-        const int token = step_token(i) + 16 * w, row = token & ((1 << a.page_shift) - 1);
+    __device__ __forceinline__ Source source(const uint16_t* base, int token, int page, uint32_t to) const {
+        const int row = token & ((1 << a.page_shift) - 1);
         const int rows = min((1 << a.page_shift) - 1, p.last - token + row);      // the last row of the page to read
         Source s;
-        s.r = uniform_rsrc((kV ? a.v : a.k) + max(page, 0) * a.page_stride + kh * a.head_stride,
+        s.r = uniform_rsrc(base + max(page, 0) * a.page_stride + kh * a.head_stride,
                            page < 0 ? 0u : (uint32_t)rows * row_bytes + (uint32_t)a.head_dim * 2u);
         // (an empty buffer with no scalar offset, so that every offset is out of its range)
         s.step = page < 0 ? 0u : row_bytes;
         s.so = (uint32_t)row * s.step;
-        s.to = lbase + (uint32_t)(((kV ? 2 : 0) + b) * kStage + w * 16 * CH * 16);
+        s.to = lbase + to;
         return s;
     }
-    template <bool kV>
+    // Load j of NL of a source.
+    template <bool kOfV>
     __device__ __forceinline__ void issue(const Source& s, int j) const {
-        lds_load16(s.r, s.to + j * 1024u, kV ? vo[j % NVO] : ko[j], kV ? s.so + (j - j % NVO) * (64 / CH) * s.step : s.so);
+        lds_load16(s.r, s.to + j * 1024u, kOfV ? vo[j % NVO] : ko[j], kOfV ? s.so + (j - j % NVO) * (64 / CH) * s.step : s.so);
     }
-    // K of step i into buffer b (steps in order); V of the step whose K came last.
+    template <bool kOfV>
+    __device__ __forceinline__ void issue_all(const Source& s) const {
+#pragma unroll
+        for (int j = 0; j < NL; ++j) issue<kOfV>(s, j);
+    }
+    // KS 1.  K of step i into buffer b (steps in order), wave w its tokens 16 w .. + 15;
+    // V of the step whose K came last.
     __device__ __forceinline__ Source next_k(int i, int b) {
         if (i - pages_at == 16) turn_pages(i);
         k_page = __builtin_amdgcn_readlane(pages, 4 * (i - pages_at) + w);
         has_load = (uint32_t)(has_pages >> (4 * (i - pages_at))) & 15u;
-        return source<false>(i, k_page, b);
+        return source(a.k, step_token(i) + 16 * w, k_page, (uint32_t)(b * kStage + w * 16 * CH * 16));
     }
-    __device__ __forceinline__ Source next_v(int i, int b) const { return source<true>(i, k_page, b); }
-    template <bool kV>
-    __device__ __forceinline__ void issue_all(const Source& s) const {
+    __device__ __forceinline__ Source next_v(int i, int b) const {
+        return source(a.v, step_token(i) + 16 * w, k_page, (uint32_t)(kV + b * kStage + w * 16 * CH * 16));
+    }
+    // KS 4.  This wave's 64 tokens of step i (steps in order, K before V).
+    template <bool kOfV>
+    __device__ __forceinline__ void issue_own(int i) {
+        if (!kOfV && i - pages_at == 64 / kGroups) turn_pages(i);
+        const int lane = kGroups * (i - pages_at) + 4 * w;
+        if (!kOfV) has_load = (uint32_t)(has_pages >> lane) & 15u;
 #pragma unroll
-        for (int j = 0; j < NL; ++j) issue<kV>(s, j);
+        for (int g = 0; g < 4; ++g)
+            issue_all<kOfV>(source(kOfV ? a.v : a.k, step_token(i) + 16 * g, __builtin_amdgcn_readlane(pages, lane + g),
+                                   (uint32_t)((kOfV ? kV : 0) + g * 16 * CH * 16)));
     }
 
     // LDS addresses of this lane's reads in the first buffers: K chunk l / 32 of token
@@ -744,7 +768,7 @@ struct PromptBlock {
         ka = lbase + (row * CH + (h ^ k_key(row))) * 16;
         const int r = 4 * h + ((l & 15) >> 2), e = (l & 16) + 4 * (l & 3);
 #pragma unroll
-        for (int d = 0; d < ND; ++d) va[d] = lbase + 2 * kStage + (r * CH + ((4 * d + (e >> 3)) ^ v_key(r))) * 16 + 2 * (e & 7);
+        for (int d = 0; d < ND; ++d) va[d] = lbase + kV + (r * CH + ((4 * d + (e >> 3)) ^ v_key(r))) * 16 + 2 * (e & 7);
     }
     __device__ __forceinline__ void read_k(u32x4 (&f)[2], int x, int b) const {
 #pragma unroll
@@ -855,22 +879,34 @@ struct PromptBlock {
             }
         });
         u32x4 vf[VD];
-#pragma unroll
-        for (int f = 0; f < VD; ++f) vf[f] = read_v(f, B);
+        first_v(vf, B);
         __builtin_amdgcn_sched_barrier(0);
+        u32x4 pw[4];
+        const float ref = settle(s, i, has, pw);
+        products(s, pw, vf, ref, B);
+    }
+    __device__ __forceinline__ void first_v(u32x4 (&vf)[VD], int b) const {
+#pragma unroll
+        for (int f = 0; f < VD; ++f) vf[f] = read_v(f, b);
+    }
+    // Step i's scores, those not seen hidden, against the maximum so far; the first
+    // weights.  Returns what the scores are taken relative to.
+    __device__ __forceinline__ float settle(f32x16 (&s)[2], int i, uint32_t has, u32x4 (&pw)[4]) {
         if (!all_see(i, has)) hide(s, i, has);
         top = highest(s);
         rescale();
         const float ref = m == -INFINITY ? 0.f : m;
-        u32x4 pw[4];
 #pragma unroll
         for (int z = 0; z < 4; ++z) weigh_pair(s, pw, z, ref);
         __builtin_amdgcn_sched_barrier(0);
-        // the weights of 16 tokens behind the products of the 16 before
+        return ref;
+    }
+    // The products with V, the weights of 16 tokens behind the products of the 16 before.
+    __device__ __forceinline__ void products(const f32x16 (&s)[2], u32x4 (&pw)[4], u32x4 (&vf)[VD], float ref, int b) {
 #pragma unroll
         for (int f = 0; f < 4 * ND; ++f) {
             o[f % ND] = mma32x32<Fmt>(vf[f % VD], pw[f / ND], o[f % ND]);
-            if (f + VD < 4 * ND) vf[f % VD] = read_v(f + VD, B);
+            if (f + VD < 4 * ND) vf[f % VD] = read_v(f + VD, b);
             if (f < 3 * ND) {
 #pragma unroll
                 for (int z = 4 + 4 * f / ND; z < 4 + 4 * (f + 1) / ND; ++z) weigh_pair(s, pw, z, ref);
@@ -922,19 +958,57 @@ struct PromptBlock {
         finish();
     }
 
-    // The same with infinities and NaN among the values.  A token that a column
+    // Steps [i0, i1) of a block of few columns: this wave's tokens of them, by itself.
+    __device__ __forceinline__ void run_own(int i0, int i1) {
+        start(i0, i1);
+        if (i0 < i1) {
+            issue_own<false>(i0);
+            issue_own<true>(i0);
+        }
+        for (int i = i0; i < i1; ++i) {
+            const uint32_t has = has_load;
+            __builtin_amdgcn_sched_barrier(0);
+            wait_vm<4 * NL>();                           // K has landed, V may be on its way
+            __builtin_amdgcn_sched_barrier(0);
+            f32x16 s[2];
+            score(s, 0, [](int) {});
+            wait_lgkm0();
+            if (i + 1 < i1) issue_own<false>(i + 1);     // (K has been read)
+            __builtin_amdgcn_sched_barrier(0);
+            u32x4 pw[4];
+            const float ref = settle(s, i, has, pw);
+            if (i + 1 < i1) wait_vm<4 * NL>();           // V has landed
+            else wait_vm<0>();
+            __builtin_amdgcn_sched_barrier(0);
+            u32x4 vf[VD];
+            first_v(vf, 0);
+            products(s, pw, vf, ref, 0);
+            wait_lgkm0();
+            if (i + 1 < i1) issue_own<true>(i + 1);
+        }
+        sum = sum_over_halves(sum);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0);
+    }
+
+    // The same as run() and run_own() with infinities and NaN among the values.  A token that a column
     // does not see has weight zero, which is as good as leaving it out unless its
     // value is one of those.  Here such values, in steps that only some columns see,
     // are kept out of the product and added to the columns that see them; the
-    // other columns' sums are made in run()'s order, to the same bits.  One step at a time.
+    // other columns' sums are made in the same order, to the same bits.  One step at a time.
     __device__ __forceinline__ void run_careful(int i0, int i1) {
         start(i0, i1);
         const int h = l >> 5;
         for (int i = i0; i < i1; ++i) {
-            issue_all<false>(next_k(i, 0));
-            issue_all<true>(next_v(i, 0));
+            if constexpr (KS == 1) {
+                issue_all<false>(next_k(i, 0));
+                issue_all<true>(next_v(i, 0));
+            } else {
+                issue_own<false>(i);
+                issue_own<true>(i);
+            }
             wait_vm<0>();
-            __builtin_amdgcn_s_barrier();
+            if (KS == 1) __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             f32x16 s[2];
             score(s, 0, [](int) {});
@@ -957,7 +1031,7 @@ struct PromptBlock {
             }
             if (edge) {
                 const int base = step_token(i);
-                const unsigned char* vb = lds + 2 * kStage;
+                const unsigned char* vb = lds + kV;
                 for (int j = 0; j < kKeys; ++j) {
                     // token j's weight: word 2 (j / 8) + (j % 4) / 2 of the lanes of half (j / 4) % 2
                     const int word = 2 * (j >> 3) + ((j & 3) >> 1);
@@ -983,36 +1057,46 @@ struct PromptBlock {
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_waitcnt(0x0070);          // the buffer has been read
-            __builtin_amdgcn_s_barrier();
+            if (KS == 1) __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
-        finish();
+        sum = sum_over_halves(sum);
+        __builtin_amdgcn_s_waitcnt(0);
+        if (KS == 1) __builtin_amdgcn_s_barrier();
+    }
+    // Is an output not finite?  It may come from a token that the column does not see.
+    __device__ __forceinline__ bool infinite() const {
+        float x = 0.f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x += o[d][r] * 0.f;
+        return !(x == 0.f);
+    }
+    // The queries of this lane's column at q, if there is one.
+    __device__ __forceinline__ void load_q(const uint16_t* at, bool real) {
+#pragma unroll
+        for (int x = 0; x < NS; ++x) {
+            const int d = 16 * x + 8 * (l >> 5);
+            q[x] = u32x4{0u, 0u, 0u, 0u};
+            if (real && d < a.head_dim) q[x] = *(const u32x4*)(at + d);
+        }
     }
 };
 
-template <class Fmt, int DP>
-__global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kernel(PromptArgs pa) {
-    using Block = PromptBlock<Fmt, DP>;
-    constexpr int ND = DP / 32;
-    __shared__ __align__(1024) unsigned char smem[4 * Block::kStage];   // (rows of 512 bytes whose chunks are told apart by XOR)
-    __shared__ int last_part, bad;
-    const AttnArgs& a = pa.a;
-    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int kh = blockIdx.x % pa.kv_heads;
-    const int rest = blockIdx.x / pa.kv_heads;
-    const int part = rest % pa.parts;
-    if (t == 0) bad = 0;                   // (run() has barriers)
-    // row tiles of every segment in one line, the last (which see the most) first;
-    // each wave finds its own way: lane l has segments per l on
+// Row tile `index` of the launch, of `cols` columns and with steps of `keys` tokens:
+// the tiles of all segments lie in one line, the last, which see the most, first.
+// Each wave finds its own way: lane l has segments per l on.  False past the last tile.
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int cols, int keys, int index, PromptTile& p) {
+    const int l = threadIdx.x & 63;
     const int per = (a.n_seqs + 63) / 64;
     auto rows_of = [&](int s, int& row0) {
         const int lo = a.seg_offset[s], hi = a.seg_offset[s + 1];
         row0 = min(max(lo, 0), a.n_rows);
         return max(min(hi, a.n_rows) - row0, 0);
     };
-    auto tiles_of = [&](int n) { return (int)(((int64_t)n * a.group + kCols - 1) / kCols); };
-    PromptTile p;
-    int seq = l * per, row0 = 0, n = 0, len = 0, mine = 0;     // the lane's first segment, or the one found
+    auto tiles_of = [&](int n) { return (int)(((int64_t)n * a.group + cols - 1) / cols); };
+    int seq = l * per, row0 = 0, n = 0, len = 0, mine = 0;     // the lane's first segment
     if (seq < a.n_seqs) {
         n = rows_of(seq, row0);
         len = kv_len(a.lens, seq, a.max_len);
@@ -1028,11 +1112,10 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
         const int o = __shfl_up(before, i, 64);
         if (l >= i) before += o;
     }
-    const int tile = __builtin_amdgcn_readlane(before, 63) - 1 - rest / pa.parts;
-    if (tile < 0) return;
+    const int tile = __builtin_amdgcn_readlane(before, 63) - 1 - index;
+    if (tile < 0) return false;
     before -= mine;
-    const uint64_t here = __ballot(tile >= before && tile < before + mine);
-    const int lane = __builtin_ctzll(here);
+    const int lane = __builtin_ctzll(__ballot(tile >= before && tile < before + mine));
     before = __builtin_amdgcn_readlane(before, lane);
     p.seq = __builtin_amdgcn_readlane(seq, lane);
     p.row0 = __builtin_amdgcn_readlane(row0, lane);
@@ -1048,37 +1131,40 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
         p.row0 = __builtin_amdgcn_readfirstlane(p.row0);
         len = __builtin_amdgcn_readfirstlane(len);
     }
-    p.col0 = (tile - before) * kCols;
+    p.col0 = (tile - before) * cols;
     p.pos0 = len - p.n;
     p.lowest = p.pos0 + p.col0 / a.group;
-    p.last = p.pos0 + min((p.col0 + kCols - 1) / a.group, p.n - 1);
+    p.last = p.pos0 + min((p.col0 + cols - 1) / a.group, p.n - 1);
     p.first = a.window ? max(0, p.lowest - a.window + 1) : 0;
     p.sinks = min(a.n_sinks, p.first);
-    p.sink_steps = (p.sinks + kKeys - 1) / kKeys;
-    p.win_step = max(p.first / kKeys, p.sink_steps);
-    p.steps = p.last < 0 ? 0 : max(0, p.sink_steps + p.last / kKeys + 1 - p.win_step);
+    p.sink_steps = (p.sinks + keys - 1) / keys;
+    p.win_step = max(p.first / keys, p.sink_steps);
+    p.steps = p.last < 0 ? 0 : max(0, p.sink_steps + p.last / keys + 1 - p.win_step);
+    return true;
+}
+
+template <class Fmt, int DP>
+__global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kernel(PromptArgs pa) {
+    using Block = PromptBlock<Fmt, DP, 1>;
+    constexpr int ND = DP / 32;
+    __shared__ __align__(1024) unsigned char smem[Block::kLds];   // (rows of 512 bytes whose chunks are told apart by XOR)
+    __shared__ int last_part, bad;
+    const AttnArgs& a = pa.a;
+    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int kh = blockIdx.x % pa.kv_heads;
+    const int rest = blockIdx.x / pa.kv_heads;
+    const int part = rest % pa.parts;
+    if (t == 0) bad = 0;                   // (run() has barriers)
+    PromptTile p;
+    if (!find_tile(a, kCols, kKeys, rest / pa.parts, p)) return;
     const int col = p.col0 + 32 * w + (l & 31);
     const int row = col / a.group, head = kh * a.group + col - row * a.group;
     const bool real = row < p.n;
-    Block blk(pa, p, smem, kh, real ? p.pos0 + row : -1);
-    {
-        const uint16_t* qr = a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim;
-#pragma unroll
-        for (int x = 0; x < Block::NS; ++x) {
-            const int d = 16 * x + 8 * (l >> 5);
-            blk.q[x] = u32x4{0u, 0u, 0u, 0u};
-            if (real && d < a.head_dim) blk.q[x] = *(const u32x4*)(qr + d);
-        }
-    }
+    Block blk(a, p, smem, kh, real ? p.pos0 + row : -1);
+    blk.load_q(a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim, real);
     const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
     blk.run(i0, i1);
-    // a value that is not finite: it may come from a token that the column does not see
-    float worst = 0.f;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) worst += blk.o[d][r] * 0.f;
-    if (!(worst == 0.f)) bad = 1;
+    if (blk.infinite()) bad = 1;
     __syncthreads();
     if (bad) blk.run_careful(i0, i1);
     if (pa.parts > 1) {
@@ -1104,27 +1190,35 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
         __syncthreads();
         if (!last_part) return;
         if (t == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const rsrc_t all = make_rsrc(pa.slots + slot * PF, (uint32_t)pa.parts * PF * 4u);
+        const int at_ms = (kCols * DP + 2 * (32 * w + (l & 31))) * 4;
         blk.m = -INFINITY;
+        for (int z = 0; z < pa.parts; ++z) blk.m = fmaxf(blk.m, __uint_as_float(bload8<kCoherent>(all, z * PF * 4 + at_ms)[0]));
+        const float ref = blk.m == -INFINITY ? 0.f : blk.m;
         blk.sum = 0.f;
+        // block by block of the output, four parts in flight
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+        for (int d = 0; d < ND; ++d) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) blk.o[d][x] = 0.f;
-        for (int z = 0; z < pa.parts; ++z) {
-            const rsrc_t r2 = make_rsrc(pa.slots + (slot + z) * PF, PF * 4u);
-            const u32x2 ms = bload8<kCoherent>(r2, (kCols * DP + 2 * (32 * w + (l & 31))) * 4);
-            const float m1 = __uint_as_float(ms[0]), mn = fmaxf(blk.m, m1), ref = mn == -INFINITY ? 0.f : mn;
-            const float f0 = __builtin_amdgcn_exp2f(blk.m - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
-            blk.m = mn;
-            blk.sum = blk.sum * f0 + __uint_as_float(ms[1]) * f1;
+            for (int z = 0; z < pa.parts; z += 4) {
+                u32x2 ms[4];
+                f32x4 y[4][4];
 #pragma unroll
-            for (int d = 0; d < ND; ++d)
+                for (int b = 0; b < 4; ++b) {
+                    const int at = z + b < pa.parts ? (z + b) * PF * 4 : kOut;
+                    ms[b] = bload8<kCoherent>(all, at + at_ms);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x4 y = as_f4(bload16<kCoherent>(r2, ((4 * d + e) * 256 + t) * 16));
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) blk.o[d][4 * e + x] = blk.o[d][4 * e + x] * f0 + y[x] * f1;
+                    for (int e = 0; e < 4; ++e) y[b][e] = as_f4(bload16<kCoherent>(all, at + ((4 * d + e) * 256 + t) * 16));
                 }
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const float f = z + b < pa.parts ? __builtin_amdgcn_exp2f(__uint_as_float(ms[b][0]) - ref) : 0.f;
+                    if (d == 0) blk.sum += __uint_as_float(ms[b][1]) * f;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) blk.o[d][x] += y[b][x >> 2][x & 3] * f;
+                }
+            }
         }
     }
     // Out through LDS, whole rows of a head at a time: a lane holds 8 bytes here and
@@ -1150,6 +1244,142 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
         const u32x4 y = *(const u32x4*)(part_lds + (j * CH + (ch ^ (j & kMask))) * 16);
         if (at >= 0 && 8 * ch < a.head_dim) *(u32x4*)(a.out + at + 8 * ch) = y;
     }
+}
+
+// Launches whose tiles of 128 columns would leave most of the chip idle (one short
+// prompt, a few rows behind a long cache): tiles of 32 columns, whose tokens the four
+// waves divide and whose results meet in LDS.  One workgroup per compute unit, its
+// tokens 64 per wave in one buffer: bound by the latency of the loads, so what counts
+// is how few of them follow one another.  (203 rows of 32 heads: 9.0 us; in tiles of 128 columns 11.6 us.)
+constexpr int kFewCols = 32;
+constexpr int few_floats(int dp) { return kFewCols * dp + 2 * kFewCols; }
+
+template <class Fmt, int DP>
+__global__ void __launch_bounds__(256, 1) lora_attn_prompt_few_kernel(PromptArgs pa) {
+    using Block = PromptBlock<Fmt, DP, 4>;
+    constexpr int ND = DP / 32, CH = DP / 8, kMask = CH < 16 ? 7 : 15;
+    __shared__ __align__(1024) unsigned char smem[Block::kLds];
+    __shared__ float lm[4][kFewCols], ls[4][kFewCols];
+    __shared__ int last_part;
+    const AttnArgs& a = pa.a;
+    const int t = threadIdx.x, l = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), c = l & 31;
+    const int kh = blockIdx.x % pa.kv_heads;
+    const int rest = blockIdx.x / pa.kv_heads;
+    const int part = rest % pa.parts;
+    PromptTile p;
+    if (!find_tile(a, kFewCols, 4 * kKeys, rest / pa.parts, p)) return;
+    float M, S;
+    f32x4 y[4];                            // block w of the output of column c
+    {
+        const int col = p.col0 + c, row = col / a.group, head = kh * a.group + col - row * a.group;
+        const bool real = row < p.n;
+        Block blk(a, p, smem, kh, real ? p.pos0 + row : -1);
+        blk.load_q(a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim, real);
+        const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
+        blk.run_own(i0, i1);
+        if (__any(blk.infinite())) blk.run_careful(i0, i1);
+        // the waves' results meet: each has its own part of LDS, read by itself so far
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *(f32x4*)(blk.lds + ((4 * d + e) * 64 + l) * 16) =
+                    f32x4{blk.o[d][4 * e], blk.o[d][4 * e + 1], blk.o[d][4 * e + 2], blk.o[d][4 * e + 3]};
+        if (l < 32) {
+            lm[w][l] = blk.m;
+            ls[w][l] = blk.sum;
+        }
+    }
+    __syncthreads();
+    {
+        M = fmaxf(fmaxf(lm[0][c], lm[1][c]), fmaxf(lm[2][c], lm[3][c]));
+        const float ref = M == -INFINITY ? 0.f : M;
+        S = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = __builtin_amdgcn_exp2f(lm[i][c] - ref);
+            S += ls[i][c] * f;
+            if (w < ND)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] += *(const f32x4*)(smem + i * 2 * Block::kStage + ((4 * w + e) * 64 + l) * 16) * f;
+        }
+    }
+    if (pa.parts > 1) {
+        constexpr int PF = few_floats(DP);
+        const int slot = (kh + pa.kv_heads * (rest / pa.parts)) * pa.parts;
+        const rsrc_t all = make_rsrc(pa.slots + (int64_t)slot * PF, (uint32_t)pa.parts * PF * 4u);
+        if (w < ND)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bstore16<kCoherent>(as_u4(y[e]), all, (part * PF + ((4 * w + e) * 64 + l) * 4) * 4);
+        if (t < 32)
+            bstore8<kCoherent>(u32x2{__float_as_uint(M), __float_as_uint(S)}, all, (part * PF + kFewCols * DP + 2 * t) * 4);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_s_waitcnt(0);                   // every thread's stores have reached the device
+        __syncthreads();
+        uint32_t* counter = pa.counters + (kh + pa.kv_heads * (rest / pa.parts)) * kSyncStride;
+        if (t == 0) {
+            last_part = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                        (uint32_t)(pa.parts - 1);
+            if (last_part) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last_part) return;
+        M = -INFINITY;
+        S = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int block = min(w, ND - 1);
+        for (int z = 0; z < pa.parts; z += 4) {          // four in flight
+            u32x2 ms[4];
+            f32x4 x[4][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int at = z + b < pa.parts ? (z + b) * PF * 4 : kOut;
+                ms[b] = bload8<kCoherent>(all, at + (kFewCols * DP + 2 * c) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[b][e] = as_f4(bload16<kCoherent>(all, at + ((4 * block + e) * 64 + l) * 16));
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float m1 = z + b < pa.parts ? __uint_as_float(ms[b][0]) : -INFINITY;
+                const float mn = fmaxf(M, m1), ref = mn == -INFINITY ? 0.f : mn;
+                const float f0 = __builtin_amdgcn_exp2f(M - ref), f1 = __builtin_amdgcn_exp2f(m1 - ref);
+                M = mn;
+                S = S * f0 + __uint_as_float(ms[b][1]) * f1;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = y[e] * f0 + x[b][e] * f1;
+            }
+        }
+    }
+    // out through LDS, past the sums: chunk i of column j in slot i ^ j % 16 (or % 8)
+    const float f = S != 0.f ? 1.f / S : 0.f;
+    unsigned char* rows = smem + Block::kStage;
+    static_assert(kFewCols * DP * 4 <= Block::kStage, "the sums end before the second half of a wave's part");
+    if (w < ND)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            *(u32x2*)(rows + (c * CH + ((4 * w + e) ^ (c & kMask))) * 16 + 8 * (l >> 5)) =
+                u32x2{Fmt::pack2(y[e][0] * f, y[e][1] * f), Fmt::pack2(y[e][2] * f, y[e][3] * f)};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFewCols * CH / 256; ++i) {
+        const int at = i * 256 + t, j = at / CH, ch = at % CH;
+        const int col = p.col0 + j, row = col / a.group, head = kh * a.group + col - row * a.group;
+        if (row < p.n && 8 * ch < a.head_dim)
+            *(u32x4*)(a.out + (p.row0 + row) * a.ldo + (int64_t)head * a.head_dim + 8 * ch) =
+                *(const u32x4*)(rows + (j * CH + (ch ^ (j & kMask))) * 16);
+    }
+}
+
+template <int DP>
+void launch_prompt_few(const PromptArgs& p, int dtype, unsigned blocks, hipStream_t st) {
+    if (dtype == LORA_F16)
+        hipLaunchKernelGGL((lora_attn_prompt_few_kernel<FmtF16, DP>), dim3(blocks), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((lora_attn_prompt_few_kernel<FmtBF16, DP>), dim3(blocks), dim3(256), 0, st, p);
 }
 
 template <int DP>
@@ -1221,12 +1451,12 @@ AttnArgs attn_args(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     return a;
 }
 
-// Parts that a row tile's tokens are cut into, so that `tiles` of them fill the
-// chip: at least 4 steps each, and no more than there are slots.
-int prompt_parts(const lora_attn_s* h, int64_t tiles, int32_t max_len) {
-    const int64_t fill = 2 * (int64_t)h->n_cu / std::max<int64_t>(1, tiles);
-    const int64_t most = (max_len + 4 * kKeys - 1) / (4 * kKeys);
-    return (int)std::max<int64_t>(1, std::min(fill, most));
+// Parts that a row tile's tokens are cut into, so that `tiles` of them come near
+// `fill` workgroups: at least `least` tokens each, and 16 at most, which the last
+// workgroup to end joins.
+int prompt_parts(int64_t fill, int64_t tiles, int32_t tokens, int32_t least) {
+    const int64_t n = std::min<int64_t>({fill / std::max<int64_t>(1, tiles), tokens / least, 16});
+    return (int)std::max<int64_t>(1, n);
 }
 
 struct HandleDevice {
@@ -1337,13 +1567,25 @@ int lora_attn_prompt(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     pa.kv_heads = c->n_kv_heads;
     // row tiles: every segment's last may be partly filled
     const int64_t cols = (int64_t)n_rows * a.group;
-    const int64_t tiles = std::min((cols + (int64_t)s->n_seqs * (kCols - 1)) / kCols, cols);
-    pa.parts = prompt_parts(h, tiles * pa.kv_heads, s->max_len);
-    const int64_t blocks = tiles * pa.kv_heads * pa.parts;
+    auto tiles_of = [&](int n) { return std::min((cols + (int64_t)s->n_seqs * (n - 1)) / n, cols) * pa.kv_heads; };
+    const int dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    const int32_t tokens = window > 0 ? (int32_t)std::min<int64_t>(s->max_len, (int64_t)window + n_sinks + n_rows) : s->max_len;
+    hipStream_t st = (hipStream_t)stream;
+    // (tiles of few columns for head_dim to 128, whose tokens of four waves fit the LDS)
+    const int64_t few = tiles_of(kFewCols);
+    if (dp <= 128 && tokens > kKeys && few <= (dp == 64 ? 2 : 1) * h->n_cu && (tokens <= 1024 || few <= h->n_cu / 2)) {
+        pa.parts = prompt_parts(h->n_cu, few, tokens, 2 * 4 * kKeys);
+        if (dp == 64) launch_prompt_few<64>(pa, c->dtype, (unsigned)(few * pa.parts), st);
+        else launch_prompt_few<128>(pa, c->dtype, (unsigned)(few * pa.parts), st);
+        return check_launch("lora_attn_prompt");
+    }
+    const int64_t tiles = tiles_of(kCols);
+    pa.parts = prompt_parts(2 * (int64_t)h->n_cu, tiles, tokens, 8 * kKeys);
+    const int64_t blocks = tiles * pa.parts;
     if (blocks > 0x7fffff) return set_error(LORA_E_SHAPE, "lora_attn_prompt: too many rows");
-    if (c->head_dim <= 64) launch_prompt<64>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
-    else if (c->head_dim <= 128) launch_prompt<128>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
-    else launch_prompt<256>(pa, c->dtype, (unsigned)blocks, (hipStream_t)stream);
+    if (dp == 64) launch_prompt<64>(pa, c->dtype, (unsigned)blocks, st);
+    else if (dp == 128) launch_prompt<128>(pa, c->dtype, (unsigned)blocks, st);
+    else launch_prompt<256>(pa, c->dtype, (unsigned)blocks, st);
     return check_launch("lora_attn_prompt");
 }
 

@@ -196,6 +196,52 @@ def test_prompt_pages_and_windows(attn, page_rows, order, window, sinks):
     c.check(window, sinks, f"prompt pages of {page_rows} {order}, window {window}, sinks {sinks}")
 
 
+# Launches with so many columns that tiles of 128 are taken (those above are of tiles
+# of 32): 256 compute units of 32 columns are 8192.
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim", [("bf16", 64, 2, 128), ("f16", 72, 1, 64), ("bf16", 40, 40, 80),
+                                                      ("f16", 66, 6, 200)])
+@pytest.mark.parametrize("page_rows,order,window,sinks", [(16, "head", 0, 0), (64, "row", 100, 3), (16, "row", 33, 70),
+                                                          (256, "head", 1, 0)])
+def test_prompt_many_columns(attn, dtype, heads, kv_heads, dim, page_rows, order, window, sinks):
+    lens, rows = [200, 1, 77, 0, 130, 64], [100, 1, 77, 0, 3, 64]
+    c = Case(dtype, heads, kv_heads, dim, page_rows, lens, rows, order=order, layers=2, seed=dim + window, pad=8)
+    c.prompt(attn, window, sinks)
+    c.check(window, sinks, f"prompt of many columns {dtype} {heads}/{kv_heads} x {dim}, window {window}, sinks {sinks}")
+
+
+def test_prompt_many_columns_long(attn):
+    c = Case("bf16", 32, 4, 128, 32, [1500, 700], [260, 129], seed=21)
+    c.prompt(attn)
+    c.check(what="prompt of many columns, 1500 tokens")
+
+
+def test_many_columns_missing_pages_and_early_rows(attn):
+    drop = [(0, 0), (0, 5), (0, 11), (1, 0), (1, 1)]
+    c = Case("bf16", 64, 2, 128, 16, [200, 32, 3], [150, 32, 10], seed=22, drop=drop)
+    c.prompt(attn)
+    c.check(what="many columns, missing pages, rows before the first token")
+    o = c.got()
+    assert (o[150:182] == 0).all() and (o[182:189] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(72, 2, 64), (68, 4, 128), (64, 64, 128)])
+def test_many_columns_hidden_values(attn, dtype, bad, heads, kv_heads, dim):
+    c = Case(dtype, heads, kv_heads, dim, 16, [130], [130], seed=23)
+    c.prompt(attn)
+    clean = c.got()
+    page, row = int(c.table[0, 90 // 16]), 90 % 16
+    c.vd[c.layer][page, :, row] = bad
+    c.prompt(attn)
+    o = c.got()
+    assert np.array_equal(o[:90], clean[:90])
+    assert not np.isfinite(o[90:]).any()
+    c.kd[c.layer][page, :, row] = bad
+    c.prompt(attn)
+    assert np.array_equal(c.got()[:90], clean[:90])
+
+
 @pytest.mark.parametrize("lens,rows,heads,kv_heads,dim", [([9000], [40], 8, 2, 128), ([5000, 7000], [3, 130], 4, 1, 64),
                                                           ([6001], [9], 4, 4, 256)])
 def test_prompt_split_over_the_cache(attn, lens, rows, heads, kv_heads, dim):
