@@ -411,7 +411,6 @@ struct ForkArgs {
     BookWs w;
     int32_t* info;
     int32_t n, first;
-    int32_t release;                       // the children give back what they hold here, not in a launch before
     IdArgs pairs;
 };
 __global__ void __launch_bounds__(kBookThreads) lora_kv_fork_pages_kernel(ForkArgs a) {
@@ -424,17 +423,6 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_fork_pages_kernel(ForkAr
     const BookWs& w = a.w;
     const int t = threadIdx.x, n = a.n, first = a.first;
     int32_t* info = a.info;
-    if (a.release) {
-        for (int i = t; i < n * b.ld_table; i += kBookThreads) {
-            const int pair = i / b.ld_table, e = i - pair * b.ld_table, child = ids[2 * pair + 1];
-            const int p = b.tables[(int64_t)child * b.ld_table + e];
-            if (e < held(b, b.lens[child]) && is_page(b, p)) atomicSub(b.refs + p, 1);
-            b.tables[(int64_t)child * b.ld_table + e] = -1;
-        }
-        __threadfence();                   // (the counts are read below)
-        __syncthreads();
-        if (t < n) b.lens[ids[2 * t + 1]] = 0;
-    }
     int len, src, want = 0;
     const bool need = t < n && fork_tail(b, ids[2 * t], len, src);
     const int at = block_scan(need ? 1 : 0, wave_sum, want);
@@ -756,11 +744,8 @@ int lora_kv_fork(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, c
     static_assert(kPairs <= kBookThreads, "one thread per pair");
     const int units = 2 * d.n_layers * d.blocks;
     IdArgs ids{};
-    // Every child's pages come back before any is handed out: in the launch that
-    // hands them out if that is one and the children's entries are few (48 children of
-    // 49 entries: 17 us in all, with a launch of its own 19.6 us).
-    const bool one = n <= kPairs && (int64_t)n * b->ld_table <= 16 * kBookThreads;
-    for (int pass = one ? 1 : 0; pass < 2; ++pass)
+    // every child's pages come back before any is handed out
+    for (int pass = 0; pass < 2; ++pass)
         for (int32_t i0 = 0; i0 < n || (pass && n == 0 && i0 == 0); i0 += kPairs) {
             const int m = std::min(kPairs, n - i0);
             for (int i = 0; i < m; ++i) {
@@ -771,7 +756,7 @@ int lora_kv_fork(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, c
                 hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, book, ids, 2, 1);
             } else {
                 hipLaunchKernelGGL(lora_kv_fork_pages_kernel, dim3(1), dim3(kBookThreads), 0, st,
-                                   ForkArgs{book, w, info, m, (int)(i0 == 0), (int)one, ids});
+                                   ForkArgs{book, w, info, m, (int)(i0 == 0), ids});
                 if (m > 0)
                     hipLaunchKernelGGL(lora_kv_fork_kernel, dim3(1 + units, m), dim3(kCopyThreads), 0, st, book, d, ids, w);
             }
