@@ -117,7 +117,7 @@ int lora_kv_append(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
 
 /*
  * What attention launches share: counters and float32 partial results of
- * key ranges that several workgroups read (about 100 MB of device memory, the
+ * key ranges that several workgroups read (about 70 MB of device memory, the
  * same for every call).  Creation allocates, and waits for `stream`; it
  * refuses a capturing stream.  Launches that share one handle must be ordered
  * on one stream.  Destroying it frees the memory: no launch may still use it.

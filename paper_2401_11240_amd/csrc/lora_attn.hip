@@ -1135,7 +1135,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int cols, int keys,
     p.pos0 = len - p.n;
     p.lowest = p.pos0 + p.col0 / a.group;
     p.last = p.pos0 + min((p.col0 + cols - 1) / a.group, p.n - 1);
-    p.first = a.window ? max(0, p.lowest - a.window + 1) : 0;
+    p.first = a.window && p.lowest > 0 ? max(0, p.lowest - a.window + 1) : 0;
     p.sinks = min(a.n_sinks, p.first);
     p.sink_steps = (p.sinks + keys - 1) / keys;
     p.win_step = max(p.first / keys, p.sink_steps);
@@ -1445,8 +1445,8 @@ AttnArgs attn_args(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     a.n_heads = n_heads;
     a.group = n_heads / c->n_kv_heads;
     a.head_dim = c->head_dim;
-    a.window = window;
-    a.n_sinks = n_sinks;
+    a.window = window < s->max_len ? window : 0;    // (one that long hides nothing)
+    a.n_sinks = std::min(n_sinks, s->max_len);
     a.scale = scale;
     return a;
 }

@@ -627,6 +627,11 @@ int check_pairs(const char* from_name, const char* to_name, const int32_t* from,
     return LORA_OK;
 }
 
+int check_words(const char* what, const void* p) {
+    if ((uintptr_t)p & 3) return set_error(LORA_E_ALIGN, std::string(what) + " not 4-byte aligned");
+    return LORA_OK;
+}
+
 Book device_book(const lora_kv_book_t* b) {
     return {b->tables, b->lens, b->refs, b->n_seqs, b->ld_table, b->n_pages, log2_of(b->page_rows)};
 }
@@ -670,7 +675,7 @@ int lora_kv_append(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     if (n_rows < 0) return set_error(LORA_E_ARG, "negative n_rows");
     if (!seg_offset && n_rows != s->n_seqs)
         return set_error(LORA_E_SHAPE, "without seg_offset, n_rows must be n_seqs");
-    if ((uintptr_t)seg_offset & 3) return set_error(LORA_E_ALIGN, "seg_offset not 4-byte aligned");
+    if (int rc = check_words("seg_offset", seg_offset)) return rc;
     const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
     if (int rc = check_kv_rows("k_new", k_new, "ldk", ldk, width, n_rows)) return rc;
     if (int rc = check_kv_rows("v_new", v_new, "ldv", ldv, width, n_rows)) return rc;
@@ -717,6 +722,8 @@ int lora_kv_workspace_bytes(const lora_kv_book_t* b, size_t* bytes) {
 int lora_kv_grow(const lora_kv_book_t* b, const int32_t* add, int32_t* info, void* ws, size_t ws_bytes, void* stream) {
     if (int rc = check_book(b)) return rc;
     if (b->n_seqs > 0 && !add) return set_error(LORA_E_ARG, "add is NULL");
+    if (int rc = check_words("add", add)) return rc;
+    if (int rc = check_words("info", info)) return rc;
     if (int rc = check_ws(b, ws, ws_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
@@ -733,6 +740,7 @@ int lora_kv_fork(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, c
     if (int rc = check_book(b)) return rc;
     if (int rc = check_book_cache(c, b)) return rc;
     if (int rc = check_pairs("parent", "child", parents, children, n, b->n_seqs)) return rc;
+    if (int rc = check_words("info", info)) return rc;
     if (int rc = check_ws(b, ws, ws_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
@@ -830,6 +838,7 @@ int lora_kv_compact(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t* 
         return set_error(LORA_E_ARG, "tables_out or refs_out is NULL");
     if (((uintptr_t)tables_out | (uintptr_t)refs_out) & 3)
         return set_error(LORA_E_ALIGN, "tables_out or refs_out not 4-byte aligned");
+    if (int rc = check_words("info", info)) return rc;
     if (int rc = check_ws(b, ws, ws_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);

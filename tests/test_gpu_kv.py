@@ -368,6 +368,45 @@ def test_rising_scores(attn):
     p.check(what="rising scores, prompt")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [2, 72])
+def test_many_small_weights(attn, dtype, heads):
+    # one token has weight 1, the 3000 others about 2^-15.3 each (below binary16's
+    # normal numbers): together they are some 7% of the sum and of the output
+    n, rows = 3001, 120 if heads == 72 else 40
+    for kind in ("prompt", "decode"):
+        c = Case(dtype, heads, 1, 64, 64, [n], [rows if kind == "prompt" else 1], seed=31)
+        k = torch.zeros(c.kd[0].shape, dtype=torch.float32)
+        k[c.table[0, 0], :, 0, 0] = 15.0         # score 15 * 5.65625 / 8 = 10.6 = 15.3 powers of two
+        c.kd[0].copy_(k)
+        c.k = k.to(DTYPES[dtype]).double().numpy()
+        v = torch.where(torch.isnan(c.vd[0]), c.vd[0], c.vd[0].abs())
+        c.vd[0].copy_(v)
+        c.v = v.double().cpu().numpy()
+        c.qd.zero_()
+        c.q[:] = 0
+        for h in range(heads):
+            c.qd[:, h * 64] = 5.65625
+            c.q[:, h, 0] = 5.65625
+        getattr(c, kind)(attn)
+        c.check(what=f"{kind}, many small weights, {dtype}, {heads} heads")
+
+
+@pytest.mark.parametrize("window", [1 << 30, (1 << 31) - 1])
+def test_windows_past_every_length(attn, window):
+    c = Case("bf16", 4, 2, 64, 16, [3, 40, 300], [10, 40, 7], seed=32)
+    c.prompt(attn, window, 5)
+    c.check(what="prompt, a window longer than all")
+    c = Case("bf16", 4, 2, 64, 16, [3, 0, 300], [1, 1, 1], seed=33)
+    c.decode(attn, window, (1 << 31) - 1)
+    c.check(what="decode, a window longer than all")
+    c.decode(attn, 20, (1 << 31) - 1)
+    c.check(20, 400, "decode, all tokens sinks")
+    p = Case("bf16", 72, 1, 64, 16, [300], [200], seed=34)
+    p.prompt(attn, 20, (1 << 31) - 1)
+    p.check(20, 400, "prompt, all tokens sinks")
+
+
 def test_offsets_past_32_bits(attn):
     dim, pr, gap = 64, 16, (1 << 31) + 4096      # elements between pages: 4 GiB and some
     lens = [40, 21]

@@ -165,6 +165,8 @@ def test_bad_book_arguments():
     assert code(lib.lora_kv_grow(ref(b), P, None, None, 1 << 20, None)) == L.LORA_E_ARG
     assert code(lib.lora_kv_grow(ref(b), P, None, P + 8, 1 << 20, None)) == L.LORA_E_ALIGN
     assert code(lib.lora_kv_grow(ref(b), P, None, P, n.value - 1, None)) == L.LORA_E_WORKSPACE
+    assert code(lib.lora_kv_grow(ref(b), P + 2, None, P, 1 << 20, None)) == L.LORA_E_ALIGN
+    assert code(lib.lora_kv_grow(ref(b), P, P + 1, P, 1 << 20, None)) == L.LORA_E_ALIGN
     fork = lambda ps, cs, bb=b, cc=c: code(lib.lora_kv_fork(ref(cc), ref(bb), len(ps), arr(*ps), arr(*cs), None, P,
                                                             1 << 20, None))
     assert fork([0], [3]) == L.LORA_E_INDEX
