@@ -28,9 +28,9 @@
  *
  * over the visible tokens j < len.  A visible token whose page is outside
  * [0, n_pages) is left out.  A row for which nothing is left, or whose
- * weights are all zero, gets zeros.  Keys and values of tokens that a row does not see have no
- * effect on it, whatever they hold (NaN included); table entries of pages in
- * which no token is visible are not used.  Scores, the softmax's maximum and
+ * weights are all zero, gets zeros.  Keys and values of tokens that a row does
+ * not see have no effect on it, whatever they hold (NaN included); table
+ * entries of pages in which no token is visible are not used.  Scores, the softmax's maximum and
  * sum and the output's sums are float32; a weight is rounded to the storage
  * type for the product with V, and the sum of weights is that of the rounded
  * ones; the output is rounded once.
@@ -53,9 +53,11 @@
  *     multiples of 8 elements (no cache stride below head_dim, leading
  *     dimensions at least n_heads or n_kv_heads times head_dim);
  *   - one page's rows of one head span less than 2 GiB;
- *   - max_len <= ld_table * page_rows, scale positive and finite, window and
+ *   - max_len <= ld_table * page_rows and <= 2^30, scale positive and finite, window and
  *     n_sinks not negative;
- *   - q and out do not overlap.
+ *   - q and out do not overlap;
+ *   - a launch's tiles can be counted in 32 bits (n_seqs * n_heads *
+ *     max_len / 128 is the order of their number): LORA_E_SHAPE if not.
  *
  * Asynchrony, errors and thread safety are lora.h's: calls are enqueued on the
  * caller's stream, allocate nothing (lora_attn_create does), copy nothing to
@@ -96,10 +98,10 @@ typedef struct {
  * pages of its first ceil(len / page_rows) table entries (entries outside
  * [0, n_pages) hold none); further entries have no meaning. */
 typedef struct {
-    int32_t* tables;            /* [n_seqs, ld_table]                  */
+    int32_t* tables;            /* [n_seqs, ld_table], below 2^31 in all */
     int32_t* lens;              /* [n_seqs]                            */
     int32_t* refs;              /* [n_pages]                           */
-    int32_t n_seqs, ld_table, n_pages;   /* n_pages <= 1048576         */
+    int32_t n_seqs, ld_table, n_pages;
     int32_t page_rows;
 } lora_kv_book_t;
 
@@ -155,10 +157,11 @@ int lora_kv_workspace_bytes(const lora_kv_book_t* b, size_t* bytes);
 /*
  * lens[s] += add[s] (DEVICE array [n_seqs]; entries below 1 are read as 0) with
  * the pages that this takes: free pages in ascending order go to sequences in
- * ascending order.  A sequence whose pages do not fit (the pages taken by the
- * sequences up to and including it exceed the free ones, or its table is too
- * short) stays as it is.  info (DEVICE [2], may be NULL): pages taken,
- * sequences that stayed.
+ * ascending order.  A sequence whose table is too short stays as it is and
+ * takes nothing.  From the first whose pages exceed the free ones that are
+ * left, sequences that need a page stay as they are (a short one does not
+ * overtake), and those that need none still grow.  info (DEVICE [2], may be
+ * NULL): pages taken, sequences that stayed.
  */
 int lora_kv_grow(const lora_kv_book_t* b, const int32_t* add, int32_t* info, void* ws, size_t ws_bytes,
                  void* stream);

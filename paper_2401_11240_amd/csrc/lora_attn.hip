@@ -581,19 +581,16 @@ __device__ __forceinline__ float add_pair<FmtBF16>(uint32_t x, float s) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"   // m0 is reserved: nothing to preserve, the clobber is what is said
 __device__ __forceinline__ void lds_load16(const u32x4& r, uint32_t lds, uint32_t off, uint32_t so) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                  :: "s"(lds), "v"(off), "s"(r), "s"(so) : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// The resource of make_rsrc() as four scalar words, five wait states after the
-// vector instructions that may write them.
+// The resource of make_rsrc() as four scalar words.
 __device__ __forceinline__ u32x4 uniform_rsrc(const void* base, uint32_t bytes) {
     const uint64_t b = (uint64_t)base;
-    u32x4 r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
-               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xffffu,
-               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), (uint32_t)kRsrcWord3};
-    asm volatile("s_nop 4" : "+s"(r));
-    return r;
+    return {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
+            (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xffffu,
+            (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), (uint32_t)kRsrcWord3};
 }
 
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;

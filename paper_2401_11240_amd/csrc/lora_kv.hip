@@ -59,6 +59,7 @@ int check_kv_seqs(const lora_kv_cache_t* c, const lora_kv_seqs_t* s) {
         return set_error(LORA_E_ARG, "tables or lens is NULL");
     if ((int64_t)s->max_len > (int64_t)s->ld_table * c->page_rows)
         return set_error(LORA_E_SHAPE, "max_len exceeds ld_table * page_rows");
+    if (s->max_len > (1 << 30)) return set_error(LORA_E_SHAPE, "max_len exceeds 2^30");
     if (((uintptr_t)s->lens | (uintptr_t)s->tables) & 3) return set_error(LORA_E_ALIGN, "tables or lens not 4-byte aligned");
     return LORA_OK;
 }
@@ -569,6 +570,8 @@ int check_book(const lora_kv_book_t* b) {
     if (!b) return set_error(LORA_E_ARG, "book is NULL");
     if (b->n_seqs < 0 || b->ld_table < 0 || b->n_pages < 0)
         return set_error(LORA_E_ARG, "negative n_seqs, ld_table or n_pages");
+    if ((int64_t)b->n_seqs * b->ld_table > 0x7fffffff)   // (the page counts of a book add up in 32 bits)
+        return set_error(LORA_E_SHAPE, "the book's tables have 2^31 entries or more");
     if (b->page_rows < 16 || b->page_rows > 65536 || (b->page_rows & (b->page_rows - 1)))
         return set_error(LORA_E_SHAPE, "page_rows must be a power of two in [16, 65536]");
     if ((b->n_seqs > 0 && (!b->lens || (b->ld_table > 0 && !b->tables))) || (b->n_pages > 0 && !b->refs))

@@ -208,3 +208,22 @@ def test_tensor_descriptions_are_checked():
             KV.Seqs(bt, bn, 5)
         with pytest.raises(ValueError):
             KV.Book(bt, bn, n, 16)
+
+
+def test_loads_into_lds_wait_for_their_scalar_registers():
+    # a buffer load needs 5 wait states after a vector instruction that wrote one of
+    # its scalar registers; inside a statement only the statement itself leaves them
+    path = os.path.join(ROOT, "paper_2401_11240_amd", "csrc", "lora_attn.hip")
+    stmts = [m for m in re.findall(r'asm volatile\("([^"]*)"', open(path).read()) if "buffer_load" in m]
+    assert stmts
+    for stmt in stmts:
+        before = stmt[:stmt.index("buffer_load")]
+        assert sum(int(n) + 1 for n in re.findall(r"s_nop (\d+)", before)) >= 5, stmt
+
+
+def test_sizes_past_32_bits_are_refused():
+    lib = KV._lib()
+    b = book(n_seqs=1 << 16, ld_table=1 << 15)
+    assert code(lib.lora_kv_free(C.byref(b), 0, None, None)) == L.LORA_E_SHAPE
+    s = seqs(ld_table=1 << 27, max_len=(1 << 30) + 1)
+    assert code(lib.lora_kv_append(C.byref(cache()), 0, C.byref(s), None, 3, P, 256, P, 256, None)) == L.LORA_E_SHAPE
