@@ -576,8 +576,9 @@ __device__ __forceinline__ float add_pair<FmtBF16>(uint32_t x, float s) {
 // range) into LDS at lds + 16 * lane; lds, so and r are the same in every lane.
 // Inline assembly without an output: for the builtin the compiler waits for
 // every such load in flight before each LDS read.  A wait and a barrier order the
-// reads after it.  The wait state after the write of m0 is here, those of the
-// resource in uniform_rsrc().
+// reads after it.  The wait states are those of a scalar register that a vector
+// instruction wrote (v_readfirstlane, or v_readlane where the compiler had put it
+// aside); they cover the write of m0.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"   // m0 is reserved: nothing to preserve, the clobber is what is said
 __device__ __forceinline__ void lds_load16(const u32x4& r, uint32_t lds, uint32_t off, uint32_t so) {
@@ -710,7 +711,7 @@ struct PromptBlock {
     // values.)
     struct Source {
         u32x4 r;
-        uint32_t so, step, to;
+        uint32_t so, step, most, to;
     };
     __device__ __forceinline__ Source source(const uint16_t* base, int token, int page, uint32_t to) const {
         const int row = token & ((1 << a.page_shift) - 1);
@@ -721,13 +722,17 @@ struct PromptBlock {
         // (an empty buffer with no scalar offset, so that every offset is out of its range)
         s.step = page < 0 ? 0u : row_bytes;
         s.so = (uint32_t)row * s.step;
+        s.most = (uint32_t)rows * s.step;
         s.to = lbase + to;
         return s;
     }
-    // Load j of NL of a source.
+    // Load j of NL of a source.  (The range of a buffer is counted from its scalar offset on,
+    // which therefore stays below its end: where all tokens of a load of V are past the
+    // last one, the last stands in for the first of them, with weight zero as well.)
     template <bool kOfV>
     __device__ __forceinline__ void issue(const Source& s, int j) const {
-        lds_load16(s.r, s.to + j * 1024u, kOfV ? vo[j % NVO] : ko[j], kOfV ? s.so + (j - j % NVO) * (64 / CH) * s.step : s.so);
+        lds_load16(s.r, s.to + j * 1024u, kOfV ? vo[j % NVO] : ko[j],
+                   kOfV ? min(s.so + (j - j % NVO) * (64 / CH) * s.step, s.most) : s.so);
     }
     template <bool kOfV>
     __device__ __forceinline__ void issue_all(const Source& s) const {
@@ -1565,6 +1570,9 @@ int lora_attn_prompt(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     // row tiles: every segment's last may be partly filled
     const int64_t cols = (int64_t)n_rows * a.group;
     auto tiles_of = [&](int n) { return std::min((cols + (int64_t)s->n_seqs * (n - 1)) / n, cols) * pa.kv_heads; };
+    // (tiles are counted in 32 bits, also where device offsets are not what they should be)
+    if ((cols / kFewCols + 1) * s->n_seqs > 0x7fffffff)
+        return set_error(LORA_E_SHAPE, "lora_attn_prompt: too many rows and sequences");
     const int dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const int32_t tokens = window > 0 ? (int32_t)std::min<int64_t>(s->max_len, (int64_t)window + n_sinks + n_rows) : s->max_len;
     hipStream_t st = (hipStream_t)stream;
