@@ -101,7 +101,7 @@ typedef struct {
     int32_t* tables;            /* [n_seqs, ld_table], below 2^31 in all */
     int32_t* lens;              /* [n_seqs]                            */
     int32_t* refs;              /* [n_pages]                           */
-    int32_t n_seqs, ld_table, n_pages;
+    int32_t n_seqs, ld_table, n_pages;   /* n_pages <= 2^30            */
     int32_t page_rows;
 } lora_kv_book_t;
 

@@ -572,6 +572,7 @@ int check_book(const lora_kv_book_t* b) {
         return set_error(LORA_E_ARG, "negative n_seqs, ld_table or n_pages");
     if ((int64_t)b->n_seqs * b->ld_table > 0x7fffffff)   // (the page counts of a book add up in 32 bits)
         return set_error(LORA_E_SHAPE, "the book's tables have 2^31 entries or more");
+    if (b->n_pages > (1 << 30)) return set_error(LORA_E_SHAPE, "n_pages exceeds 2^30");
     if (b->page_rows < 16 || b->page_rows > 65536 || (b->page_rows & (b->page_rows - 1)))
         return set_error(LORA_E_SHAPE, "page_rows must be a power of two in [16, 65536]");
     if ((b->n_seqs > 0 && (!b->lens || (b->ld_table > 0 && !b->tables))) || (b->n_pages > 0 && !b->refs))
@@ -684,6 +685,10 @@ int lora_kv_append(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     if (int rc = check_kv_rows("v_new", v_new, "ldv", ldv, width, n_rows)) return rc;
     if (width > (1 << 24)) return set_error(LORA_E_SHAPE, "n_kv_heads * head_dim exceeds 2^24");
     if (n_rows == 0 || s->n_seqs == 0 || c->n_pages == 0) return LORA_OK;
+    // rows of a workgroup: two chunks per thread
+    const int group_rows = std::max(1, std::min(kAppendRows, 2 * kCopyThreads / (int)(width / 8)));
+    const int64_t blocks = ((int64_t)n_rows + group_rows - 1) / group_rows;
+    if (blocks > 0xffffff) return set_error(LORA_E_SHAPE, "lora_kv_append: too many rows");
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
     if (!g.ok) return no_device("lora_kv_append");
@@ -708,10 +713,8 @@ int lora_kv_append(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     a.page_shift = log2_of(c->page_rows);
     a.row_chunks = (int)(width / 8);
     a.dim_chunks = c->head_dim / 8;
-    // rows of a workgroup: two chunks per thread
-    a.group_rows = std::max(1, std::min(kAppendRows, 2 * kCopyThreads / a.row_chunks));
-    const int blocks = (n_rows + a.group_rows - 1) / a.group_rows;
-    hipLaunchKernelGGL(lora_kv_append_kernel, dim3(blocks), dim3(kCopyThreads), 0, st, a);
+    a.group_rows = group_rows;
+    hipLaunchKernelGGL(lora_kv_append_kernel, dim3((unsigned)blocks), dim3(kCopyThreads), 0, st, a);
     return check_launch("lora_kv_append");
 }
 

@@ -227,3 +227,9 @@ def test_sizes_past_32_bits_are_refused():
     assert code(lib.lora_kv_free(C.byref(b), 0, None, None)) == L.LORA_E_SHAPE
     s = seqs(ld_table=1 << 27, max_len=(1 << 30) + 1)
     assert code(lib.lora_kv_append(C.byref(cache()), 0, C.byref(s), None, 3, P, 256, P, 256, None)) == L.LORA_E_SHAPE
+    b = book(n_pages=(1 << 30) + 1)
+    assert code(lib.lora_kv_free(C.byref(b), 0, None, None)) == L.LORA_E_SHAPE
+    s = seqs(n_seqs=(1 << 31) - 1, ld_table=1, max_len=16)
+    c = cache(n_kv_heads=1, head_dim=128)
+    rows = (1 << 31) - 1
+    assert code(lib.lora_kv_append(C.byref(c), 0, C.byref(s), None, rows, P, 128, P, 128, None)) == L.LORA_E_SHAPE
