@@ -1570,8 +1570,8 @@ int lora_attn_prompt(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     // row tiles: every segment's last may be partly filled
     const int64_t cols = (int64_t)n_rows * a.group;
     auto tiles_of = [&](int n) { return std::min((cols + (int64_t)s->n_seqs * (n - 1)) / n, cols) * pa.kv_heads; };
-    // (tiles are counted in 32 bits, also where device offsets are not what they should be)
-    if ((cols / kFewCols + 1) * s->n_seqs > 0x7fffffff)
+    // (columns and tiles are counted in 32 bits, also where device offsets are not what they should be)
+    if (cols > 0x7fffff00 || (cols / kFewCols + 1) * s->n_seqs > 0x7fffffff)
         return set_error(LORA_E_SHAPE, "lora_attn_prompt: too many rows and sequences");
     const int dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const int32_t tokens = window > 0 ? (int32_t)std::min<int64_t>(s->max_len, (int64_t)window + n_sinks + n_rows) : s->max_len;
