@@ -646,6 +646,7 @@ struct PromptBlock {
     static constexpr int kStage = kKeys * CH * 16;   // bytes of K (or V) of 64 tokens
     static constexpr int kV = KS == 1 ? 2 * kStage : kStage;       // V in LDS: behind two buffers of K, or one
     static constexpr int kLds = 4 * kStage * (KS == 1 ? 1 : 2);
+    static constexpr bool kAcc = DP == 256 || KS == 4;   // o in accumulation registers
     static constexpr int kGroups = 4 * KS;           // 16-token groups of a step
     const AttnArgs& a;
     const PromptTile& p;
@@ -847,7 +848,13 @@ struct PromptBlock {
             m = rise ? top : m;
             sum *= f;
 #pragma unroll
-            for (int d = 0; d < ND; ++d) o[d] *= f;
+            for (int d = 0; d < ND; ++d) {
+                // (where o is in accumulation registers: without this the compiler moves all of it out
+                // of them in every step, for a product that few steps need)
+                if (kAcc) asm volatile("" : "+a"(o[d]));
+                o[d] *= f;
+                if (kAcc) asm volatile("" : "+a"(o[d]));
+            }
         }
     }
     // Weights of pair z of this lane's 32 tokens: pw[t] is the B operand of tokens 16 t on.
