@@ -1518,13 +1518,14 @@ int prompt_parts(int64_t fill, int64_t tiles, int32_t tokens, int32_t least) {
 
 struct HandleDevice {
     int prev = -1;
-    bool ok = false;
+    bool ok = false, moved = false;
     explicit HandleDevice(int device) {
         if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = prev == device || hipSetDevice(device) == hipSuccess;
+        moved = prev != device;
+        ok = !moved || hipSetDevice(device) == hipSuccess;
     }
     ~HandleDevice() {
-        if (prev >= 0) (void)hipSetDevice(prev);
+        if (moved) (void)hipSetDevice(prev);
     }
 };
 

@@ -7,7 +7,7 @@ namespace lora {
 // The device a stream belongs to current for the launch.
 struct StreamDevice {
     int prev = -1;
-    bool ok = false;
+    bool ok = false, moved = false;
     explicit StreamDevice(hipStream_t s) {
         int dev = -1;
         if (hipGetDevice(&prev) != hipSuccess) return;
@@ -16,10 +16,11 @@ struct StreamDevice {
         } else {
             dev = prev;
         }
-        ok = dev == prev || hipSetDevice(dev) == hipSuccess;
+        moved = dev != prev;
+        ok = !moved || hipSetDevice(dev) == hipSuccess;
     }
     ~StreamDevice() {
-        if (prev >= 0) (void)hipSetDevice(prev);
+        if (moved) (void)hipSetDevice(prev);
     }
 };
 

@@ -64,10 +64,7 @@ class Cache:
         n = [int(x) for x in k.shape]
         self._c = _Cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3), dtype,
                          n[0], n[1], n[2], n[3], n[4])
-
-    @property
-    def c(self):
-        return C.byref(self._c)
+        self.c = C.byref(self._c)
 
 
 class Seqs:
@@ -78,10 +75,7 @@ class Seqs:
         _table(tables, lens)
         self.tables, self.lens = tables, lens
         self._c = _Seqs(tables.data_ptr(), lens.data_ptr(), int(lens.shape[0]), int(tables.shape[1]), int(max_len))
-
-    @property
-    def c(self):
-        return C.byref(self._c)
+        self.c = C.byref(self._c)
 
 
 class Book:
@@ -93,10 +87,7 @@ class Book:
         self.tables, self.lens, self.refs = tables, lens, refs
         self._c = _Book(tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), int(lens.shape[0]), int(tables.shape[1]),
                         int(refs.shape[0]), int(page_rows))
-
-    @property
-    def c(self):
-        return C.byref(self._c)
+        self.c = C.byref(self._c)
 
 
 _bound = None
@@ -132,9 +123,15 @@ def _lib():
     return lib
 
 
-_addr = _lora._addr
 _stream = _lora._stream
 _check = _lora._check
+
+
+def _addr(p) -> int:
+    try:                                   # (a call of a few rows costs the host what this costs it)
+        return p.data_ptr()
+    except AttributeError:
+        return 0 if p is None else int(p)
 
 
 def _ids(a):
