@@ -189,7 +189,7 @@ def main() -> None:
     import torch
     dev, dt = torch.device("cuda:0"), torch.bfloat16
     n_layers, hidden, heads, kv_heads, dim = 4, 4096, 32, 32, 128
-    window, sinks, max_len, n_seqs = 256, 16, 2048, 24
+    window, sinks, max_len, n_seqs = 256, 16, 1536, 24
     st = torch.cuda.Stream()
     with torch.cuda.stream(st):
         layers, kept = random_layers(n_layers, hidden, heads, kv_heads, dim, dt, [8, 16, 32, 64], dev, stream=st)
