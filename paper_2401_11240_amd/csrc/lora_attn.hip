@@ -85,7 +85,8 @@ using namespace lora;
 
 namespace {
 // Workgroups of the decode kernel per compute unit: registers for a tile's K and V
-// in flight beside the output.
+// in flight beside the output.  (Two of width 256 spill: 64 sequences of 64 to 8192
+// tokens, 32/8 heads, 199 against 190 us.)
 constexpr int decode_per_cu(int dp) { return dp == 256 ? 1 : dp == 128 ? 3 : 4; }
 }
 
