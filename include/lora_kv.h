@@ -9,7 +9,7 @@
  * that decode one token, lora_attn_prompt for prompt segments), and its output
  * is the input of the adapted o projection.  Requests start, branch and end
  * between steps: their pages are handed out, shared, released and moved by the
- * lora_kv_grow, _fork, _free, _trim, _copy and _compact calls.
+ * lora_kv_grow, _grow_step, _fork, _fork_step, _free, _trim, _copy and _compact calls.
  *
  * Cache.  A page holds page_rows consecutive tokens of one sequence, for every
  * layer and every key-value head.  Element d of head h of row r of page p in
@@ -37,7 +37,7 @@
  *
  * Tables, lengths and reference counts are in DEVICE memory and are read when
  * a launch runs: a decode step recorded in a HIP graph is replayed for the
- * next token, while lora_kv_grow, recorded with it, moves the lengths and
+ * next token, while lora_kv_grow_step, recorded with it, moves the lengths and
  * hands out pages.  What the device holds cannot be checked by the call;
  * every kernel checks it where it is used: a length is read as at most
  * max_len and at least 0, an entry outside [0, n_pages) as no page, segment
@@ -88,7 +88,7 @@ typedef struct {
 /* The sequences of a step (HOST structure of DEVICE pointers). */
 typedef struct {
     const int32_t* tables;      /* [n_seqs, ld_table]: page ids        */
-    const int32_t* lens;        /* [n_seqs]: tokens, this step's included */
+    const int32_t* lens;        /* [n_seqs]: tokens, this step's included (lora_kv_grow_step's step_lens) */
     int32_t n_seqs, ld_table;
     int32_t max_len;            /* no length above this is read: sizes the launch */
 } lora_kv_seqs_t;
@@ -150,8 +150,8 @@ int lora_attn_prompt(lora_attn_t a, const lora_kv_cache_t* c, int32_t layer, con
                      const int32_t* seg_offset, int32_t n_rows, int32_t n_heads, const void* q, int64_t ldq,
                      void* out, int64_t ldo, float scale, int32_t window, int32_t n_sinks, void* stream);
 
-/* Device workspace of lora_kv_grow, _fork and _compact for this book, in
- * bytes; any contents, 16-byte aligned, overwritten. */
+/* Device workspace of lora_kv_grow, _fork (with or without _step) and _compact for
+ * this book, in bytes; any contents, 16-byte aligned, overwritten. */
 int lora_kv_workspace_bytes(const lora_kv_book_t* b, size_t* bytes);
 
 /*
@@ -167,16 +167,39 @@ int lora_kv_grow(const lora_kv_book_t* b, const int32_t* add, int32_t* info, voi
                  void* stream);
 
 /*
+ * The same for the rows of one step, with what the step has to know.  No length
+ * passes max_len (at most ld_table * page_rows; a sequence that would pass it
+ * stays as it is).  step_lens (DEVICE [n_seqs], not the book's lens) gets
+ * the new length of each sequence that grew, and 0 for one that stayed or had
+ * nothing to add.
+ *
+ * A sequence that stayed has no room for its rows: with lens as the lengths of the
+ * step, lora_kv_append would store them over its last tokens, which other
+ * sequences may share.  With step_lens as the lengths (lora_kv_seqs_t.lens) such rows
+ * are not stored and attention gives them zeros, also in a recorded step, where the host cannot
+ * look at info in between.  The rows of a sequence in that step are at most add[s].
+ */
+int lora_kv_grow_step(const lora_kv_book_t* b, const int32_t* add, int32_t max_len, int32_t* step_lens, int32_t* info,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Sequence children[i] becomes a copy of parents[i] (HOST arrays of n, read
  * during the call; the children distinct and none a parent).  What a child
  * held is released first.  Full pages are shared; the rows of a partly filled
  * last page are copied, in every layer, into a page of the child's own: free
  * pages in ascending order go to the pairs in the order given.  A child whose page
- * does not fit is left empty.  So an appended token never lands in a shared
- * page.  info (DEVICE [2], may be NULL): pages taken, children left empty.
+ * does not fit is left empty.  So the tokens that a later grow gives never lie in a
+ * shared page; for a sequence that got none, see lora_kv_grow_step.
+ * info (DEVICE [2], may be NULL): pages taken, children left empty.
  */
 int lora_kv_fork(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, const int32_t* parents,
                  const int32_t* children, int32_t* info, void* ws, size_t ws_bytes, void* stream);
+
+/* The same between steps that use step_lens: the children's become 0, so that they have
+ * no rows before the next lora_kv_grow_step. */
+int lora_kv_fork_step(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, const int32_t* parents,
+                      const int32_t* children, int32_t* step_lens, int32_t* info, void* ws, size_t ws_bytes,
+                      void* stream);
 
 /* Sequences seqs[0 .. n) (HOST array, distinct) release their pages: length 0,
  * table entries -1. */

@@ -110,7 +110,11 @@ class Step:
 
 
 class Server:
-    """The sequences of a cache: pages, lengths, and the steps that use them."""
+    """The sequences of a cache: pages, lengths, and the steps that use them.
+
+    ``grow`` comes before each step: ``seqs``, which the step is run with, has the sequences
+    that it gave their tokens (``step_lens``).  The others have no row in that step: nothing
+    of theirs is stored, and attention gives their rows zeros."""
 
     def __init__(self, cache: KV.Cache, n_seqs: int, max_len: int, stream=None):
         import torch
@@ -121,21 +125,26 @@ class Server:
         i32 = dict(dtype=torch.int32, device=dev)
         self.tables = torch.full((n_seqs, ld), -1, **i32)
         self.lens = torch.zeros(n_seqs, **i32)
+        self.step_lens = torch.zeros(n_seqs, **i32)
         self.refs = torch.zeros(n_pages, **i32)
         self.info = torch.zeros(2, **i32)
         self.book = KV.Book(self.tables, self.lens, self.refs, page_rows)
-        self.seqs = KV.Seqs(self.tables, self.lens, max_len)
+        self.seqs = KV.Seqs(self.tables, self.step_lens, max_len)
         self.ws_bytes = KV.lora_kv_workspace_bytes(self.book)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
         self.attn = KV.lora_attn_create(dev.index or 0, stream)
 
     def grow(self, add) -> None:
-        """``add``: int32 device tensor [n_seqs].  ``info`` then holds (pages taken,
-        sequences that did not fit); reading it waits for the stream."""
-        KV.lora_kv_grow(self.book, add, self.info, self.ws, self.ws_bytes, self.stream)
+        """``add``: int32 device tensor [n_seqs], the step's rows of each sequence.  ``info``
+        then holds (pages taken, sequences that did not fit), ``step_lens`` 0 for those and
+        for those without rows; reading them waits for the stream."""
+        KV.lora_kv_grow_step(self.book, add, self.tables.shape[1] * self.book.page_rows, self.step_lens, self.info,
+                             self.ws, self.ws_bytes, self.stream)
 
     def fork(self, parents, children) -> None:
-        KV.lora_kv_fork(self.cache, self.book, parents, children, self.info, self.ws, self.ws_bytes, self.stream)
+        """Between a step and the next ``grow``: the children have no rows before it."""
+        KV.lora_kv_fork_step(self.cache, self.book, parents, children, self.step_lens, self.info, self.ws,
+                             self.ws_bytes, self.stream)
 
     def free(self, seqs) -> None:
         KV.lora_kv_free(self.book, seqs, self.stream)

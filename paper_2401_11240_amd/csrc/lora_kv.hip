@@ -300,11 +300,12 @@ __host__ __device__ inline BookWs book_ws(void* ws, int n_pages, int n_seqs) {
 }
 
 // One workgroup: the counts of 1024 sequences at a time in a scan, the free pages in another.
-__global__ void __launch_bounds__(kBookThreads) lora_kv_grow_kernel(Book b, const int32_t* add, int32_t* info, BookWs w) {
+// No length passes room; step_lens may be NULL.
+__global__ void __launch_bounds__(kBookThreads) lora_kv_grow_kernel(Book b, const int32_t* add, int64_t room,
+                                                                    int32_t* step_lens, int32_t* info, BookWs w) {
     __shared__ int wave_sum[kBookThreads / 64];
     __shared__ int stayed;
     const int t = threadIdx.x;
-    const int64_t room = (int64_t)b.ld_table << b.page_shift;
     if (t == 0) stayed = 0;
     // pages wanted by the sequences up to and including each, those too long for their table left out
     auto wanted = [&](int s, int& len, int& to) {
@@ -364,7 +365,11 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_grow_kernel(Book b, cons
     for (int s = t; s < b.n_seqs; s += kBookThreads) {
         int len, to;
         const int n = wanted(s, len, to);
-        if (to >= 0 && (n == 0 || w.sums[s] <= found)) b.lens[s] = to;
+        const bool grows = to >= 0 && (n == 0 || w.sums[s] <= found);
+        if (grows) b.lens[s] = to;
+        // (a sequence that got nothing has no row in the step: stored at its length's end, it
+        // would go over the last token, which others may share)
+        if (step_lens) step_lens[s] = grows && to > len ? to : 0;
     }
     if (info && t == 0) {
         info[0] = taken;
@@ -451,10 +456,13 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_fork_pages_kernel(ForkAr
 
 // Workgroups y < n: row y of the children's tables and lengths (x == 0), and unit x of
 // the copy of its last page's rows.
-__global__ void __launch_bounds__(kCopyThreads) lora_kv_fork_kernel(Book b, PageDims d, IdArgs ids, BookWs w) {
+__global__ void __launch_bounds__(kCopyThreads) lora_kv_fork_kernel(Book b, PageDims d, IdArgs ids, BookWs w,
+                                                                    int32_t* step_lens) {
     const int pair = blockIdx.y;
     const int parent = ids.id[2 * pair], child = ids.id[2 * pair + 1];
     const int fresh = w.list[pair];
+    // (what the child had of a step under way would land in pages that it now shares)
+    if (step_lens && blockIdx.x == 0 && threadIdx.x == 0) step_lens[child] = 0;
     if (fresh == -2) return;               // the child is empty already
     int len, src;
     fork_tail(b, parent, len, src);
@@ -677,6 +685,70 @@ int check_page_size(const lora_kv_cache_t* c) {
 
 int no_device(const char* what) { return set_error(LORA_E_HIP, std::string(what) + ": cannot select the stream's device"); }
 
+// step_lens of a step's calls: an array of its own beside the book's lengths.
+int check_step_lens(const lora_kv_book_t* b, const int32_t* step_lens) {
+    if (b->n_seqs > 0 && !step_lens) return set_error(LORA_E_ARG, "step_lens is NULL");
+    if (int rc = check_words("step_lens", step_lens)) return rc;
+    const uintptr_t x = (uintptr_t)step_lens, y = (uintptr_t)b->lens, n = 4 * (uintptr_t)b->n_seqs;
+    if (x < y + n && y < x + n) return set_error(LORA_E_OVERLAP, "step_lens and lens overlap");
+    return LORA_OK;
+}
+
+int enqueue_grow(const char* name, const lora_kv_book_t* b, const int32_t* add, int64_t room, int32_t* step_lens,
+                 int32_t* info, void* ws, size_t ws_bytes, void* stream) {
+    if (b->n_seqs > 0 && !add) return set_error(LORA_E_ARG, "add is NULL");
+    if (int rc = check_words("add", add)) return rc;
+    if (int rc = check_words("info", info)) return rc;
+    if (int rc = check_ws(b, ws, ws_bytes)) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    StreamDevice g(st);
+    if (!g.ok) return no_device(name);
+    hipLaunchKernelGGL(lora_kv_grow_kernel, dim3(1), dim3(kBookThreads), 0, st, device_book(b), add, room, step_lens,
+                       info, book_ws(ws, b->n_pages, b->n_seqs));
+    return check_launch(name);
+}
+
+int enqueue_fork(const char* name, const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, const int32_t* parents,
+                 const int32_t* children, int32_t* step_lens, int32_t* info, void* ws, size_t ws_bytes, void* stream) {
+    if (int rc = check_kv_cache(c)) return rc;
+    if (int rc = check_page_size(c)) return rc;
+    if (int rc = check_book(b)) return rc;
+    if (int rc = check_book_cache(c, b)) return rc;
+    if (int rc = check_pairs("parent", "child", parents, children, n, b->n_seqs)) return rc;
+    if (int rc = check_words("info", info)) return rc;
+    if (int rc = check_ws(b, ws, ws_bytes)) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    StreamDevice g(st);
+    if (!g.ok) return no_device(name);
+    const Book book = device_book(b);
+    const PageDims d = page_dims(c);
+    const BookWs w = book_ws(ws, b->n_pages, b->n_seqs);
+    constexpr int kPairs = kArgIds / 2;
+    static_assert(kPairs <= kBookThreads, "one thread per pair");
+    const int units = 2 * d.n_layers * d.blocks;
+    IdArgs ids{};
+    // every child's pages come back before any is handed out
+    for (int pass = 0; pass < 2; ++pass)
+        for (int32_t i0 = 0; i0 < n || (pass && n == 0 && i0 == 0); i0 += kPairs) {
+            const int m = std::min(kPairs, n - i0);
+            for (int i = 0; i < m; ++i) {
+                ids.id[2 * i] = parents[i0 + i];
+                ids.id[2 * i + 1] = children[i0 + i];
+            }
+            if (pass == 0) {
+                hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, book, ids, 2, 1);
+            } else {
+                hipLaunchKernelGGL(lora_kv_fork_pages_kernel, dim3(1), dim3(kBookThreads), 0, st,
+                                   ForkArgs{book, w, info, m, (int)(i0 == 0), ids});
+                if (m > 0)
+                    hipLaunchKernelGGL(lora_kv_fork_kernel, dim3(1 + units, m), dim3(kCopyThreads), 0, st, book, d, ids, w,
+                                       step_lens);
+            }
+            if (int rc = check_launch(name)) return rc;
+        }
+    return LORA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -737,56 +809,30 @@ int lora_kv_workspace_bytes(const lora_kv_book_t* b, size_t* bytes) {
 
 int lora_kv_grow(const lora_kv_book_t* b, const int32_t* add, int32_t* info, void* ws, size_t ws_bytes, void* stream) {
     if (int rc = check_book(b)) return rc;
-    if (b->n_seqs > 0 && !add) return set_error(LORA_E_ARG, "add is NULL");
-    if (int rc = check_words("add", add)) return rc;
-    if (int rc = check_words("info", info)) return rc;
-    if (int rc = check_ws(b, ws, ws_bytes)) return rc;
-    hipStream_t st = (hipStream_t)stream;
-    StreamDevice g(st);
-    if (!g.ok) return no_device("lora_kv_grow");
-    hipLaunchKernelGGL(lora_kv_grow_kernel, dim3(1), dim3(kBookThreads), 0, st, device_book(b), add, info,
-                       book_ws(ws, b->n_pages, b->n_seqs));
-    return check_launch("lora_kv_grow");
+    return enqueue_grow("lora_kv_grow", b, add, (int64_t)b->ld_table * b->page_rows, nullptr, info, ws, ws_bytes, stream);
+}
+
+int lora_kv_grow_step(const lora_kv_book_t* b, const int32_t* add, int32_t max_len, int32_t* step_lens, int32_t* info,
+                      void* ws, size_t ws_bytes, void* stream) {
+    if (int rc = check_book(b)) return rc;
+    if (max_len < 0) return set_error(LORA_E_ARG, "negative max_len");
+    if ((int64_t)max_len > (int64_t)b->ld_table * b->page_rows)
+        return set_error(LORA_E_SHAPE, "max_len exceeds ld_table * page_rows");
+    if (int rc = check_step_lens(b, step_lens)) return rc;
+    return enqueue_grow("lora_kv_grow_step", b, add, max_len, step_lens, info, ws, ws_bytes, stream);
 }
 
 int lora_kv_fork(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, const int32_t* parents,
                  const int32_t* children, int32_t* info, void* ws, size_t ws_bytes, void* stream) {
-    if (int rc = check_kv_cache(c)) return rc;
-    if (int rc = check_page_size(c)) return rc;
+    return enqueue_fork("lora_kv_fork", c, b, n, parents, children, nullptr, info, ws, ws_bytes, stream);
+}
+
+int lora_kv_fork_step(const lora_kv_cache_t* c, const lora_kv_book_t* b, int32_t n, const int32_t* parents,
+                      const int32_t* children, int32_t* step_lens, int32_t* info, void* ws, size_t ws_bytes,
+                      void* stream) {
     if (int rc = check_book(b)) return rc;
-    if (int rc = check_book_cache(c, b)) return rc;
-    if (int rc = check_pairs("parent", "child", parents, children, n, b->n_seqs)) return rc;
-    if (int rc = check_words("info", info)) return rc;
-    if (int rc = check_ws(b, ws, ws_bytes)) return rc;
-    hipStream_t st = (hipStream_t)stream;
-    StreamDevice g(st);
-    if (!g.ok) return no_device("lora_kv_fork");
-    const Book book = device_book(b);
-    const PageDims d = page_dims(c);
-    const BookWs w = book_ws(ws, b->n_pages, b->n_seqs);
-    constexpr int kPairs = kArgIds / 2;
-    static_assert(kPairs <= kBookThreads, "one thread per pair");
-    const int units = 2 * d.n_layers * d.blocks;
-    IdArgs ids{};
-    // every child's pages come back before any is handed out
-    for (int pass = 0; pass < 2; ++pass)
-        for (int32_t i0 = 0; i0 < n || (pass && n == 0 && i0 == 0); i0 += kPairs) {
-            const int m = std::min(kPairs, n - i0);
-            for (int i = 0; i < m; ++i) {
-                ids.id[2 * i] = parents[i0 + i];
-                ids.id[2 * i + 1] = children[i0 + i];
-            }
-            if (pass == 0) {
-                hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, book, ids, 2, 1);
-            } else {
-                hipLaunchKernelGGL(lora_kv_fork_pages_kernel, dim3(1), dim3(kBookThreads), 0, st,
-                                   ForkArgs{book, w, info, m, (int)(i0 == 0), ids});
-                if (m > 0)
-                    hipLaunchKernelGGL(lora_kv_fork_kernel, dim3(1 + units, m), dim3(kCopyThreads), 0, st, book, d, ids, w);
-            }
-            if (int rc = check_launch("lora_kv_fork")) return rc;
-        }
-    return LORA_OK;
+    if (int rc = check_step_lens(b, step_lens)) return rc;
+    return enqueue_fork("lora_kv_fork_step", c, b, n, parents, children, step_lens, info, ws, ws_bytes, stream);
 }
 
 int lora_kv_free(const lora_kv_book_t* b, int32_t n, const int32_t* seqs, void* stream) {

@@ -13,8 +13,8 @@ import numpy as np
 from . import lora as _lora
 
 EXPORTS = ("lora_kv_append", "lora_attn_create", "lora_attn_destroy", "lora_attn_decode", "lora_attn_prompt",
-           "lora_kv_workspace_bytes", "lora_kv_grow", "lora_kv_fork", "lora_kv_free", "lora_kv_trim", "lora_kv_copy",
-           "lora_kv_compact")
+           "lora_kv_workspace_bytes", "lora_kv_grow", "lora_kv_grow_step", "lora_kv_fork", "lora_kv_fork_step",
+           "lora_kv_free", "lora_kv_trim", "lora_kv_copy", "lora_kv_compact")
 
 
 class _Cache(C.Structure):
@@ -84,7 +84,7 @@ class Book:
     def __init__(self, tables, lens, refs, page_rows: int):
         _table(tables, lens)
         _int32(refs, 1, "refs")
-        self.tables, self.lens, self.refs = tables, lens, refs
+        self.tables, self.lens, self.refs, self.page_rows = tables, lens, refs, int(page_rows)
         self._c = _Book(tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), int(lens.shape[0]), int(tables.shape[1]),
                         int(refs.shape[0]), int(page_rows))
         self.c = C.byref(self._c)
@@ -109,7 +109,9 @@ def _lib():
         "lora_attn_prompt": [vp, cache, i32, seqs, vp, i32, i32, vp, i64, vp, i64, f32, i32, i32, vp],
         "lora_kv_workspace_bytes": [book, C.POINTER(sz)],
         "lora_kv_grow": [book, vp, vp, vp, sz, vp],
+        "lora_kv_grow_step": [book, vp, i32, vp, vp, vp, sz, vp],
         "lora_kv_fork": [cache, book, i32, i32p, i32p, vp, vp, sz, vp],
+        "lora_kv_fork_step": [cache, book, i32, i32p, i32p, vp, vp, vp, sz, vp],
         "lora_kv_free": [book, i32, i32p, vp],
         "lora_kv_trim": [book, i32, i32, vp],
         "lora_kv_copy": [cache, i32, i32p, i32p, vp],
@@ -178,12 +180,30 @@ def lora_kv_grow(book: Book, add, info, ws, ws_bytes: int, stream=None) -> None:
     _check(_lib().lora_kv_grow(book.c, _addr(add), _addr(info), _addr(ws), ws_bytes, _stream(stream)))
 
 
-def lora_kv_fork(cache: Cache, book: Book, parents, children, info, ws, ws_bytes: int, stream=None) -> None:
+def lora_kv_grow_step(book: Book, add, max_len: int, step_lens, info, ws, ws_bytes: int, stream=None) -> None:
+    """Grow, with the lengths that the step's calls use (``Seqs``) in ``step_lens``."""
+    _check(_lib().lora_kv_grow_step(book.c, _addr(add), max_len, _addr(step_lens), _addr(info), _addr(ws), ws_bytes,
+                                    _stream(stream)))
+
+
+def _pairs(parents, children):
     p, pp = _ids(parents)
     c, cp = _ids(children)
     if p.size != c.size:
         raise ValueError("parents and children differ in number")
+    return p, pp, c, cp
+
+
+def lora_kv_fork(cache: Cache, book: Book, parents, children, info, ws, ws_bytes: int, stream=None) -> None:
+    p, pp, c, cp = _pairs(parents, children)
     _check(_lib().lora_kv_fork(cache.c, book.c, p.size, pp, cp, _addr(info), _addr(ws), ws_bytes, _stream(stream)))
+
+
+def lora_kv_fork_step(cache: Cache, book: Book, parents, children, step_lens, info, ws, ws_bytes: int,
+                      stream=None) -> None:
+    p, pp, c, cp = _pairs(parents, children)
+    _check(_lib().lora_kv_fork_step(cache.c, book.c, p.size, pp, cp, _addr(step_lens), _addr(info), _addr(ws), ws_bytes,
+                                    _stream(stream)))
 
 
 def lora_kv_free(book: Book, seqs, stream=None) -> None:

@@ -1,0 +1,198 @@
+"""Steps in which not every sequence has a row: sequences that found no page or no
+room in their table, and sequences that pause.  What they hold, and what others share with
+them, stays as it is bit for bit; the rows of the others are stored and attend as always."""
+import numpy as np
+import pytest
+
+import kv_reference as R
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():   # collected on CPU-only hosts, never run there
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2401_11240_amd import attention as T  # noqa: E402
+from paper_2401_11240_amd import kv as KV  # noqa: E402
+from paper_2401_11240_amd import lora as L  # noqa: E402
+
+DEV = torch.device("cuda:0")
+HIDDEN, HEADS, KV_HEADS, DIM, LAYERS, PR = 128, 4, 2, 32, 2, 16
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+class Stack:
+    """A server of n_pages pages and its book in Python lists."""
+
+    def __init__(self, n_seqs, n_pages, max_len, dtype=torch.bfloat16):
+        self.n_seqs, self.max_len, self.dtype = n_seqs, max_len, dtype
+        self.st = torch.cuda.current_stream(DEV)
+        self.layers, self.kept = T.random_layers(LAYERS, HIDDEN, HEADS, KV_HEADS, DIM, dtype, [4, 8], DEV, 3, self.st)
+        self.gen = torch.Generator().manual_seed(n_pages)
+        shape = (LAYERS, n_pages, KV_HEADS, PR, DIM)
+        self.k, self.v = (torch.randn(shape, generator=self.gen).to(dtype).to(DEV) for _ in range(2))
+        self.srv = T.Server(KV.Cache(self.k, self.v), n_seqs, max_len, self.st)
+        ld = self.srv.tables.shape[1]
+        self.ref = R.Book([[-1] * ld for _ in range(n_seqs)], [0] * n_seqs, n_pages, PR)
+        self.steps = {}
+
+    def step(self, rows):
+        if tuple(rows) not in self.steps:
+            self.steps[tuple(rows)] = T.Step(self.layers, self.srv.cache, rows, [s % 2 for s in range(self.n_seqs)], HEADS,
+                                             stream=self.st)
+        return self.steps[tuple(rows)]
+
+    def x(self, n):
+        return torch.randn((n, HIDDEN), generator=self.gen).to(self.dtype).to(DEV)
+
+    def grown(self, add):
+        """The Python book grown: info, and which sequences have their rows."""
+        before = list(self.ref.lens)
+        info = self.ref.grow(add)
+        return info, [b > a for a, b in zip(before, self.ref.lens)]
+
+    def token(self, add, rows, launch=None):
+        """grow(add) and a step of these rows; launch() does both from a recorded graph."""
+        step, n = self.step(rows), sum(rows)
+        before = self.k.clone(), self.v.clone()
+        if launch is None:
+            self.srv.grow(torch.tensor(add, dtype=torch.int32, device=DEV))
+            step.run(self.srv.attn, self.srv.seqs, self.x(n), torch.empty((n, HIDDEN), dtype=self.dtype, device=DEV),
+                     self.st)
+        else:
+            launch()
+        torch.cuda.synchronize()
+        info, has = self.grown(add)
+        assert self.srv.info.tolist() == info
+        assert self.srv.lens.tolist() == self.ref.lens and self.srv.refs.tolist() == self.ref.refs
+        table = self.srv.tables.cpu().numpy()
+        k, v = f64(self.k[-1]), f64(self.v[-1])
+        newk, newv = (t.view(-1, KV_HEADS, DIM) for t in (step.k, step.v))
+        written = torch.zeros((before[0].shape[1], PR), dtype=torch.bool)
+        q, a, at = f64(step.q).reshape(-1, HEADS, DIM), f64(step.a).reshape(-1, HEADS, DIM), 0
+        for s, r in enumerate(rows):
+            if not has[s]:
+                assert (a[at:at + r] == 0).all(), (s, "rows of a sequence that got nothing")
+            else:
+                first = self.ref.lens[s] - r
+                for i in range(r):
+                    page, row = int(table[s, (first + i) // PR]), (first + i) % PR
+                    assert self.ref.refs[page] == 1
+                    assert torch.equal(self.k[-1, page, :, row], newk[at + i])
+                    assert torch.equal(self.v[-1, page, :, row], newv[at + i])
+                    written[page, row] = True
+                o, m, reach = R.attention(q[at:at + r], k, v, table[s], self.ref.lens[s], first, step.scale, 0, 0)
+                tol = R.allowance(o, m, reach, DIM, self.ref.lens[s], self.dtype == torch.bfloat16)
+                assert (np.abs(a[at:at + r] - o) <= tol).all(), s
+            at += r
+        keep = ~written.to(DEV)[None, :, None, :, None].expand_as(self.k)
+        for t, b in zip((self.k, self.v), before):
+            assert torch.equal(t[keep].view(torch.int16), b[keep].view(torch.int16)), "a token that is no row's was changed"
+        return has
+
+    def close(self):
+        torch.cuda.synchronize()
+        for s in self.steps.values():
+            s.release()
+        self.srv.release()
+        for layer in self.layers:
+            for p in (layer.q, layer.k, layer.v, layer.o):
+                L.lora_release_adapters(p.table)
+
+
+@pytest.fixture
+def stack(request):
+    s = Stack(*request.param)
+    yield s
+    s.close()
+
+
+@pytest.mark.parametrize("stack", [(4, 3, 64)], indirect=True)
+@pytest.mark.parametrize("recorded", [False, True])
+def test_forked_sequences_without_a_page_for_their_token(stack, recorded):
+    # 32 tokens in two full pages that three sequences share, and one page for three tokens
+    s, st = stack, stack.st
+    assert s.token([32, 0, 0, 0], [32, 0, 0, 0])[0]
+    s.srv.fork([0, 0], [1, 2])
+    s.ref.fork([0, 0], [1, 2])
+    rows = [1] * 4
+    launch = None
+    if recorded:
+        step, x, y = s.step(rows), s.x(4), torch.empty((4, HIDDEN), dtype=s.dtype, device=DEV)
+        add = torch.zeros(4, dtype=torch.int32, device=DEV)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        s.srv.stream = side
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            s.srv.grow(add)
+            step.run(s.srv.attn, s.srv.seqs, x, y, side)
+        s.srv.stream = st
+
+    def token(a):
+        def replay():
+            add.copy_(torch.tensor(a, dtype=torch.int32))
+            x.copy_(s.x(4))
+            torch.cuda.synchronize()
+            graph.replay()
+        return s.token(a, rows, replay if recorded else launch)
+
+    for _ in range(3):
+        assert token([1, 1, 1, 0]) == [True, False, False, False]
+    assert token([0, 1, 0, 1]) == [False] * 4        # one pauses, one has no page, one is empty and gets none
+    s.srv.free([0])
+    s.ref.free([0])
+    assert token([0, 1, 1, 0]) == [False, True, False, False]
+    assert token([1, 1, 1, 0]) == [False, True, False, False]
+    if recorded:
+        del graph
+
+
+@pytest.mark.parametrize("stack", [(3, 12, 48)], indirect=True)
+def test_full_tables_and_chunks_without_room(stack):
+    s = stack
+    assert s.token([40, 32, 5], [40, 32, 5]) == [True] * 3
+    assert s.token([9, 7, 0], [9, 7, 0]) == [False, True, False]       # 49 tokens do not fit a table of 48
+    assert s.token([8, 0, 20], [8, 0, 20]) == [True, False, True]
+    assert s.token([1, 9, 1], [1, 9, 1]) == [False, True, True]
+    assert s.token([1, 1, 1], [1, 1, 1]) == [False, False, True]       # the first two are at 48
+    assert s.token([0, 0, 0], [1, 1, 1]) == [False] * 3
+
+
+@pytest.mark.parametrize("stack", [(4, 9, 64)], indirect=True)
+def test_a_child_has_no_row_before_it_grows(stack):
+    # the children were in the step before the fork, with lengths of their own
+    s = stack
+    assert s.token([32, 20, 3, 0], [32, 20, 3, 0]) == [True, True, True, False]
+    s.srv.fork([0, 0], [1, 2])
+    s.ref.fork([0, 0], [1, 2])
+    before = s.k.clone(), s.v.clone()
+    assert s.srv.step_lens.tolist()[1:3] == [0, 0]
+    assert s.token([1, 1, 1, 1], [1] * 4) == [True] * 4
+    pages = s.srv.tables[0, :2].tolist()
+    for t, b in zip((s.k, s.v), before):
+        assert torch.equal(t[:, pages].view(torch.int16), b[:, pages].view(torch.int16))
+
+
+def test_grow_step_against_the_book():
+    n, n_pages = 1300, 700
+    i32 = dict(dtype=torch.int32, device=DEV)
+    tables, lens, refs = torch.full((n, 6), -1, **i32), torch.zeros(n, **i32), torch.zeros(n_pages, **i32)
+    step_lens, info = torch.full((n,), -3, **i32), torch.zeros(2, **i32)
+    book = KV.Book(tables, lens, refs, PR)
+    nb = KV.lora_kv_workspace_bytes(book)
+    ws = torch.empty(nb, dtype=torch.uint8, device=DEV)
+    ref = R.Book(tables.tolist(), [0] * n, n_pages, PR)
+    rng = np.random.default_rng(4)
+    for rep in range(5):
+        add = [int(x) for x in rng.choice([0, 1, 1, 5, 16, 40, -3, 100], size=n)]
+        before = list(ref.lens)
+        KV.lora_kv_grow_step(book, torch.tensor(add, **i32), 6 * PR, step_lens, info, ws, nb,
+                             torch.cuda.current_stream())
+        assert info.tolist() == ref.grow(add)
+        assert lens.tolist() == ref.lens and refs.tolist() == ref.refs
+        assert step_lens.tolist() == [b if b > a else 0 for a, b in zip(before, ref.lens)], rep
