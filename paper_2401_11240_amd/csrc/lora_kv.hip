@@ -289,7 +289,7 @@ __device__ int find_free(const Book& b, int want, int32_t* list, int* wave_sum) 
 
 // Workspace: int32 words.  [0, n_pages) and [n_pages, 2 n_pages): page lists;
 // [2 n_pages, 3 n_pages): the compaction's numbering; then n_seqs running
-// sums, and two counters.
+// sums (a fork's pages by pair: its children are distinct, so at most n_seqs), and two counters.
 struct BookWs {
     int32_t *list, *list2, *map, *sums, *count;
 };
@@ -421,7 +421,7 @@ __device__ __forceinline__ bool fork_tail(const Book& b, int parent, int& len, i
 // and rows are copied (48 children: 2.7 + 4.5 + 12.5 us, 62 MB).  With the first two
 // in one it took longer (22.8 against 19.6 us): one workgroup then releases what 48 did.
 //
-// The pages of n children: list[i] gets pair i's, or -1 where it needs none, or -2 where none is left.
+// The pages of n children: sums[i] gets pair i's, or -1 where it needs none, or -2 where none is left.
 struct ForkArgs {
     Book book;
     BookWs w;
@@ -442,10 +442,10 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_fork_pages_kernel(ForkAr
     int len, src, want = 0;
     const bool need = t < n && fork_tail(b, ids[2 * t], len, src);
     const int at = block_scan(need ? 1 : 0, wave_sum, want);
-    const int found = find_free(b, want, w.list2, wave_sum);
+    const int found = find_free(b, want, w.list, wave_sum);
     if (t < n) {
-        const int page = !need ? -1 : at < found ? w.list2[at] : -2;
-        w.list[t] = page;
+        const int page = !need ? -1 : at < found ? w.list[at] : -2;
+        w.sums[t] = page;
         if (page >= 0) b.refs[page] = 1;
     }
     if (info && t == 0) {
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kCopyThreads) lora_kv_fork_kernel(Book b, Page
                                                                     int32_t* step_lens) {
     const int pair = blockIdx.y;
     const int parent = ids.id[2 * pair], child = ids.id[2 * pair + 1];
-    const int fresh = w.list[pair];
+    const int fresh = w.sums[pair];
     // (what the child had of a step under way would land in pages that it now shares)
     if (step_lens && blockIdx.x == 0 && threadIdx.x == 0) step_lens[child] = 0;
     if (fresh == -2) return;               // the child is empty already

@@ -196,3 +196,23 @@ def test_grow_step_against_the_book():
         assert info.tolist() == ref.grow(add)
         assert lens.tolist() == ref.lens and refs.tolist() == ref.refs
         assert step_lens.tolist() == [b if b > a else 0 for a, b in zip(before, ref.lens)], rep
+
+
+@pytest.mark.parametrize("n_pages,kids", [(100, 120), (30, 200), (3, 239), (70, 600)])
+def test_more_children_than_pages(n_pages, kids):
+    # one short parent whose last page every child wants a copy of, and one of a full page
+    from test_gpu_kv import Pages
+    for rep in range(4):
+        p = Pages(kids + 2, 2, n_pages, PR, [5, 16], seed=rep)
+        children = [int(c) for c in np.random.default_rng(rep).permutation(np.arange(2, kids + 2))]
+        parents = [int(i % 7 == 3) for i in range(kids)]
+        k, v = p.k.clone(), p.v.clone()
+        KV.lora_kv_fork(p.cache, p.book, parents, children, p.info, p.ws, p.nb, torch.cuda.current_stream())
+        info, copies = p.ref.fork(parents, children)
+        assert p.info.tolist() == info
+        p.same()
+        for src, dst, rows in copies:
+            for w, t in ((k, p.k), (v, p.v)):
+                w[:, dst, :, :rows] = w[:, src, :, :rows].clone()
+        assert torch.equal(p.k.view(torch.int16), k.view(torch.int16))
+        assert torch.equal(p.v.view(torch.int16), v.view(torch.int16))
