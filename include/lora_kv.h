@@ -90,7 +90,8 @@ typedef struct {
     const int32_t* tables;      /* [n_seqs, ld_table]: page ids        */
     const int32_t* lens;        /* [n_seqs]: tokens, this step's included (lora_kv_grow_step's step_lens) */
     int32_t n_seqs, ld_table;
-    int32_t max_len;            /* no length above this is read: sizes the launch */
+    int32_t max_len;            /* no length above this is read: sizes the launch
+                                   (and bounds lora_kv_grow_step, or is ld_table * page_rows) */
 } lora_kv_seqs_t;
 
 /* Who holds which page (HOST structure of DEVICE pointers).  refs[p] counts

@@ -114,14 +114,15 @@ class Server:
 
     ``grow`` comes before each step: ``seqs``, which the step is run with, has the sequences
     that it gave their tokens (``step_lens``).  The others have no row in that step: nothing
-    of theirs is stored, and attention gives their rows zeros."""
+    of theirs is stored, and attention gives their rows zeros.  No sequence grows past
+    ``max_len`` tokens, whether or not its last page has room for more."""
 
     def __init__(self, cache: KV.Cache, n_seqs: int, max_len: int, stream=None):
         import torch
         dev = cache.k.device
         n_pages, page_rows = int(cache.k.shape[1]), int(cache.k.shape[3])
         ld = -(-max_len // page_rows)
-        self.cache, self.stream = cache, stream
+        self.cache, self.stream, self.max_len = cache, stream, max_len
         i32 = dict(dtype=torch.int32, device=dev)
         self.tables = torch.full((n_seqs, ld), -1, **i32)
         self.lens = torch.zeros(n_seqs, **i32)
@@ -138,8 +139,8 @@ class Server:
         """``add``: int32 device tensor [n_seqs], the step's rows of each sequence.  ``info``
         then holds (pages taken, sequences that did not fit), ``step_lens`` 0 for those and
         for those without rows; reading them waits for the stream."""
-        KV.lora_kv_grow_step(self.book, add, self.tables.shape[1] * self.book.page_rows, self.step_lens, self.info,
-                             self.ws, self.ws_bytes, self.stream)
+        KV.lora_kv_grow_step(self.book, add, self.max_len, self.step_lens, self.info, self.ws, self.ws_bytes,
+                             self.stream)
 
     def fork(self, parents, children) -> None:
         """Between a step and the next ``grow``: the children have no rows before it."""

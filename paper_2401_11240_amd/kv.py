@@ -84,7 +84,7 @@ class Book:
     def __init__(self, tables, lens, refs, page_rows: int):
         _table(tables, lens)
         _int32(refs, 1, "refs")
-        self.tables, self.lens, self.refs, self.page_rows = tables, lens, refs, int(page_rows)
+        self.tables, self.lens, self.refs = tables, lens, refs
         self._c = _Book(tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), int(lens.shape[0]), int(tables.shape[1]),
                         int(refs.shape[0]), int(page_rows))
         self.c = C.byref(self._c)

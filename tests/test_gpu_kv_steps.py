@@ -52,7 +52,8 @@ class Stack:
     def grown(self, add):
         """The Python book grown: info, and which sequences have their rows."""
         before = list(self.ref.lens)
-        info = self.ref.grow(add)
+        past = len(self.ref.t[0]) * PR + 1       # (the list book knows the table's end alone)
+        info = self.ref.grow([past if a > 0 and n + a > self.max_len else a for n, a in zip(before, add)])
         return info, [b > a for a, b in zip(before, self.ref.lens)]
 
     def token(self, add, rows, launch=None):
@@ -161,6 +162,18 @@ def test_full_tables_and_chunks_without_room(stack):
     assert s.token([1, 9, 1], [1, 9, 1]) == [False, True, True]
     assert s.token([1, 1, 1], [1, 1, 1]) == [False, False, True]       # the first two are at 48
     assert s.token([0, 0, 0], [1, 1, 1]) == [False] * 3
+
+
+@pytest.mark.parametrize("stack", [(3, 40, 100), (3, 40, 33)], indirect=True)
+def test_the_longest_length_ends_inside_a_page(stack):
+    s, m = stack, stack.max_len
+    assert s.token([m - 3, m, 7], [m - 3, m, 7]) == [True] * 3
+    for i in range(5):
+        assert s.token([1, 1, 1], [1, 1, 1]) == [i < 3, False, True], i
+    assert s.token([1, 1, 9], [4, 2, 9]) == [False, False, True]         # chunks
+    assert s.token([1, 1, m - 20], [4, 2, m - 20]) == [False, False, False]
+    assert s.token([0, 0, m - 21], [1, 1, m - 21]) == [False, False, True]
+    assert s.srv.lens.tolist() == [m] * 3
 
 
 @pytest.mark.parametrize("stack", [(4, 9, 64)], indirect=True)
