@@ -48,7 +48,7 @@ class Layer:
 
 class Step:
     """What the layers of one step share: segment s of the batch holds the last
-    rows of sequence s.  Creation allocates and waits for ``stream``; ``run``
+    rows of sequence s, and every sequence has a segment (of length 0 if it has no rows).  Creation allocates and waits for ``stream``; ``run``
     only enqueues, and may be recorded in a HIP graph."""
 
     def __init__(self, layers: Sequence[Layer], cache: KV.Cache, seg_lens: Sequence[int], seg_adapter: Sequence[int],
@@ -60,6 +60,7 @@ class Step:
         self.width, self.kv_width = n_heads * head_dim, int(cache.k.shape[2]) * head_dim
         offset = np.concatenate([[0], np.cumsum(seg_lens)]).astype(np.int32)
         self.n_rows = int(offset[-1])
+        self.n_segments = len(seg_lens)
         self.single = all(n == 1 for n in seg_lens)      # one row per sequence: the decode form
         self.batch = L.Batch(offset, np.asarray(seg_adapter, np.int32), self.n_rows)
         dev, dt = cache.k.device, cache.k.dtype
@@ -78,6 +79,12 @@ class Step:
         L.lora_base_plan_apply(self._plans[p.shape], p.table, x, x.stride(0), p.wt, p.wt.stride(0), y, y.stride(0),
                                stream)
 
+    def _check_seqs(self, seqs: KV.Seqs):
+        # (the launches read an offset per sequence)
+        if int(seqs.lens.shape[0]) != self.n_segments:
+            raise ValueError(f"a step of {self.n_segments} segments with {int(seqs.lens.shape[0])} sequences: one segment "
+                             "per sequence is needed, of no rows where it has none")
+
     def project(self, layer: int, x, stream=None) -> None:
         """q, k and v of the step's rows, into ``self.q``, ``self.k`` and ``self.v``."""
         w = self.layers[layer]
@@ -86,6 +93,7 @@ class Step:
 
     def attend(self, attn: int, layer: int, seqs: KV.Seqs, y, stream=None) -> None:
         """The rows' keys and values into the cache, attention, the o projection."""
+        self._check_seqs(seqs)
         one = self.single
         KV.lora_kv_append(self.cache, layer, seqs, None if one else self.seg_offset, self.n_rows, self.k,
                           self.kv_width, self.v, self.kv_width, stream)
@@ -98,6 +106,7 @@ class Step:
 
     def run(self, attn: int, seqs: KV.Seqs, x, y, stream=None) -> None:
         """Every layer: the first reads x, the others what the one before wrote to y."""
+        self._check_seqs(seqs)
         for i in range(len(self.layers)):
             self.project(i, x if i == 0 else y, stream)
             self.attend(attn, i, seqs, y, stream)

@@ -229,3 +229,19 @@ def test_more_children_than_pages(n_pages, kids):
                 w[:, dst, :, :rows] = w[:, src, :, :rows].clone()
         assert torch.equal(p.k.view(torch.int16), k.view(torch.int16))
         assert torch.equal(p.v.view(torch.int16), v.view(torch.int16))
+
+
+@pytest.mark.parametrize("stack", [(3, 12, 48)], indirect=True)
+@pytest.mark.parametrize("rows", [[3, 2], [1, 1], [1, 1, 1, 1], [4]])
+def test_a_segment_per_sequence_is_needed(stack, rows):
+    s = stack
+    step = T.Step(s.layers, s.srv.cache, rows, [0] * len(rows), HEADS, stream=s.st)
+    s.steps[tuple(rows)] = step
+    x = s.x(sum(rows))
+    y = torch.empty_like(x)
+    k = s.k.clone()
+    for call in (lambda: step.run(s.srv.attn, s.srv.seqs, x, y, s.st),
+                 lambda: step.attend(s.srv.attn, 0, s.srv.seqs, y, s.st)):
+        with pytest.raises(ValueError, match="segments"):
+            call()
+    assert torch.equal(k, s.k)
