@@ -61,6 +61,14 @@ class Step:
         offset = np.concatenate([[0], np.cumsum(seg_lens)]).astype(np.int32)
         self.n_rows = int(offset[-1])
         self.n_segments = len(seg_lens)
+        if len(seg_adapter) != self.n_segments or min(seg_lens, default=0) < 0:
+            raise ValueError("seg_lens and seg_adapter: a length of at least 0 and an adapter for every segment are needed")
+        for i, layer in enumerate(self.layers):
+            want = (("q", layer.q, 1, self.width), ("k", layer.k, 1, self.kv_width), ("v", layer.v, 1, self.kv_width),
+                    ("o", layer.o, 0, self.width))
+            for name, p, side, n in want:
+                if p.shape[side] != n:
+                    raise ValueError(f"layer {i}: the {name} projection is {p.shape}, the heads take {n}")
         self.single = all(n == 1 for n in seg_lens)      # one row per sequence: the decode form
         self.batch = L.Batch(offset, np.asarray(seg_adapter, np.int32), self.n_rows)
         dev, dt = cache.k.device, cache.k.dtype
@@ -85,15 +93,24 @@ class Step:
             raise ValueError(f"a step of {self.n_segments} segments with {int(seqs.lens.shape[0])} sequences: one segment "
                              "per sequence is needed, of no rows where it has none")
 
+    def _check_rows(self, name: str, t, width: int):
+        # (the launches read or write n_rows rows of this width)
+        if t.dim() != 2 or t.shape[0] < self.n_rows or t.shape[1] < width or t.dtype != self.q.dtype or \
+                t.device != self.q.device or t.stride(1) != 1:
+            raise ValueError(f"{name}: a {self.q.dtype} tensor of [{self.n_rows}, {width}] or more on {self.q.device}, dense "
+                             f"in the last dimension, is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
     def project(self, layer: int, x, stream=None) -> None:
         """q, k and v of the step's rows, into ``self.q``, ``self.k`` and ``self.v``."""
         w = self.layers[layer]
+        self._check_rows("x", x, w.q.shape[0])
         for p, y in ((w.q, self.q), (w.k, self.k), (w.v, self.v)):
             self._apply(p, x, y, stream)
 
     def attend(self, attn: int, layer: int, seqs: KV.Seqs, y, stream=None) -> None:
         """The rows' keys and values into the cache, attention, the o projection."""
         self._check_seqs(seqs)
+        self._check_rows("y", y, self.layers[layer].o.shape[1])
         one = self.single
         KV.lora_kv_append(self.cache, layer, seqs, None if one else self.seg_offset, self.n_rows, self.k,
                           self.kv_width, self.v, self.kv_width, stream)
@@ -107,6 +124,8 @@ class Step:
     def run(self, attn: int, seqs: KV.Seqs, x, y, stream=None) -> None:
         """Every layer: the first reads x, the others what the one before wrote to y."""
         self._check_seqs(seqs)
+        if self.layers:
+            self._check_rows("y", y, self.layers[0].o.shape[1])
         for i in range(len(self.layers)):
             self.project(i, x if i == 0 else y, stream)
             self.attend(attn, i, seqs, y, stream)

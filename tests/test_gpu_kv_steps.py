@@ -245,3 +245,32 @@ def test_a_segment_per_sequence_is_needed(stack, rows):
         with pytest.raises(ValueError, match="segments"):
             call()
     assert torch.equal(k, s.k)
+
+
+@pytest.mark.parametrize("stack", [(2, 12, 48)], indirect=True)
+def test_rows_and_projections_of_other_sizes_are_refused(stack):
+    s, st = stack, stack.st
+    for rows, adapters in (([2, 3], [0]), ([2, 3], [0, 1, 0]), ([2, -1], [0, 1])):
+        with pytest.raises(ValueError, match="segment"):
+            T.Step(s.layers, s.srv.cache, rows, adapters, HEADS, stream=st)
+    for heads in (2, 8):
+        with pytest.raises(ValueError, match="projection"):
+            T.Step(s.layers, s.srv.cache, [1, 1], [0, 1], heads, stream=st)
+    step = s.step([2, 3])
+    s.srv.grow(torch.tensor([2, 3], dtype=torch.int32, device=DEV))
+    x, y, k = s.x(5), torch.zeros((5, HIDDEN), dtype=s.dtype, device=DEV), s.k.clone()
+    wide = torch.zeros((5, 2 * HIDDEN), dtype=s.dtype, device=DEV)
+    for bad in (x[:4], x[:, :64], x.half(), x.float(), x.cpu(), wide[:, ::2], x.view(-1)):
+        for args in ((bad, y), (x, bad)):
+            with pytest.raises(ValueError):
+                step.run(s.srv.attn, s.srv.seqs, *args, st)
+        with pytest.raises(ValueError):
+            step.attend(s.srv.attn, 0, s.srv.seqs, bad, st)
+        with pytest.raises(ValueError):
+            step.project(0, bad, st)
+    assert torch.equal(k, s.k) and (y == 0).all()
+    wide[:, :HIDDEN] = x
+    step.run(s.srv.attn, s.srv.seqs, wide, y, st)            # rows further apart
+    other = torch.zeros_like(y)
+    step.run(s.srv.attn, s.srv.seqs, x, other, st)
+    assert torch.equal(y, other) and not (y == 0).all()
