@@ -48,8 +48,9 @@ class Layer:
 
 class Step:
     """What the layers of one step share: segment s of the batch holds the last
-    rows of sequence s, and every sequence has a segment (of length 0 if it has no rows).  Creation allocates and waits for ``stream``; ``run``
-    only enqueues, and may be recorded in a HIP graph."""
+    rows of sequence s, and every sequence has a segment (of length 0 if it has no rows).
+    Creation allocates and waits for ``stream``; ``run`` only enqueues, and may be
+    recorded in a HIP graph."""
 
     def __init__(self, layers: Sequence[Layer], cache: KV.Cache, seg_lens: Sequence[int], seg_adapter: Sequence[int],
                  n_heads: int, window: int = 0, n_sinks: int = 0, stream=None):
@@ -89,9 +90,9 @@ class Step:
 
     def _check_seqs(self, seqs: KV.Seqs):
         # (the launches read an offset per sequence)
-        if int(seqs.lens.shape[0]) != self.n_segments:
-            raise ValueError(f"a step of {self.n_segments} segments with {int(seqs.lens.shape[0])} sequences: one segment "
-                             "per sequence is needed, of no rows where it has none")
+        if seqs.n_seqs != self.n_segments:
+            raise ValueError(f"a step of {self.n_segments} segments with {seqs.n_seqs} sequences: one segment per sequence "
+                             "is needed, of no rows where it has none")
 
     def _check_rows(self, name: str, t, width: int):
         # (the launches read or write n_rows rows of this width)

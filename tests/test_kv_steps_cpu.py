@@ -47,3 +47,39 @@ def test_step_lengths_are_checked():
     assert fork(book(), parents=(0,), children=(3,)) == L.LORA_E_INDEX
     assert fork(book(), parents=(0, 1), children=(1, 2)) == L.LORA_E_ARG
     assert fork(book(page_rows=32)) == L.LORA_E_SHAPE
+
+
+def test_tensors_on_the_host_and_arrays_of_other_types_are_refused():
+    # nothing is launched: every call raises before it reaches the library
+    torch = pytest.importorskip("torch")
+    i32 = dict(dtype=torch.int32)
+    k = torch.zeros((1, 4, 2, 16, 8), dtype=torch.float16)
+    c = KV.Cache(k, k.clone())
+    tables, lens, refs, info = (torch.zeros(n, **i32) for n in ((3, 4), 3, 4, 2))
+    seqs, book = KV.Seqs(tables, lens, 64), KV.Book(tables, lens, refs, 16)
+    ws = torch.zeros(1 << 10, dtype=torch.uint8)
+    off, q = torch.zeros(4, **i32), torch.zeros((3, 16), dtype=torch.float16)
+    calls = [lambda: KV.lora_kv_append(c, 0, seqs, off, 3, q, 16, q, 16), lambda: KV.lora_kv_grow(book, lens, info, ws, 1024),
+             lambda: KV.lora_attn_decode(1, c, 0, seqs, 2, q, 16, q, 16, 1.0),
+             lambda: KV.lora_attn_prompt(1, c, 0, seqs, off, 3, 2, q, 16, q, 16, 1.0),
+             lambda: KV.lora_kv_grow_step(book, lens, 64, lens.clone(), info, ws, 1024),
+             lambda: KV.lora_kv_fork(c, book, [0], [1], info, ws, 1024),
+             lambda: KV.lora_kv_fork_step(c, book, [0], [1], lens.clone(), info, ws, 1024),
+             lambda: KV.lora_kv_free(book, [0]), lambda: KV.lora_kv_trim(book, 4), lambda: KV.lora_kv_copy(c, [0], [1]),
+             lambda: KV.lora_kv_compact(c, book, tables, refs, info, ws, 1024)]
+    for call in calls:
+        with pytest.raises(ValueError, match="device tensors"):
+            call()
+    meta = torch.zeros(3, device="meta", **i32)
+    for make in (lambda: KV.Seqs(tables, meta, 64), lambda: KV.Book(tables, lens, meta, 16),
+                 lambda: KV.Cache(k, k.to("meta"))):
+        with pytest.raises(ValueError, match="one device"):
+            make()
+    assert KV._words("add", lens, 3, book) == lens.data_ptr() and KV._words("add", None, 3, book) == 0
+    assert KV._words("add", P, 3, book) == P and KV._space(ws, 1024, book) == ws.data_ptr()
+    for bad in (lens.long(), lens.float(), lens.short(), lens[:2], torch.zeros(6, **i32)[::2], meta):
+        with pytest.raises(ValueError, match="add"):
+            KV._words("add", bad, 3, book)
+    for bad in (ws[:1023], torch.zeros(2048, dtype=torch.uint8)[::2], ws.to("meta")):
+        with pytest.raises(ValueError, match="ws"):
+            KV._space(bad, 1024, book)
