@@ -46,6 +46,14 @@ class Layer:
     o: Projection
 
 
+def _ordered(stream, device):
+    """A context in which tensors are made in the order of the stream's launches: they
+    may not be filled on another stream, nor be memory that one still uses."""
+    import torch
+    handle = L._stream(stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device))
+
+
 class Step:
     """What the layers of one step share: segment s of the batch holds the last
     rows of sequence s, and every sequence has a segment (of length 0 if it has no rows).
@@ -73,11 +81,12 @@ class Step:
         self.single = all(n == 1 for n in seg_lens)      # one row per sequence: the decode form
         self.batch = L.Batch(offset, np.asarray(seg_adapter, np.int32), self.n_rows)
         dev, dt = cache.k.device, cache.k.dtype
-        self.seg_offset = torch.from_numpy(offset).to(dev)
-        self.q = torch.empty((self.n_rows, self.width), dtype=dt, device=dev)
-        self.k = torch.empty((self.n_rows, self.kv_width), dtype=dt, device=dev)
-        self.v = torch.empty_like(self.k)
-        self.a = torch.empty_like(self.q)
+        with _ordered(stream, dev):
+            self.seg_offset = torch.from_numpy(offset).to(dev)
+            self.q = torch.empty((self.n_rows, self.width), dtype=dt, device=dev)
+            self.k = torch.empty((self.n_rows, self.kv_width), dtype=dt, device=dev)
+            self.v = torch.empty_like(self.k)
+            self.a = torch.empty_like(self.q)
         self._plans = {}
         for layer in self.layers:
             for p in (layer.q, layer.k, layer.v, layer.o):
@@ -153,21 +162,22 @@ class Server:
         ld = -(-max_len // page_rows)
         self.cache, self.stream, self.max_len = cache, stream, max_len
         i32 = dict(dtype=torch.int32, device=dev)
-        self.tables = torch.full((n_seqs, ld), -1, **i32)
-        self.lens = torch.zeros(n_seqs, **i32)
-        self.step_lens = torch.zeros(n_seqs, **i32)
-        self.refs = torch.zeros(n_pages, **i32)
-        self.info = torch.zeros(2, **i32)
-        self.book = KV.Book(self.tables, self.lens, self.refs, page_rows)
-        self.seqs = KV.Seqs(self.tables, self.step_lens, max_len)
-        self.ws_bytes = KV.lora_kv_workspace_bytes(self.book)
-        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+        with _ordered(stream, dev):
+            self.tables = torch.full((n_seqs, ld), -1, **i32)
+            self.lens = torch.zeros(n_seqs, **i32)
+            self.step_lens = torch.zeros(n_seqs, **i32)
+            self.refs = torch.zeros(n_pages, **i32)
+            self.info = torch.zeros(2, **i32)
+            self.book = KV.Book(self.tables, self.lens, self.refs, page_rows)
+            self.seqs = KV.Seqs(self.tables, self.step_lens, max_len)
+            self.ws_bytes = KV.lora_kv_workspace_bytes(self.book)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
         self.attn = KV.lora_attn_create(dev.index or 0, stream)
 
     def grow(self, add) -> None:
         """``add``: int32 device tensor [n_seqs], the step's rows of each sequence.  ``info``
         then holds (pages taken, sequences that did not fit), ``step_lens`` 0 for those and
-        for those without rows; reading them waits for the stream."""
+        for those without rows; to be read on the server's stream, which the host then waits for."""
         KV.lora_kv_grow_step(self.book, add, self.max_len, self.step_lens, self.info, self.ws, self.ws_bytes,
                              self.stream)
 

@@ -274,3 +274,50 @@ def test_rows_and_projections_of_other_sizes_are_refused(stack):
     other = torch.zeros_like(y)
     step.run(s.srv.attn, s.srv.seqs, x, other, st)
     assert torch.equal(y, other) and not (y == 0).all()
+
+
+@pytest.mark.parametrize("form", ["torch", "handle", "default"])
+def test_a_server_on_a_stream_that_is_not_current(form):
+    # the current stream is busy while the server is made and used on the other one
+    n_seqs, rows, dt = 3, [5, 20, 1], torch.bfloat16
+    layers, kept = T.random_layers(1, HIDDEN, HEADS, KV_HEADS, DIM, dt, [4, 8], DEV, 3, torch.cuda.current_stream())
+    gen = torch.Generator().manual_seed(2)
+    x = torch.randn((sum(rows), HIDDEN), generator=gen).to(dt).to(DEV)
+    add = torch.tensor(rows, dtype=torch.int32, device=DEV)
+    busy = torch.randn((8192, 8192), device=DEV)
+    shape = (1, 6, KV_HEADS, PR, DIM)
+
+    def serve(stream):
+        cache = KV.Cache(*(torch.zeros(shape, dtype=dt, device=DEV) for _ in range(2)))
+        y = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        if stream is not None:
+            for _ in range(12):
+                torch.mm(busy, busy)             # some milliseconds each in float32
+        srv = T.Server(cache, n_seqs, 32, stream)
+        step = T.Step(layers, cache, rows, [0, 1, 0], HEADS, stream=stream)
+        srv.grow(add)
+        step.run(srv.attn, srv.seqs, x, y, stream)
+        torch.cuda.synchronize()
+        out = [t.clone() for t in (y, cache.k, cache.v, srv.tables, srv.lens, srv.refs, srv.info)]
+        torch.cuda.synchronize()
+        step.release()
+        srv.release()
+        return out
+
+    want = serve(None)                           # everything on the default stream
+    assert want[4].tolist() == rows and want[6].tolist() == [4, 0] and not (want[0] == 0).all()
+    side = torch.cuda.Stream()
+    if form == "default":                        # a side stream is current, and the default one is used
+        with torch.cuda.stream(side):
+            for _ in range(12):
+                torch.mm(busy, busy)
+            got = serve(None)
+    else:
+        got = serve(side if form == "torch" else side.cuda_stream)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    for layer in layers:
+        for p in (layer.q, layer.k, layer.v, layer.o):
+            L.lora_release_adapters(p.table)
+    del kept
