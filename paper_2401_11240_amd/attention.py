@@ -87,14 +87,39 @@ class Step:
             self.k = torch.empty((self.n_rows, self.kv_width), dtype=dt, device=dev)
             self.v = torch.empty_like(self.k)
             self.a = torch.empty_like(self.q)
-        self._plans = {}
-        for layer in self.layers:
-            for p in (layer.q, layer.k, layer.v, layer.o):
-                if p.shape not in self._plans:
-                    self._plans[p.shape] = L.lora_base_plan_create(p.table, self.batch, stream)
+        self._plans, self._plan_of = [], {}              # plans with their shapes; a table's plan
+        try:
+            for layer in self.layers:
+                for p in (layer.q, layer.k, layer.v, layer.o):
+                    self._plan_for(p, stream)
+        except Exception:
+            self.release()
+            raise
+
+    def _plan_for(self, p: Projection, stream):
+        """One plan serves all tables of a shape whose adapters agree in rank."""
+        if p.table in self._plan_of:
+            return
+        for shape, plan in self._plans:
+            if shape == p.shape and self._fits(plan, p):
+                break
+        else:
+            plan = L.lora_base_plan_create(p.table, self.batch, stream)
+            self._plans.append((p.shape, plan))
+        self._plan_of[p.table] = plan
+
+    @staticmethod
+    def _fits(plan: int, p: Projection) -> bool:
+        # (a call without operands enqueues nothing: it is refused for the table where that does not
+        # fit the plan, for the missing x where it does; a plan of no rows takes it)
+        try:
+            L.lora_base_plan_apply(plan, p.table, None, p.shape[0], None, p.shape[0], None, p.shape[1])
+        except L.LoraError as e:
+            return e.code == L.LORA_E_ARG
+        return True
 
     def _apply(self, p: Projection, x, y, stream):
-        L.lora_base_plan_apply(self._plans[p.shape], p.table, x, x.stride(0), p.wt, p.wt.stride(0), y, y.stride(0),
+        L.lora_base_plan_apply(self._plan_of[p.table], p.table, x, x.stride(0), p.wt, p.wt.stride(0), y, y.stride(0),
                                stream)
 
     def _check_seqs(self, seqs: KV.Seqs):
@@ -142,9 +167,9 @@ class Step:
 
     def release(self) -> None:
         """Frees the plans: no launch, recorded or enqueued, may still use them."""
-        for p in self._plans.values():
-            L.lora_base_plan_destroy(p)
-        self._plans = {}
+        for _, plan in self._plans:
+            L.lora_base_plan_destroy(plan)
+        self._plans, self._plan_of = [], {}
 
 
 class Server:

@@ -321,3 +321,49 @@ def test_a_server_on_a_stream_that_is_not_current(form):
         for p in (layer.q, layer.k, layer.v, layer.o):
             L.lora_release_adapters(p.table)
     del kept
+
+
+def test_projections_of_one_shape_and_other_ranks():
+    # q, k, v and o are all HIDDEN x HIDDEN here; their adapters differ in rank, between layers too
+    dt, st = torch.float16, torch.cuda.current_stream()
+    heads, dim, n = 4, HIDDEN // 4, [3, 20, 1]
+    parts = [T.random_layers(1, HIDDEN, heads, heads, dim, dt, ranks, DEV, i, st)
+             for i, ranks in enumerate([[4, 8], [8, 4], [16, 8], [4, 8], [4, 8, 2]])]
+    one = [p[0][0] for p in parts]
+    layers = [T.Layer(one[0].q, one[1].k, one[2].v, one[3].o), T.Layer(one[3].q, one[0].k, one[0].v, one[1].o),
+              T.Layer(one[4].q, one[4].k, one[4].v, one[4].o)]
+    cache = KV.Cache(*(torch.zeros((3, 9, heads, PR, dim), dtype=dt, device=DEV) for _ in range(2)))
+    srv = T.Server(cache, 3, 32, st)
+    step = T.Step(layers, cache, n, [0, 1, 0], heads, stream=st)
+    x = torch.randn((sum(n), HIDDEN), generator=torch.Generator().manual_seed(1)).to(dt).to(DEV)
+    y = torch.empty_like(x)
+    srv.grow(torch.tensor(n, dtype=torch.int32, device=DEV))
+
+    def alone(p, src):                           # the projection's one call, without a plan
+        batch = L.Batch(step.batch.seg_offset, [0, 1, 0], sum(n))
+        nb = L.lora_base_workspace_bytes(p.table, batch)
+        ws, out = torch.empty(nb, dtype=torch.uint8, device=DEV), torch.empty_like(src)
+        L.lora_base_apply(p.table, batch, src, HIDDEN, p.wt, HIDDEN, out, HIDDEN, ws, nb, st)
+        torch.cuda.synchronize()
+        return out
+
+    src = x
+    for i, layer in enumerate(layers):
+        step.project(i, src, st)
+        step.attend(srv.attn, i, srv.seqs, y, st)
+        torch.cuda.synchronize()
+        for p, a, b in ((layer.q, src, step.q), (layer.k, src, step.k), (layer.v, src, step.v), (layer.o, step.a, y)):
+            assert torch.equal(alone(p, a), b), i
+        src = y.clone()
+    done = y.clone()
+    step.run(srv.attn, srv.seqs, x, y, st)
+    assert torch.equal(done, y)
+    assert len(step._plans) == 3                 # ranks (4, 8), (8, 4), (16, 8): the third adapter is in no segment
+    torch.cuda.synchronize()
+    step.release()
+    with pytest.raises(L.LoraError):             # an adapter that a table lacks: nothing is left behind
+        T.Step(layers, cache, n, [0, 2, 0], heads, stream=st)
+    srv.release()
+    for layer in one:
+        for p in (layer.q, layer.k, layer.v, layer.o):
+            L.lora_release_adapters(p.table)
