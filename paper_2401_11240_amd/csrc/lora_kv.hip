@@ -392,18 +392,22 @@ __global__ void __launch_bounds__(kCopyThreads) lora_kv_release_kernel(Book b, I
     if (threadIdx.x == 0) b.lens[s] = 0;
 }
 
+// (a grid of one workgroup per sequence ends where its threads pass 32 bits)
+constexpr int kTrimBlocks = 1 << 20;
+
 __global__ void __launch_bounds__(kCopyThreads) lora_kv_trim_kernel(Book b, int32_t window, int32_t n_sinks) {
-    const int s = blockIdx.x;
-    const int len = b.lens[s];
-    const int n = held(b, len);
-    int32_t* table = b.tables + (int64_t)s * b.ld_table;
-    for (int e = threadIdx.x; e < n; e += kCopyThreads) {
-        const int64_t first = (int64_t)e << b.page_shift, last = first + (1 << b.page_shift) - 1;
-        // the row at position len sees tokens from len + 1 - window on; later rows later ones
-        if (last > (int64_t)len - window || first < n_sinks) continue;
-        const int p = table[e];
-        if (is_page(b, p)) atomicSub(b.refs + p, 1);
-        table[e] = -1;
+    for (int64_t s = blockIdx.x; s < b.n_seqs; s += gridDim.x) {
+        const int len = b.lens[s];
+        const int n = held(b, len);
+        int32_t* table = b.tables + s * b.ld_table;
+        for (int e = threadIdx.x; e < n; e += kCopyThreads) {
+            const int64_t first = (int64_t)e << b.page_shift, last = first + (1 << b.page_shift) - 1;
+            // the row at position len sees tokens from len + 1 - window on; later rows later ones
+            if (last > (int64_t)len - window || first < n_sinks) continue;
+            const int p = table[e];
+            if (is_page(b, p)) atomicSub(b.refs + p, 1);
+            table[e] = -1;
+        }
     }
 }
 
@@ -865,7 +869,8 @@ int lora_kv_trim(const lora_kv_book_t* b, int32_t window, int32_t n_sinks, void*
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
     if (!g.ok) return no_device("lora_kv_trim");
-    hipLaunchKernelGGL(lora_kv_trim_kernel, dim3(b->n_seqs), dim3(kCopyThreads), 0, st, device_book(b), window, n_sinks);
+    hipLaunchKernelGGL(lora_kv_trim_kernel, dim3(std::min(b->n_seqs, kTrimBlocks)), dim3(kCopyThreads), 0, st,
+                       device_book(b), window, n_sinks);
     return check_launch("lora_kv_trim");
 }
 

@@ -367,3 +367,19 @@ def test_projections_of_one_shape_and_other_ranks():
     for layer in one:
         for p in (layer.q, layer.k, layer.v, layer.o):
             L.lora_release_adapters(p.table)
+
+
+def test_trim_of_more_sequences_than_a_grid_takes():
+    n, held = (1 << 20) + 300, 400               # the last ones have three pages each
+    i32 = dict(dtype=torch.int32, device=DEV)
+    tables, lens = torch.full((n, 3), -1, **i32), torch.zeros(n, **i32)
+    tables[n - held:] = torch.randperm(3 * held, generator=torch.Generator().manual_seed(0)).view(held, 3).to(DEV)
+    lens[n - held:] = torch.arange(33, 33 + 16, device=DEV).repeat(held // 16).int()
+    refs = torch.ones(3 * held, **i32)
+    before = tables.clone()
+    KV.lora_kv_trim(KV.Book(tables, lens, refs, PR), 10, 1, torch.cuda.current_stream())
+    gone = lens[n - held:] - 10 >= 31            # the second page; the first holds the sink
+    want = before.clone()
+    want[n - held:, 1] = torch.where(gone, -1, before[n - held:, 1])
+    assert torch.equal(tables, want)
+    assert gone.any() and refs.sum().item() == 3 * held - int(gone.sum())
