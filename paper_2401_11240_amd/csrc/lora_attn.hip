@@ -65,7 +65,7 @@
 //
 //   A hidden token's value may be anything. Its weight is zero, which keeps it out
 //   unless it is an infinity or a NaN. So a tile whose output is not finite is
-//   computed again by run_careful().
+//   computed again by run_careful(), and so is one whose scores reach 2^21 powers of two.
 //
 //   Measured: 2048 rows behind 14336 tokens, 64/8 heads of width 128, bf16: 0.98-1.0
 //   ms, 1.03-1.05 PFLOP/s (library products reach 1.3 at their best), matrix cores
@@ -584,6 +584,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kCols = 128;                 // columns (row, head) of a workgroup: 32 per wave
 constexpr int kKeys = 64;                  // tokens per step
 constexpr float kSlack = 8.f;              // how far (in powers of two) a maximum may rise before the sums are rescaled
+// A score of this many powers of two and more: s c - m in one rounding is then off from s c rounded, which
+// m is, by half an ulp of m, an eighth of a power of two here, and from 2^31 on by more than weights hold.
+constexpr float kWild = 0x1p21f;
 
 struct PromptArgs {
     AttnArgs a;
@@ -906,11 +909,22 @@ struct PromptBlock {
             }
         }
     }
+    // A score relative to ref, in powers of two.  kAnySize: also where they are very large (kWild); the product is
+    // then rounded as that of the maximum was.
+    template <bool kAnySize>
+    __device__ __forceinline__ float relative(float s, float ref) const {
+        const float x = __builtin_fmaf(s, c, -ref);
+        if (!kAnySize) return x;
+        float y = s * c;
+        asm volatile("" : "+v"(y));                      // not one rounding after all
+        return fabsf(ref) >= kWild ? y - ref : x;
+    }
     // Weights of pair z of this lane's 32 tokens: pw[t] is the B operand of tokens 16 t on.
+    template <bool kAnySize = false>
     __device__ __forceinline__ void weigh_pair(const f32x16 (&s)[2], u32x4 (&pw)[4], int z, float ref) {
         const int kt = z >> 3, r = 2 * (z & 7);
-        uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r], c, -ref)),
-                                __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r + 1], c, -ref)));
+        uint32_t x = Fmt::pack2(__builtin_amdgcn_exp2f(relative<kAnySize>(s[kt][r], ref)),
+                                __builtin_amdgcn_exp2f(relative<kAnySize>(s[kt][r + 1], ref)));
         asm volatile("" : "+v"(x));                      // here, and not where the compiler would rather have it
         pw[z >> 2][z & 3] = x;
         sum = add_pair<Fmt>(x, sum);
@@ -1049,7 +1063,8 @@ struct PromptBlock {
         __builtin_amdgcn_s_waitcnt(0);
     }
 
-    // The same as run() and run_own() with infinities and NaN among the values.  A token that a column
+    // The same as run() and run_own() with infinities and NaN among the values, or with scores of any
+    // size (kWild).  A token that a column
     // does not see has weight zero, which is as good as leaving it out unless its
     // value is one of those.  Here such values, in steps that only some columns see,
     // are kept out of the product and added to the columns that see them; the
@@ -1077,7 +1092,7 @@ struct PromptBlock {
             const float ref = m == -INFINITY ? 0.f : m;
             u32x4 pw[4];
 #pragma unroll
-            for (int z = 0; z < 16; ++z) weigh_pair(s, pw, z, ref);
+            for (int z = 0; z < 16; ++z) weigh_pair<true>(s, pw, z, ref);
 #pragma unroll
             for (int f = 0; f < 4 * ND; ++f) {
                 u32x4 x = read_v(f, 0);
@@ -1122,14 +1137,16 @@ struct PromptBlock {
         __builtin_amdgcn_s_waitcnt(0);
         if (KS == 1) __builtin_amdgcn_s_barrier();
     }
-    // Is an output not finite?  It may come from a token that the column does not see.
-    __device__ __forceinline__ bool infinite() const {
+    // Is an output not finite?  It may come from a token that the column does not see.  Or was the column's
+    // largest score too large for the fast weights?  (One that was on the way to a maximum nearer to zero
+    // has left nothing, or infinities.)
+    __device__ __forceinline__ bool doubtful() const {
         float x = 0.f;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) x += o[d][r] * 0.f;
-        return !(x == 0.f);
+        return !(x == 0.f) || (fabsf(m) >= kWild && m != -INFINITY);
     }
     // The queries of this lane's column at q, if there is one.
     __device__ __forceinline__ void load_q(const uint16_t* at, bool real) {
@@ -1222,7 +1239,7 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
     blk.load_q(a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim, real);
     const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
     blk.run(i0, i1);
-    if (blk.infinite()) bad = 1;
+    if (blk.doubtful()) bad = 1;
     __syncthreads();
     if (bad) blk.run_careful(i0, i1);
     if (pa.parts > 1) {
@@ -1335,7 +1352,7 @@ __global__ void __launch_bounds__(256, 1) lora_attn_prompt_few_kernel(PromptArgs
         blk.load_q(a.q + (p.row0 + (real ? row : 0)) * a.ldq + (int64_t)head * a.head_dim, real);
         const int i0 = (int)((int64_t)p.steps * part / pa.parts), i1 = (int)((int64_t)p.steps * (part + 1) / pa.parts);
         blk.run_own(i0, i1);
-        if (__any(blk.infinite())) blk.run_careful(i0, i1);
+        if (__any(blk.doubtful())) blk.run_careful(i0, i1);
         // the waves' results meet: each has its own part of LDS, read by itself so far
 #pragma unroll
         for (int d = 0; d < ND; ++d)
