@@ -116,6 +116,13 @@ constexpr int kWaveTokens = 32;
 constexpr int kHeads = 16;                 // q heads per group tile (columns of the MFMA)
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// Weights are taken 2^kLift above their maximum's 1, in binary16, and the factor cancels in the division by their
+// sum: what is rounded to zero begins 2^-32 below the largest instead of 2^-25 (131072 tokens just below
+// 2^-25, behind a first token that holds the maximum, were 0.4% of a sum and came out as none).
+// With kSlack more the largest is 2^15.
+template <class Fmt>
+constexpr float kLift = Fmt::kNarrowRange ? 7.f : 0.f;
+
 constexpr int kCounters = 3;               // per workgroup: see arrive()
 
 // The join gives a tile's q heads 16 threads each, of 256; what they leave goes to parts.
@@ -278,8 +285,8 @@ struct DecodeWave {
                           fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
         top = max_over_quarters(top);
         const float mn = fmaxf(m, top);
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        const float f = __builtin_amdgcn_exp2f(m - ref);
+        const float most = mn == -INFINITY ? 0.f : mn, ref = most - kLift<Fmt>;
+        const float f = __builtin_amdgcn_exp2f(m - most);
         m = mn;
         u32x4 pw;
         float add = 0.f;
@@ -917,7 +924,7 @@ struct PromptBlock {
         if (!kAnySize) return x;
         float y = s * c;
         asm volatile("" : "+v"(y));                      // not one rounding after all
-        return fabsf(ref) >= kWild ? y - ref : x;
+        return fabsf(ref) >= kWild ? y - m + kLift<Fmt> : x;     // (ref itself would be rounded)
     }
     // Weights of pair z of this lane's 32 tokens: pw[t] is the B operand of tokens 16 t on.
     template <bool kAnySize = false>
@@ -967,7 +974,7 @@ struct PromptBlock {
         if (!all_see(i, has)) hide(s, i, has);
         top = highest(s);
         rescale();
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = m == -INFINITY ? 0.f : m - kLift<Fmt>;
 #pragma unroll
         for (int z = 0; z < 4; ++z) weigh_pair(s, pw, z, ref);
         __builtin_amdgcn_sched_barrier(0);
@@ -1089,7 +1096,7 @@ struct PromptBlock {
             if (edge) hide(s, i, has_load);
             top = highest(s);
             rescale();
-            const float ref = m == -INFINITY ? 0.f : m;
+            const float ref = m == -INFINITY ? 0.f : m - kLift<Fmt>;
             u32x4 pw[4];
 #pragma unroll
             for (int z = 0; z < 16; ++z) weigh_pair<true>(s, pw, z, ref);

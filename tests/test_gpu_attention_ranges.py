@@ -86,3 +86,39 @@ def test_scores_that_come_up_from_far_below(attn, dtype, heads):
             _, _, reach = R.attention(c.q[r:r + 1], near, c.v, c.table[0], lo + r + 1, lo + r, c.scale, 0, 0)
             tol = R.allowance(ref, m, reach, 64, 400, dtype == "bf16")
             assert (np.abs(got[r:r + 1] - ref) <= tol).all(), (kind, r)
+
+
+@pytest.mark.parametrize("kind,heads,lens", [("prompt", 2, [131072]), ("prompt", 72, [131072]), ("prompt", 2, [20000, 9000]),
+                                             ("decode", 2, [1024] * 1024), ("decode", 16, [131072, 5])])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_long_tail_of_weights_far_below_the_largest(attn, dtype, kind, heads, lens):
+    # the first token has weight 1 and value 0, the others 2^-26.4 and values of 1 to 2: they are the output.
+    # A weight of 2^-26.4, times 2^7, is off by half of binary16's smallest, 2^-25 of 2^-19.4: 2^-5.6 of it, all
+    # alike, in the output and (hardly) in the sum; bfloat16 rounds it by 2^-9.  Then the output's own rounding.
+    rows = [{72: 120}.get(heads, 40) if kind == "prompt" else 1 for _ in lens]
+    c = Case(dtype, heads, 1, 64, 256, lens, [min(r, n) for r, n in zip(rows, lens)], seed=37)
+    k = torch.zeros(c.kd[0].shape, dtype=torch.float32)
+    for s in range(len(lens)):
+        k[c.table[s, 0], :, 0, 0] = 15.0
+    c.kd[0].copy_(k)
+    v = torch.where(torch.isnan(c.vd[0]), c.vd[0], 1 + c.vd[0].abs().clamp(max=1))
+    for s in range(len(lens)):
+        v[int(c.table[s, 0]), :, 0] = 0
+    c.vd[0].copy_(v)
+    c.qd.zero_()
+    for h in range(heads):
+        c.qd[:, h * 64] = 9.75                   # 15 * 9.75 / 8 = 18.28 = 26.4 powers of two
+    getattr(c, kind)(attn)
+    got = c.got()
+    vv = c.vd[0].double().cpu().numpy()
+    w = np.exp(-15 * 9.75 / 8)
+    at = 0
+    for s, n in enumerate(lens):
+        tokens = vv[c.table[s, :-(-n // 256)], 0].reshape(-1, 64)[:n]
+        sums = np.cumsum(tokens, axis=0)
+        for r in range(c.rows[s]):
+            j = n - c.rows[s] + r                # sees tokens 0 .. j
+            want = w * sums[j] / (1 + w * j)
+            tol = (2.0 ** -5.6 if dtype == "f16" else 2.0 ** -8) * 1.1 * want + 2.0 ** -25
+            assert (np.abs(got[at] - want) <= tol).all(), (s, r, got[at, 0, :4], want[:4])
+            at += 1
