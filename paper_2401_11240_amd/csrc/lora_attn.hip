@@ -1175,7 +1175,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, int cols, int keys,
     auto rows_of = [&](int s, int& row0) {
         const int lo = a.seg_offset[s], hi = a.seg_offset[s + 1];
         row0 = min(max(lo, 0), a.n_rows);
-        return max(min(hi, a.n_rows) - row0, 0);
+        return max(min(max(hi, 0), a.n_rows) - row0, 0);       // (both in [0, n_rows]: no difference wraps)
     };
     auto tiles_of = [&](int n) { return (int)(((int64_t)n * a.group + cols - 1) / cols); };
     int seq = l * per, row0 = 0, n = 0, len = 0, mine = 0;     // the lane's first segment
