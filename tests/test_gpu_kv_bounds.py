@@ -1,4 +1,5 @@
-"""What the device's arrays hold leads nowhere outside the buffers."""
+"""What the device's arrays hold leads nowhere outside the buffers, and a launch sized for
+more tokens than there are gives what one sized for them gives."""
 import itertools
 
 import pytest
@@ -62,3 +63,21 @@ def test_offsets_out_of_order_stay_inside(attn, heads, kv_heads, dim, page_rows)
     # the handle's counters are as they were: an ordinary launch
     c.prompt(attn)
     c.check(what="after offsets out of order")
+
+
+@pytest.mark.parametrize("lens,rows", [([203], [203]), ([203, 1, 0, 40], [100, 1, 0, 40]), ([1], [1])])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(32, 32, 128), (4, 2, 64), (64, 2, 128), (8, 1, 256), (72, 1, 64)])
+@pytest.mark.parametrize("max_len,window,sinks", [(1024, 0, 0), (32768, 0, 0), (1 << 20, 0, 0), (32768, 50, 3)])
+def test_capacity_far_above_the_lengths(attn, lens, rows, heads, kv_heads, dim, max_len, window, sinks):
+    # most parts of such a launch have no token
+    c = Case("bf16", heads, kv_heads, dim, 16, lens, rows, seed=len(lens))
+    tables = torch.full((len(lens), max_len // 16), -1, dtype=torch.int32, device=DEV)
+    tables[:, :c.tables.shape[1]] = c.tables
+    c.seqs = KV.Seqs(tables, c.lens_d, max_len)
+    c.prompt(attn, window, sinks)
+    c.check(window, sinks, f"prompt {rows} behind {lens}, capacity {max_len}, {heads}/{kv_heads} x {dim}")
+    c = Case("f16", heads, kv_heads, dim, 16, lens, [1] * len(lens), seed=len(lens))
+    c.seqs = KV.Seqs(tables, c.lens_d, max_len)
+    tables[:, :c.tables.shape[1]] = c.tables
+    c.decode(attn, window, sinks)
+    c.check(window, sinks, f"decode {lens}, capacity {max_len}")
