@@ -1288,10 +1288,10 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
                 f32x4 y[4][4];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    const int at = z + b < pa.parts ? (z + b) * PF * 4 : kOut;
-                    ms[b] = bload8<kCoherent>(all, at + at_ms);
+                    const uint32_t at = z + b < pa.parts ? (uint32_t)(z + b) * PF * 4 : (uint32_t)kOut;
+                    ms[b] = bload8<kCoherent>(all, (int)(at + at_ms));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[b][e] = as_f4(bload16<kCoherent>(all, at + ((4 * d + e) * 256 + t) * 16));
+                    for (int e = 0; e < 4; ++e) y[b][e] = as_f4(bload16<kCoherent>(all, (int)(at + ((4 * d + e) * 256 + t) * 16)));
                 }
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
@@ -1419,10 +1419,10 @@ __global__ void __launch_bounds__(256, 1) lora_attn_prompt_few_kernel(PromptArgs
             f32x4 x[4][4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const int at = z + b < pa.parts ? (z + b) * PF * 4 : kOut;
-                ms[b] = bload8<kCoherent>(all, at + (kFewCols * DP + 2 * c) * 4);
+                const uint32_t at = z + b < pa.parts ? (uint32_t)(z + b) * PF * 4 : (uint32_t)kOut;
+                ms[b] = bload8<kCoherent>(all, (int)(at + (kFewCols * DP + 2 * c) * 4));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[b][e] = as_f4(bload16<kCoherent>(all, at + ((4 * block + e) * 64 + l) * 16));
+                for (int e = 0; e < 4; ++e) x[b][e] = as_f4(bload16<kCoherent>(all, (int)(at + ((4 * block + e) * 64 + l) * 16)));
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
