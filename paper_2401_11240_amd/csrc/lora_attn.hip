@@ -106,7 +106,7 @@ struct AttnArgs {
     const int32_t *tables, *lens, *seg_offset;
     int64_t page_stride, head_stride, row_stride, ldq, ldo;
     int32_t n_rows, n_seqs, ld_table, max_len, n_pages, page_shift;
-    int32_t n_heads, group, head_dim;
+    int32_t group, head_dim;
     int32_t window, n_sinks;
     float scale;
 };
@@ -1524,7 +1524,6 @@ AttnArgs attn_args(const lora_kv_cache_t* c, int32_t layer, const lora_kv_seqs_t
     a.n_pages = c->n_pages;
     a.page_shift = 0;
     while ((1 << a.page_shift) < c->page_rows) ++a.page_shift;
-    a.n_heads = n_heads;
     a.group = n_heads / c->n_kv_heads;
     a.head_dim = c->head_dim;
     a.window = window < s->max_len ? window : 0;    // (one that long hides nothing)
