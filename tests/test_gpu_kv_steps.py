@@ -383,3 +383,37 @@ def test_trim_of_more_sequences_than_a_grid_takes():
     want[n - held:, 1] = torch.where(gone, -1, before[n - held:, 1])
     assert torch.equal(tables, want)
     assert gone.any() and refs.sum().item() == 3 * held - int(gone.sum())
+
+
+@pytest.mark.parametrize("stack", [(6, 20, 90), (6, 11, 70), (6, 64, 90)], indirect=True)
+@pytest.mark.parametrize("seed", range(2))
+def test_service_on_a_pool_that_runs_out(stack, seed):
+    # prompts, chunks, tokens, branches, ends and compactions in random order
+    s, rng = stack, np.random.default_rng(seed)
+    granted = refused = 0
+    for _ in range(40):
+        what = rng.integers(6)
+        if what == 0:
+            gone = [int(i) for i in rng.permutation(6)[:rng.integers(3)]]
+            s.srv.free(gone)
+            s.ref.free(gone)
+        elif what == 1:
+            ids = [int(i) for i in rng.permutation(6)]
+            parents, kids = ids[:2], ids[2:2 + rng.integers(3)]
+            pairs = [parents[int(i)] for i in rng.integers(0, 2, len(kids))]
+            s.srv.fork(pairs, kids)
+            s.ref.fork(pairs, kids)
+        elif what == 2:
+            s.srv.compact()
+            s.ref.compact()
+        form = rng.integers(3)
+        if form == 0:
+            add = [int(a) for a in rng.choice([0, 1, 1, 1], size=6)]
+            rows = [1] * 6
+        else:
+            rows = [int(a) for a in rng.choice([0, 1, 3, 16, 17, 40], size=6)]
+            add = [r if rng.integers(5) else 0 for r in rows]
+        has = s.token(add, rows)
+        granted += sum(has)
+        refused += sum(1 for a, h in zip(add, has) if a and not h)
+    assert granted and refused
