@@ -378,8 +378,9 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_grow_kernel(Book b, cons
 }
 
 // Sequence ids in the arguments give their pages back: one workgroup each, which
-// leaves length 0 and entries -1.  (stride 2, first 1: the children of pairs)
-__global__ void __launch_bounds__(kCopyThreads) lora_kv_release_kernel(Book b, IdArgs ids, int stride, int first) {
+// leaves length 0 and entries -1.  (stride 2, first 1: the children of pairs; step_lens may be NULL)
+__global__ void __launch_bounds__(kCopyThreads) lora_kv_release_kernel(Book b, IdArgs ids, int stride, int first,
+                                                                       int32_t* step_lens) {
     const int s = ids.id[blockIdx.x * stride + first];
     const int n = held(b, b.lens[s]);
     int32_t* table = b.tables + (int64_t)s * b.ld_table;
@@ -389,7 +390,11 @@ __global__ void __launch_bounds__(kCopyThreads) lora_kv_release_kernel(Book b, I
         table[e] = -1;
     }
     __syncthreads();
-    if (threadIdx.x == 0) b.lens[s] = 0;
+    if (threadIdx.x == 0) {
+        b.lens[s] = 0;
+        // (rows that a child had in a step under way would land in pages that it shares from here on)
+        if (step_lens) step_lens[s] = 0;
+    }
 }
 
 // (a grid of one workgroup per sequence ends where its threads pass 32 bits)
@@ -460,13 +465,10 @@ __global__ void __launch_bounds__(kBookThreads) lora_kv_fork_pages_kernel(ForkAr
 
 // Workgroups y < n: row y of the children's tables and lengths (x == 0), and unit x of
 // the copy of its last page's rows.
-__global__ void __launch_bounds__(kCopyThreads) lora_kv_fork_kernel(Book b, PageDims d, IdArgs ids, BookWs w,
-                                                                    int32_t* step_lens) {
+__global__ void __launch_bounds__(kCopyThreads) lora_kv_fork_kernel(Book b, PageDims d, IdArgs ids, BookWs w) {
     const int pair = blockIdx.y;
     const int parent = ids.id[2 * pair], child = ids.id[2 * pair + 1];
     const int fresh = w.sums[pair];
-    // (what the child had of a step under way would land in pages that it now shares)
-    if (step_lens && blockIdx.x == 0 && threadIdx.x == 0) step_lens[child] = 0;
     if (fresh == -2) return;               // the child is empty already
     int len, src;
     fork_tail(b, parent, len, src);
@@ -740,13 +742,12 @@ int enqueue_fork(const char* name, const lora_kv_cache_t* c, const lora_kv_book_
                 ids.id[2 * i + 1] = children[i0 + i];
             }
             if (pass == 0) {
-                hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, book, ids, 2, 1);
+                hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, book, ids, 2, 1, step_lens);
             } else {
                 hipLaunchKernelGGL(lora_kv_fork_pages_kernel, dim3(1), dim3(kBookThreads), 0, st,
                                    ForkArgs{book, w, info, m, (int)(i0 == 0), ids});
                 if (m > 0)
-                    hipLaunchKernelGGL(lora_kv_fork_kernel, dim3(1 + units, m), dim3(kCopyThreads), 0, st, book, d, ids, w,
-                                       step_lens);
+                    hipLaunchKernelGGL(lora_kv_fork_kernel, dim3(1 + units, m), dim3(kCopyThreads), 0, st, book, d, ids, w);
             }
             if (int rc = check_launch(name)) return rc;
         }
@@ -856,7 +857,8 @@ int lora_kv_free(const lora_kv_book_t* b, int32_t n, const int32_t* seqs, void* 
     for (int32_t i0 = 0; i0 < n; i0 += kArgIds) {
         const int m = std::min(kArgIds, n - i0);
         for (int i = 0; i < m; ++i) ids.id[i] = seqs[i0 + i];
-        hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, device_book(b), ids, 1, 0);
+        hipLaunchKernelGGL(lora_kv_release_kernel, dim3(m), dim3(kCopyThreads), 0, st, device_book(b), ids, 1, 0,
+                           (int32_t*)nullptr);
         if (int rc = check_launch("lora_kv_free")) return rc;
     }
     return LORA_OK;
