@@ -33,7 +33,9 @@
  * entries of pages in which no token is visible are not used.  Scores, the softmax's maximum and
  * sum and the output's sums are float32; a weight is rounded to the storage
  * type for the product with V, and the sum of weights is that of the rounded
- * ones; the output is rounded once.
+ * ones; the output is rounded once.  (Against 64 bits that is a relative error of 0.0019 to
+ * 0.0023 in bfloat16 and 0.00022 to 0.00026 in binary16, where the output's rounding
+ * alone is 0.0017 and 0.0002.)  Binary16 weights below 2^-32 of the largest are zero.
  *
  * Tables, lengths and reference counts are in DEVICE memory and are read when
  * a launch runs: a decode step recorded in a HIP graph is replayed for the
@@ -208,7 +210,8 @@ int lora_kv_free(const lora_kv_book_t* b, int32_t n, const int32_t* seqs, void* 
 
 /* Every sequence releases the pages in which no row still to come (position
  * len or later) sees a token with this window and these sinks; their table
- * entries become -1.  window >= 1. */
+ * entries become -1.  window >= 1.  Between a step and the next grow: once the lengths
+ * have grown, the step's own rows are no longer to come. */
 int lora_kv_trim(const lora_kv_book_t* b, int32_t window, int32_t n_sinks, void* stream);
 
 /* Pages src[i] to dst[i], every layer, all rows (HOST arrays of n; the dst

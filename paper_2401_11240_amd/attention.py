@@ -215,6 +215,7 @@ class Server:
         KV.lora_kv_free(self.book, seqs, self.stream)
 
     def trim(self, window: int, n_sinks: int = 0) -> None:
+        """Between a step and the next ``grow``, which moves the window's end."""
         KV.lora_kv_trim(self.book, window, n_sinks, self.stream)
 
     def compact(self) -> None:

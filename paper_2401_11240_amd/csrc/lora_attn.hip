@@ -43,8 +43,12 @@
 //   s_j = scale log2(e) q . K[j],  w_j = 2^(s_j - m),  O = sum w_j V[j],  S = sum w_j
 //
 // and when a maximum rises by more than kSlack powers of two, O and S are multiplied
-// by 2^(old - new). Smaller rises leave m as it is: weights to 2^kSlack lose nothing
-// in either type, and the product is needed in few steps.
+// by 2^(old - new). Smaller rises leave m as it is, so that the product is needed in few
+// steps. Weights are then up to 2^kSlack, and the heaviest, 1 with the exact maximum, is
+// rounded like the others. What rounding weights costs, as relative error against 64 bits (the
+// output's own rounding alone, with weights in float32: 0.0016-0.0017 in bf16, 0.00020 in f16): with the
+// exact maximum, in the decode kernel, 0.0019 and 0.00022; here 0.0020 (prompts of 256 to 1024 rows) to 0.0023
+// (16384 tokens) and 0.00023 to 0.00026.
 //
 //   Tile: 128 columns, 32 per wave; steps of 64 tokens. S^T = K Q^T and O^T = V^T P^T
 //   on v_mfma_f32_32x32x16: a lane has one column's scores, so maximum and sum need
@@ -67,13 +71,14 @@
 //   unless it is an infinity or a NaN. So a tile whose output is not finite is
 //   computed again by run_careful(), and so is one whose scores reach 2^21 powers of two.
 //
-//   Measured: 2048 rows behind 14336 tokens, 64/8 heads of width 128, bf16: 0.98-1.0
-//   ms, 1.03-1.05 PFLOP/s (library products reach 1.3 at their best), matrix cores
+//   Measured: 2048 rows behind 14336 tokens, 64/8 heads of width 128, bf16: 0.94-1.0
+//   ms, 1.03-1.09 PFLOP/s (library products reach 1.3 at their best), matrix cores
 //   busy for 55% of the cycles; four prompts of 2500 to 6000 rows under a window of
 //   1024, 24/8 heads of width 64, f16: 130 us, 0.6 PFLOP/s (twice the weights per
-//   product: vector instructions are issued in 70% of the cycles); sixteen prompts of
-//   256 to 1024 rows, 32/32 heads: 86 us, 3 TB/s (tiles of six steps on average,
-//   whose start and end count).
+//   product: vector instructions are issued in 72% of the cycles); sixteen prompts of
+//   256 to 1024 rows, 32/32 heads: 85 us, 3 TB/s (tiles of six steps on average,
+//   whose start and end count). Widths between 64, 128 and 256 do the work of the next of them: the first case takes
+//   620 us at 64, 853-888 at 72 to 96, 944 at 128, 1639-1722 at 136 to 192, 1828 at 256.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -1332,7 +1337,7 @@ __global__ void __launch_bounds__(256, prompt_per_cu(DP)) lora_attn_prompt_kerne
 // prompt, a few rows behind a long cache): tiles of 32 columns, whose tokens the four
 // waves divide and whose results meet in LDS.  One workgroup per compute unit, its
 // tokens 64 per wave in one buffer: bound by the latency of the loads, so what counts
-// is how few of them follow one another.  (203 rows of 32 heads: 9.0 us; in tiles of 128 columns 11.6 us.)
+// is how few of them follow one another.  (203 rows of 32 heads: 9.1 us; in tiles of 128 columns 11.9 us.)
 constexpr int kFewCols = 32;
 constexpr int few_floats(int dp) { return kFewCols * dp + 2 * kFewCols; }
 
@@ -1656,7 +1661,16 @@ int lora_attn_prompt(lora_attn_t h, const lora_kv_cache_t* c, int32_t layer, con
     const int dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
     const int32_t tokens = window > 0 ? (int32_t)std::min<int64_t>(s->max_len, (int64_t)window + n_sinks + n_rows) : s->max_len;
     hipStream_t st = (hipStream_t)stream;
-    // (tiles of few columns for head_dim to 128, whose tokens of four waves fit the LDS)
+    // Tiles of 32 columns (head_dim to 128, where the tokens of four waves fit the LDS) where they run in one round: one
+    // workgroup per compute unit, two of width 64; past 1024 tokens, which tiles of 128 columns share out as well, in
+    // half a round. Both sides, us, tiles of 128 / of 32, 32/32 heads, f16:
+    //   width 128, tokens:    the rows'   512        1024       2048       4096       16384
+    //     128 tiles, 128 rows  8.5/9.1    15.9/11.5  21.3/14.1  22.3/18.1  30.4/28.8  73.8/86.9
+    //     256 tiles, 256 rows  11.1/9.3   15.9/12.0  21.6/16.2  23.9/24.0  46.6/44.5  103/148
+    //     320 tiles, 300 rows  12.2/16.8  16.9/21.2  22.5/29.0  30.5/45.0  46.3/78.5  131/282
+    //   width 64, 512 tiles, 512 rows     12.6/10.0  17.1/14.0  23.0/22.4  33.5/38.2  106/145
+    // and 7.2/8.9 for 64 rows of 64 tokens. What counts is max_len, as the lengths are on the device: with 4096 and more
+    // there, 203 rows of 203 tokens take tiles of 128, most of whose parts are empty (25.6 us, 9.3 in tiles of 32).
     const int64_t few = tiles_of(kFewCols);
     if (dp <= 128 && tokens > kKeys && few <= (dp == 64 ? 2 : 1) * h->n_cu && (tokens <= 1024 || few <= h->n_cu / 2)) {
         pa.parts = prompt_parts(h->n_cu, few, tokens, 2 * 4 * kKeys);
