@@ -36,6 +36,8 @@
  * ones; the output is rounded once.  (Against 64 bits that is a relative error of 0.0019 to
  * 0.0023 in bfloat16 and 0.00022 to 0.00026 in binary16, where the output's rounding
  * alone is 0.0017 and 0.0002.)  Binary16 weights below 2^-32 of the largest are zero.
+ * The output's sums are divided at the end: bfloat16 values of 2^119 and more, or of 2^127
+ * over the number of tokens, may pass float32's range in them.
  *
  * Tables, lengths and reference counts are in DEVICE memory and are read when
  * a launch runs: a decode step recorded in a HIP graph is replayed for the
