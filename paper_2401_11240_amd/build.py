@@ -15,6 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "liblora.so")
 SOURCES = ["lora_api.hip", "lora_kernels.hip", "lora_base.hip", "lora_cold.hip", "lora_kv.hip", "lora_attn.hip",
+           "lora_mx.hip", "lora_mx_gemm.hip", "lora_sample.hip",
            "lora_sched.cpp", "lora_cpu.cpp"]
 ARCH = "gfx950"
 

@@ -1,0 +1,422 @@
+"""Rows in blocks, the norm and the product (include/lora_mx.h) against their definitions in
+64 bits (mx_reference.py): codes and scales bit for bit, the rest within tolerances that count
+roundings."""
+import numpy as np
+import pytest
+
+import mx_reference as R
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():   # collected on CPU-only hosts, never run there
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2401_11240_amd import lora as L  # noqa: E402
+from paper_2401_11240_amd import mx as MX  # noqa: E402
+
+DEV = torch.device("cuda:0")
+TYPE = {R.F16: torch.float16, R.BF16: torch.bfloat16, R.F32: torch.float32}
+HALF = {R.F16: 2.0 ** -11, R.BF16: 2.0 ** -8, R.F32: 2.0 ** -24}     # a rounding, relative
+FLOOR = {R.F16: 2.0 ** -25, R.BF16: 2.0 ** -134, R.F32: 2.0 ** -150}  # and below the normal range
+FORMATS = [R.E4M3, R.E2M1]
+NAMES = {R.F16: "f16", R.BF16: "bf16", R.F32: "f32"}
+FMT_NAMES = {R.E4M3: "e4m3", R.E2M1: "e2m1"}
+dtypes16 = pytest.mark.parametrize("dtype", [R.F16, R.BF16], ids=NAMES.get)
+dtypes = pytest.mark.parametrize("dtype", [R.F16, R.BF16, R.F32], ids=NAMES.get)
+formats = pytest.mark.parametrize("fmt", FORMATS, ids=FMT_NAMES.get)
+
+
+def stream():
+    return torch.cuda.current_stream(DEV)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def matrix(v, dtype, pad=0, fill=7.0):
+    """A device matrix with `pad` elements behind each row, and its view without them."""
+    whole = torch.full((v.shape[0], v.shape[1] + pad), fill, dtype=TYPE[dtype], device=DEV)
+    whole[:, :v.shape[1]] = torch.from_numpy(np.ascontiguousarray(v)).to(DEV).to(TYPE[dtype])
+    return whole, whole[:, :v.shape[1]]
+
+
+def rows_of(n, h, fmt, pad_codes=0, pad_scales=0, fill=0xAB):
+    codes = torch.full((n, MX.code_bytes(h, fmt) + pad_codes), fill, dtype=torch.uint8, device=DEV)
+    scales = torch.full((n, MX.scale_bytes(h) + pad_scales), fill, dtype=torch.uint8, device=DEV)
+    return MX.Rows(codes, scales, fmt, h)
+
+
+def stored(q):
+    return (q.codes.cpu().numpy(), q.scales.cpu().numpy())
+
+
+def hard_values(rng, rows, h, dtype):
+    """Normal rows with blocks of every kind among them: zeros, tiny, huge, ties, infinities, NaN."""
+    v = rng.standard_normal((rows, h)) * np.exp2(rng.integers(-6, 7, (rows, 1)))
+    for r in range(rows):
+        for b in range(R.blocks(h)):
+            s = slice(32 * b, min(h, 32 * b + 32))
+            n = s.stop - s.start
+            kind = rng.integers(0, 14)
+            if kind == 0:
+                v[r, s] = 0
+            elif kind == 1:
+                v[r, s] = rng.integers(-96, 97, n) / 16            # ties of both formats
+            elif kind == 2:
+                v[r, s] = rng.choice([6.0, -6.0, 7.0, 448.0, -464.0, 496.0, 5.0, 0.25, -0.25, -0.0], n)
+            elif kind == 3:
+                v[r, s.start + int(rng.integers(0, n))] = rng.choice([np.inf, -np.inf, np.nan])
+            elif kind == 4:
+                v[r, s] *= 2.0 ** (-20 if dtype == R.F16 else -125)  # subnormal
+            elif kind == 5:
+                v[r, s] = rng.choice([1, -1], n) * (60000.0 if dtype == R.F16 else 3.3e38) * rng.random(n)
+            elif kind == 6:
+                v[r, s] = rng.choice([1.0, -1.0, 2.0, 0.5], n) * np.exp2(rng.integers(-8, 8))
+    return v
+
+
+SHAPES = [(1, 8), (1, 4096), (3, 32), (5, 40), (7, 4104), (2, 13824), (203, 512), (1030, 64), (9, 24)]
+
+
+@dtypes
+@formats
+@pytest.mark.parametrize("rows,h", SHAPES)
+def test_quantize_is_the_definition_bit_for_bit(rows, h, fmt, dtype):
+    rng = np.random.default_rng([1, rows, h, fmt, dtype])
+    whole, x = matrix(hard_values(rng, rows, h, dtype), dtype, pad=16)
+    q = rows_of(rows, h, fmt, pad_codes=32, pad_scales=4)
+    MX.lora_mx_quantize(x, x.stride(0) if rows > 1 else h, dtype, q, stream())
+    codes, scales = stored(q)
+    want_c, want_s = R.quantize(f64(x), fmt)
+    n = R.blocks(h)
+    assert np.array_equal(scales[:, :n], want_s)
+    assert np.array_equal(codes[:, :want_c.shape[1]], want_c)
+    assert (codes[:, want_c.shape[1]:] == 0xAB).all() and (scales[:, n:] == 0xAB).all()   # nothing past the blocks
+
+
+@dtypes
+@formats
+def test_dequantize_every_code_and_scale(fmt, dtype):
+    # row s: scale s; every code in its blocks
+    n = 256 if fmt == R.E4M3 else 32
+    codes = np.tile(np.arange(256 if fmt == R.E4M3 else 16, dtype=np.uint8), (256, 2 if fmt == R.E2M1 else 1))
+    if fmt == R.E2M1:
+        codes = codes[:, 0::2] | (codes[:, 1::2] << 4)
+    q = rows_of(256, n, fmt)
+    q.codes.copy_(torch.from_numpy(codes))
+    q.scales.copy_(torch.from_numpy(np.repeat(np.arange(256, dtype=np.uint8)[:, None], q.scales.shape[1], 1)))
+    whole, y = matrix(np.zeros((256, n)), dtype, pad=8)
+    MX.lora_mx_dequantize(q, y, y.stride(0), dtype, stream())
+    want = torch.from_numpy(R.values(*stored(q), fmt, n)).to(DEV)
+    want = want.float().to(TYPE[dtype])      # exact in float32 (or past it)
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(y, nan=0.0, posinf=1e9, neginf=-1e9), torch.nan_to_num(want, nan=0.0, posinf=1e9, neginf=-1e9))
+    assert (whole[:, n:] == 7).all()
+
+
+@dtypes
+@formats
+@pytest.mark.parametrize("rows,h", [(1, 8), (5, 40), (3, 4104), (77, 1024)])
+def test_values_of_blocks_go_there_and_back(rows, h, fmt, dtype):
+    rng = np.random.default_rng([2, rows, h, fmt])
+    whole, x = matrix(rng.standard_normal((rows, h)), dtype)
+    q, again = rows_of(rows, h, fmt), rows_of(rows, h, fmt)
+    y = torch.empty_like(x)
+    MX.lora_mx_quantize(x, h, dtype, q, stream())
+    MX.lora_mx_dequantize(q, y, h, dtype, stream())
+    want = R.values(*R.quantize(f64(x), fmt), fmt, h)
+    assert np.array_equal(f64(y), want)
+    MX.lora_mx_quantize(y, h, dtype, again, stream())
+    MX.lora_mx_dequantize(again, x, h, dtype, stream())
+    assert torch.equal(x, y)
+
+
+# -- norm -------------------------------------------------------------------
+
+def check_norm_blocks(q, y64, rows, h, fmt, slack):
+    """The blocks of rows whose exact values are y64, computed in float32 with a relative error of
+    at most `slack` before the rounding to codes."""
+    codes, scales = stored(q)
+    n = R.blocks(h)
+    pad = np.zeros((rows, n * 32))
+    pad[:, :h] = y64
+    b = pad.reshape(rows, n, 32)
+    m = np.abs(b).max(2)
+    lo, hi = (np.where(m > 0, np.maximum(0, np.frexp(m * f)[1] - 1 - R.EMAX[fmt] + 127), 0)
+              for f in (1 - slack, 1 + slack))
+    s = scales[:, :n].astype(np.int64)
+    assert ((s == lo) | (s == hi)).all()
+    got = R.values(codes, scales, fmt, n * 32).reshape(rows, n, 32)
+    unit = np.ldexp(1.0, s - 127)[..., None]
+    a = np.abs(b) / unit
+    top, small = R.GRID[fmt][-1], (2.0 ** -10 if fmt == R.E4M3 else 0.25)
+    step = np.maximum(a * (2.0 ** -4 if fmt == R.E4M3 else 2.0 ** -2), small)      # half a step
+    bound = np.where(a > top, a - top + step, step) + a * slack
+    assert (np.abs(got - b) <= bound * unit).all()
+    assert (got.reshape(rows, -1)[:, h:] == 0).all()
+
+
+# float32 before the outputs' rounding, relative: the sum of squares of h terms in chains of at most
+# h / 64 + 64 roundings (a lane's chunks, then lanes and waves), halved by the root; the sum x + r counts
+# twice in a square and once itself; division, root, two products
+def norm_slack(h):
+    return (h / 64 + 64) * 2.0 ** -25 + 8 * 2.0 ** -24
+
+
+NORM_SHAPES = [(1, 8), (1, 64), (3, 512), (1, 4096), (5, 2056), (2, 5120), (3, 8200), (2, 13824), (2, 65536), (1030, 40),
+               (1030, 2048), (1025, 2056), (300, 1000)]
+
+
+@dtypes16
+@pytest.mark.parametrize("rows,h", NORM_SHAPES)
+def test_norm_against_64_bits(rows, h, dtype):
+    rng = np.random.default_rng([3, rows, h, dtype])
+    for fmt in FORMATS:
+        wx, x = matrix(rng.standard_normal((rows, h)) * np.where(rng.random(h) > 0.99, 30, 1), dtype, pad=8)
+        wr, r = matrix(rng.standard_normal((rows, h)) * 3, dtype, pad=24)
+        g = torch.from_numpy(1 + 0.3 * rng.standard_normal(h)).to(DEV).to(TYPE[dtype])
+        wt, total = matrix(np.zeros((rows, h)), dtype, pad=16)
+        wy, y = matrix(np.zeros((rows, h)), dtype, pad=8)
+        q = rows_of(rows, h, fmt, pad_codes=16, pad_scales=4)
+        MX.lora_norm(x, h + 8, r, h + 24, g, 1e-5, rows, h, dtype, total, h + 16, y, h + 8, q, stream())
+        s64, y64 = R.norm(f64(x), f64(r), f64(g), np.float64(np.float32(1e-5)))
+        # the sum of two values of 16 bits rounded twice: to float32 and to 16 bits
+        assert (np.abs(f64(total) - s64) <= np.abs(s64) * (HALF[dtype] + 2.0 ** -24) + FLOOR[dtype]).all()
+        # where x and r cancel, s is as wrong as its rounding to float32, not worse
+        err = np.abs(y64) * (norm_slack(h) + HALF[dtype]) + FLOOR[dtype]
+        assert (np.abs(f64(y) - y64) <= err).all()
+        check_norm_blocks(q, y64, rows, h, fmt, norm_slack(h))
+        for whole, n, fill in ((wt, h, 7), (wy, h, 7), (q.codes, MX.code_bytes(h, fmt), 0xAB), (q.scales, R.blocks(h), 0xAB)):
+            assert (whole[:, n:] == fill).all()
+
+
+@dtypes16
+@pytest.mark.parametrize("rows,h", [(1, 4096), (1027, 1032), (6, 8200)])
+def test_norm_forms(rows, h, dtype):
+    """Without residual, weight or sum, with one output alone, in place: the bits of the whole call."""
+    rng = np.random.default_rng([4, rows, h])
+    _, x = matrix(rng.standard_normal((rows, h)), dtype)
+    _, r = matrix(rng.standard_normal((rows, h)), dtype)
+    _, g = matrix(rng.standard_normal((1, h)), dtype)
+    ones, zeros = torch.ones_like(g), torch.zeros_like(x)
+
+    def call(x, r, g, total, y, q):
+        MX.lora_norm(x, h, r, h, g, 1e-6, rows, h, dtype, total, h, y, h, q, stream())
+
+    t0, y0, q0 = torch.empty_like(x), torch.empty_like(x), rows_of(rows, h, R.E4M3)
+    call(x, r, g, t0, y0, q0)
+    y1, q1 = torch.empty_like(x), rows_of(rows, h, R.E4M3)
+    call(x, r, g, None, y1, None)
+    assert torch.equal(y0, y1)
+    call(x, r, g, None, None, q1)
+    assert torch.equal(q0.codes, q1.codes) and torch.equal(q0.scales[:, :R.blocks(h)], q1.scales[:, :R.blocks(h)])
+    # without a residual or a weight: as with zeros and ones
+    ya, yb = torch.empty_like(x), torch.empty_like(x)
+    call(x, zeros, ones, None, ya, None)
+    call(x, None, None, None, yb, None)
+    assert torch.equal(ya, yb)
+    # in place
+    xs, rs = x.clone(), r.clone()
+    call(xs, rs, g, rs, xs, None)
+    assert torch.equal(rs, t0) and torch.equal(xs, y0)
+    xs, rs = x.clone(), r.clone()
+    call(xs, rs, g, xs, rs, q1)
+    assert torch.equal(xs, t0) and torch.equal(rs, y0) and torch.equal(q0.codes, q1.codes)
+
+
+@dtypes16
+def test_norm_of_zeros_infinities_and_nan(dtype):
+    rows, h = 5, 136
+    v = np.zeros((rows, h))
+    v[1] = 1
+    v[2, 5], v[3, 7] = np.inf, np.nan
+    v[4] = 1e-4 if dtype == R.F16 else 1e-30
+    _, x = matrix(v, dtype)
+    y, q = torch.empty_like(x), rows_of(rows, h, R.E4M3)
+    MX.lora_norm(x, h, None, 0 or h, None, 1e-5, rows, h, dtype, None, h, y, h, q, stream())
+    got = f64(y)
+    assert (got[0] == 0).all() and (stored(q)[0][0, :160] == 0).all() and (stored(q)[1][0, :5] == 0).all()
+    assert np.abs(got[1] - 1).max() <= 2 * HALF[dtype]
+    assert np.isnan(got[2, 5]) and (np.delete(got[2], 5) == 0).all()
+    assert stored(q)[1][2, 0] == 255 and (stored(q)[1][2, 1:5] == 0).all()
+    assert np.isnan(got[3]).all() and (stored(q)[1][3, :5] == 255).all()
+    want = R.norm(f64(x)[4:], None, None, np.float64(np.float32(1e-5)))[1]
+    assert (np.abs(got[4:] - want) <= np.abs(want) * (HALF[dtype] + norm_slack(h)) + FLOOR[dtype]).all()
+
+
+# -- product ----------------------------------------------------------------
+
+def random_rows(rng, n, h, fmt, spread=3, pad_codes=0, pad_scales=0):
+    """Random codes (no NaN) and scales around 1, zero codes past h, NaN in what lies between rows."""
+    q = rows_of(n, h, fmt, pad_codes, pad_scales, fill=0xFF)
+    if fmt == R.E4M3:
+        c = rng.integers(0, 127, (n, R.blocks(h) * 32)) | (rng.integers(0, 2, (n, R.blocks(h) * 32)) << 7)
+        c[:, h:] = 0
+    else:
+        c = rng.integers(0, 16, (n, R.blocks(h) * 32))
+        c[:, h:] = 0
+        c = c[:, 0::2] | (c[:, 1::2] << 4)
+    q.codes[:, :c.shape[1]] = torch.from_numpy(c.astype(np.uint8)).to(DEV)
+    s = rng.integers(127 - spread, 128 + spread, (n, R.blocks(h))).astype(np.uint8)
+    q.scales[:, :s.shape[1]] = torch.from_numpy(s).to(DEV)
+    return q
+
+
+def apply(x, w, dtype, pad=8):
+    whole, y = matrix(np.zeros((x.n_rows, w.n_rows)), dtype, pad)
+    n = MX.lora_mx_workspace_bytes(x, w)
+    ws = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    MX.lora_mx_apply(x, w, y, w.n_rows + pad, dtype, ws, n, stream())
+    assert (whole[:, w.n_rows:] == 7).all() and (ws[n:] == 0xFF).all()
+    return y
+
+
+def largest_of_8(q, v):
+    """The largest magnitude of every eight elements, none below the format's smallest normal one."""
+    n = R.blocks(q.h)
+    a = np.pad(np.abs(v), ((0, 0), (0, 32 * n - q.h))).reshape(len(v), n, 4, 8).max(3)
+    unit = np.ldexp(1.0, stored(q)[1][:, :n].astype(int) - 127)[..., None]
+    return np.maximum(a, unit * (2.0 ** -6 if q.fmt == R.E4M3 else 1)).reshape(len(v), -1)
+
+
+def check_product(x, w, y, dtype):
+    h = x.h
+    vx, vw = R.values(*stored(x), x.fmt, h), R.values(*stored(w), w.fmt, h)
+    want, size = vx @ vw.T, np.abs(vx) @ np.abs(vw).T
+    # products are exact in float32; at most h + 16 additions, each off by half a step of a partial sum
+    bound = (h + 16) * 2.0 ** -24 * size
+    if x.fmt == R.E4M3:
+        # of eight consecutive products the matrix instruction cuts off what is below 2^-13 of the power of two
+        # under the largest (8-bit codes below 2^-6 and 4-bit ones below 1 counting as those): less than
+        # that from each of the other seven
+        bound += 7 * 2.0 ** -13 * (largest_of_8(x, vx) @ largest_of_8(w, vw).T)
+    got = f64(y)
+    if dtype == R.F16:
+        big = np.abs(want) >= 65504
+        got, want, bound = np.where(big, 0, got), np.where(big, 0, want), np.where(big, 0, bound)
+    assert (np.abs(got - want) <= bound + HALF[dtype] * (np.abs(want) + bound) + FLOOR[dtype]).all()
+
+
+PRODUCTS = [(1, 8, 8), (1, 32, 16), (2, 40, 24), (3, 128, 8), (16, 136, 264), (17, 512, 40), (1, 4096, 4096), (1, 4104, 1032),
+            (8, 2048, 512), (33, 1024, 264), (64, 640, 1024), (65, 672, 128), (130, 264, 520), (257, 1056, 264), (300, 520, 776),
+            (512, 2048, 512)]
+
+
+@dtypes
+@formats
+@pytest.mark.parametrize("rows,h,h_out", PRODUCTS)
+def test_product_against_64_bits(rows, h, h_out, fmt, dtype):
+    rng = np.random.default_rng([5, rows, h, h_out, fmt, dtype])
+    spread = 1 if dtype == R.F16 and fmt == R.E4M3 else 3
+    x = random_rows(rng, rows, h, fmt, spread, pad_codes=32, pad_scales=4)
+    w = random_rows(rng, h_out, h, R.E2M1, spread, pad_codes=16, pad_scales=8)
+    check_product(x, w, apply(x, w, dtype), dtype)
+
+
+@formats
+def test_product_of_whole_numbers_is_exact(fmt):
+    """Codes of small whole numbers and scales of 1: every sum is exact, so any misplaced element shows."""
+    rng = np.random.default_rng([6, fmt])
+    for rows, h, h_out in ((1, 4096, 256), (20, 1032, 136), (64, 512, 512), (200, 2080, 1032), (520, 768, 520)):
+        x, w = random_rows(rng, rows, h, fmt), random_rows(rng, h_out, h, R.E2M1)
+        vx, vw = rng.integers(-2, 3, (rows, h)).astype(float), rng.integers(-4, 5, (h_out, h)).astype(float)
+        for q, v in ((x, vx), (w, vw)):
+            code = R.nearest_code(np.abs(v), q.fmt) | (np.signbit(v).astype(np.uint8) << (7 if q.fmt == R.E4M3 else 3))
+            code = np.pad(code, ((0, 0), (0, R.blocks(h) * 32 - h)))
+            code = code if q.fmt == R.E4M3 else code[:, 0::2] | (code[:, 1::2] << 4)
+            q.codes[:, :code.shape[1]] = torch.from_numpy(code).to(DEV)
+            q.scales[:, :R.blocks(h)] = 127
+        y = apply(x, w, R.F32)
+        vw = np.sign(vw) * R.GRID[R.E2M1][R.nearest_code(np.abs(vw), R.E2M1)]
+        assert np.array_equal(f64(y), vx @ vw.T)
+
+
+@formats
+@pytest.mark.parametrize("rows,h,h_out", [(1, 512, 64), (40, 1024, 128), (300, 1032, 264), (600, 512, 520)])
+def test_product_keeps_nan_to_its_row_and_column(rows, h, h_out, fmt):
+    rng = np.random.default_rng([7, rows])
+    x, w = random_rows(rng, rows, h, fmt), random_rows(rng, h_out, h, R.E2M1)
+    clean = apply(x, w, R.F32)
+    r, n = rows // 2, h_out - 3
+    x.scales[r, (h - 1) // 32] = 255
+    w.scales[n, 0] = 255
+    y = apply(x, w, R.F32)
+    assert torch.isnan(y[r]).all() and torch.isnan(y[:, n]).all()
+    keep = torch.ones_like(y, dtype=torch.bool)
+    keep[r], keep[:, n] = False, False
+    assert torch.equal(y[keep], clean[keep])
+
+
+def test_product_same_bits_every_time_and_recorded():
+    rng = np.random.default_rng(8)
+    for rows, h, h_out in ((1, 4096, 1024), (48, 2048, 1032), (600, 1024, 1544)):
+        x, w = random_rows(rng, rows, h, R.E4M3), random_rows(rng, h_out, h, R.E2M1)
+        want = apply(x, w, R.BF16)
+        n = MX.lora_mx_workspace_bytes(x, w)
+        ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+        y = torch.empty((rows, h_out), dtype=torch.bfloat16, device=DEV)
+        st = torch.cuda.Stream()
+        st.wait_stream(stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            MX.lora_mx_apply(x, w, y, h_out, R.BF16, ws, n, st)
+        for _ in range(3):
+            y.fill_(-1)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y, want)
+        # new rows in the same buffers
+        x.codes.copy_(random_rows(rng, rows, h, R.E4M3).codes)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, apply(x, w, R.BF16))
+
+
+def test_calls_on_a_stream_of_their_own_and_of_no_rows():
+    st = torch.cuda.Stream()
+    rng = np.random.default_rng(9)
+    h, rows = 1024, 64
+    _, x = matrix(rng.standard_normal((rows, h)), R.BF16)
+    q, w = rows_of(rows, h, R.E4M3), random_rows(rng, 256, h, R.E2M1)
+    y, z = torch.empty_like(x), torch.zeros((rows, 256), dtype=torch.bfloat16, device=DEV)
+    n = MX.lora_mx_workspace_bytes(q, w)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    MX.lora_norm(x, h, None, h, None, 1e-5, rows, h, R.BF16, None, h, y, h, q, st)
+    MX.lora_mx_apply(q, w, z, 256, R.BF16, ws, n, st)
+    st.synchronize()
+    check_product(q, w, z, R.BF16)
+    none = rows_of(0, h, R.E4M3)
+    MX.lora_norm(x, h, None, h, None, 1e-5, 0, h, R.BF16, None, h, y, h, none, st)
+    MX.lora_mx_quantize(x, h, R.BF16, none, st)
+    MX.lora_mx_dequantize(none, x, h, R.BF16, st)
+    MX.lora_mx_apply(none, w, z, 256, R.BF16, ws, n, st)
+    torch.cuda.synchronize()
+
+
+def test_calls_allocate_nothing():
+    h, rows = 512, 40
+    rng = np.random.default_rng(10)
+    _, x = matrix(rng.standard_normal((rows, h)), R.F16)
+    q, w, y = rows_of(rows, h, R.E4M3), random_rows(rng, 128, h, R.E2M1), torch.empty_like(x)
+    z = torch.empty((rows, 128), dtype=torch.float16, device=DEV)
+    n = MX.lora_mx_workspace_bytes(q, w)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+
+    def calls():
+        MX.lora_norm(x, h, None, h, None, 1e-5, rows, h, R.F16, None, h, y, h, q, stream())
+        MX.lora_mx_quantize(x, h, R.F16, q, stream())
+        MX.lora_mx_dequantize(q, y, h, R.F16, stream())
+        MX.lora_mx_apply(q, w, z, 128, R.F16, ws, n, stream())
+
+    calls()
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info(DEV)[0]
+    for _ in range(3):
+        calls()
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info(DEV)[0] == free
+    assert L.lora_abi_version() == 4
