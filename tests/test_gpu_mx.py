@@ -302,7 +302,7 @@ def check_product(x, w, y, dtype):
 
 PRODUCTS = [(1, 8, 8), (1, 32, 16), (2, 40, 24), (3, 128, 8), (16, 136, 264), (17, 512, 40), (1, 4096, 4096), (1, 4104, 1032),
             (8, 2048, 512), (33, 1024, 264), (64, 640, 1024), (65, 672, 128), (130, 264, 520), (257, 1056, 264), (300, 520, 776),
-            (512, 2048, 512)]
+            (512, 2048, 512), (24, 8192, 128), (2, 512, 8200), (20, 1000, 16392), (2056, 264, 4104)]
 
 
 @dtypes
