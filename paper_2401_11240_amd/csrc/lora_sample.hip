@@ -1,20 +1,21 @@
 // gfx950 kernels of the next token of every row (include/lora_sample.h).
 //
-// A logit's order is that of a 32-bit key.  The way to the token:
+// The way to the token:
 //
-//   1. the largest key of the row (weights are relative to it);
-//   2. a histogram over bins of 1/16 in (l_max - l) / T: logits, and weights where they are needed, per bin.  From
-//      its running sums come a first bin `lo` and a last bin `hi`: logits of bins below lo are kept by all
-//      filters, those above hi by none (what lies past 32 weighs nothing);
+//   1. the largest logit of the row (weights are relative to it);
+//   2. a histogram over bins of 1/16 in (l_max - l) / T: logits and weights per bin.  From its running sums come a
+//      first bin `lo` and a last bin `hi`: logits of bins below lo are kept by all filters, those above hi by none
+//      (what lies past 32 weighs nothing).  Where top_k is small, every thread's largest logit is enough: at
+//      least top_k logits are as large as the top_k-th of those, and not many more;
 //   3. the logits of bins lo .. hi in a list, in the order of their indices, and where lo is not 0 the
 //      weights below it, summed by segments of the row;
-//   4. in the list, which one workgroup holds, both thresholds exactly: the top_k-th largest logit and
-//      the last one of the top_p start, found digit by digit of the key from sums per digit, from the largest down;
-//      what equal logits share of a threshold goes to the lowest indices.  Then the segment, and
-//      in it the logit, where the running sum passes the target.
+//   4. one workgroup sorts the list, falling, and finds in its running sums the last logit that is kept; then, in the
+//      order of the indices again, the segment and in it the logit where the running sum passes the target.
 //
-// A list holds kList logits.  Rows that need a longer one (a top_k of thousands, thousands of equal logits at a
-// threshold) are done by one workgroup from memory, digit by digit over the whole row (slow_row).
+// Where there are rows enough a workgroup takes a row all the way, otherwise a row is divided into slices, a workgroup
+// each, with a launch for each step.  A list holds kList logits.  Rows that need a longer one (a top_k of thousands,
+// thousands of equal logits at a threshold) are done by one workgroup, thresholds digit by digit of an ordered key
+// (slow_row).
 //
 // Sums are whole numbers, so neither the order of atomic additions nor the division of a row over workgroups changes
 // a bit.
@@ -33,6 +34,9 @@ constexpr int kSampleThreads = 1024, kWaves = kSampleThreads / 64;
 constexpr int kDigits = 2048;
 constexpr int kBins = 512, kBinsPerNat = 16;   // the last bin: 31.9 and more, whose weights are zero
 constexpr int kList = 4096;                // logits of a list
+constexpr int kWaveList = kList / kWaves;  // of one wave's part of it
+constexpr int kRanked = 256;               // up to which a list is ranked by comparing all with all
+constexpr int kSmallK = 512;               // top_k up to which threads' largest logits bound it
 constexpr int kMaxSlices = 16;
 constexpr int kMaxVocab = 1 << 19;
 constexpr int kWeightBits = 43;            // sums of 2^19 weights stay below 2^62 (and exact)
@@ -49,6 +53,7 @@ struct SampleArgs {
     unsigned char* ws;
     int64_t ws_row;                        // bytes of a row's workspace
     int n_vocab, slices;
+    int seg;                               // logits of a wave's segment
 };
 
 template <int DT>
@@ -68,12 +73,16 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
 
+// Larger for larger logits, of equal ones for the lowest index.
+__device__ __forceinline__ uint64_t ranked(float l, int i) { return (uint64_t)key_of(l) << 32 | (0xffffffffu - (uint32_t)i); }
+__device__ __forceinline__ int index_of(uint64_t r) { return (int)(0xffffffffu - (uint32_t)r); }
+
 // The weight 2^43 exp((l - max) / T), rounded: exp(d / T) = 2^(k / 64) e^r, k = round(64 d / (T ln 2)),
 // |r| <= ln 2 / 128, 2^(k / 64) from a table of its 64 fractions and e^r by its series up to r^5 (the
 // next term is below 4e-17).  Adding 2^52 leaves the rounded whole number in the low bits.
-__device__ __forceinline__ uint64_t weight(uint32_t key, uint32_t top, double lmax, double rate, const double* frac) {
-    if (key == top) return 1ull << kWeightBits;
-    const double d = ((double)logit_of(key) - lmax) * rate;
+__device__ __forceinline__ uint64_t weight(float l, float top, double lmax, double rate, const double* frac) {
+    if (l == top) return 1ull << kWeightBits;
+    const double d = ((double)l - lmax) * rate;
     if (!(d > -64.0 * (kWeightBits + 2))) return 0;
     const double k = __builtin_rint(d);
     const double r = (d - k) * 0x1.62e42fefa39efp-7;          // ln 2 / 64
@@ -92,20 +101,22 @@ __device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return __shfl
 __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) { return __shfl_xor((unsigned long long)v, d, 64); }
 
 // What the filters leave open (step 2).
-struct Cut {
+struct Cut {                               // (read as whole words)
     uint64_t all;                          // sum of all weights (0 where it is not needed)
     uint64_t below;                        // of bins below lo
-    int mode, lo, hi, n;                   // kListed ..; the list's bins and logits
-    int k_cuts;                            // whether top_k leaves out a logit that weighs anything
+    int lo, hi;                            // the list's bins
+    int k_cuts;                            // whether top_k may leave out a logit that weighs anything
+    int slow;
 };
-enum { kListed, kSlow };
 
 struct Shared {
     unsigned long long hist[kDigits];      // per digit
     unsigned long long mass[kBins];
-    uint32_t count[kBins], before[kBins];  // before: of the slices in front
-    uint64_t list[kList];                  // key << 32 | index
+    uint32_t count[kBins];
+    uint64_t list[kList];                  // ranked() of logits
+    uint64_t weights[kRanked];
     uint64_t segs[kMaxSlices * kWaves];
+    uint32_t seg_n[kMaxSlices * kWaves];
     double frac[64];
     uint64_t part[kWaves], parts[kWaves], ties[kWaves];
     uint64_t above;
@@ -156,45 +167,49 @@ __device__ __forceinline__ void find_digit(uint64_t above, double limit, Shared&
 // A row's settings.
 struct Row {
     const void* z;
-    float T, p, m, lmax_f, bin_rate;
+    float T, p, m, lmax_f, bin_top, bin_rate;
     double lmax, rate, least, u;           // least: the weight that min_p asks for
-    int row, V, k;
-    uint32_t top;
-    int top_at;
+    int row, V, k, top_at;
     bool has_k, has_p, done;               // done: nothing to draw (nothing left, or the largest logit alone)
 
     __device__ __forceinline__ Row(const SampleArgs& a, int r, int dt) : row(r), V(a.n_vocab) {
         z = (const unsigned char*)a.logits + r * a.ld * (dt == LORA_F32 ? 4 : 2);
-        T = a.temperature ? a.temperature[r] : 1.f;
-        p = a.top_p ? a.top_p[r] : 1.f;
-        m = a.min_p ? a.min_p[r] : 0.f;
-        k = a.top_k ? a.top_k[r] : 0;
+        // (without branches: the loads are on their way together; for an array that is not there u is read)
         const float uf = a.u[r];
+        const float t = *((a.temperature ? a.temperature : a.u) + r), q = *((a.top_p ? a.top_p : a.u) + r),
+                    n = *((a.min_p ? a.min_p : a.u) + r);
+        const int i = *((a.top_k ? a.top_k : (const int32_t*)a.u) + r);
+        T = a.temperature ? t : 1.f;
+        p = a.top_p ? q : 1.f;
+        m = a.min_p ? n : 0.f;
+        k = a.top_k ? i : 0;
         u = uf >= 1.f ? 1.0 : uf > 0.f ? (double)uf : 0.0;
         has_k = k > 0 && k < V;
         has_p = p < 1.f;
         least = m > 0.f ? (double)(m < 1.f ? m : 1.f) * kOne : 0;
     }
-    // best: the largest key and, complemented, the lowest of its indices
     __device__ __forceinline__ void set_top(uint64_t best) {
-        top = (uint32_t)(best >> 32);
-        top_at = (int)(0xffffffffu - (uint32_t)best);
-        done = top <= kKeyNone || !(T > 0.f);
-        lmax_f = logit_of(top);
+        lmax_f = logit_of((uint32_t)(best >> 32));
+        top_at = index_of(best);
+        done = (uint32_t)(best >> 32) <= kKeyNone || !(T > 0.f);
         lmax = lmax_f;
         rate = 64 * 1.4426950408889634 / (double)T;
-        bin_rate = (float)kBinsPerNat / T;
+        // (finite and not 0, so that only the difference decides where it is infinite)
+        bin_rate = fminf(fmaxf((float)kBinsPerNat / T, 1e-37f), 1e38f);
+        bin_top = fminf(lmax_f, 3.402823466e38f);
     }
-    __device__ __forceinline__ uint64_t weight_of(uint32_t key, const double* frac) const { return weight(key, top, lmax, rate, frac); }
+    // top_k is small: the histogram is of threads' largest logits, and K's weights are summed in the list
+    __device__ __forceinline__ bool small_k() const { return has_k && k <= kSmallK; }
+    __device__ __forceinline__ uint64_t weight_of(float l, const double* frac) const { return weight(l, lmax_f, lmax, rate, frac); }
     __device__ __forceinline__ uint64_t kept(uint64_t w) const { return (double)w >= least ? w : 0; }
-    // (each step is monotone in the key; a difference that is not a number, of infinities, is the last bin)
-    __device__ __forceinline__ int bin_of(uint32_t key) const {
-        const float f = (lmax_f - logit_of(key)) * bin_rate;
-        return key == top ? 0 : f < (float)(kBins - 1) ? (int)f : kBins - 1;
+    // (each step is monotone; what is -infinity or weighs nothing is in the last bin)
+    __device__ __forceinline__ int bin_of(float l) const {
+        return (int)__builtin_amdgcn_fmed3f((bin_top - l) * bin_rate, 0.f, (float)(kBins - 1));
     }
     __device__ __forceinline__ void finish(const SampleArgs& a) const {
-        a.tokens[row] = top <= kKeyNone ? -1 : top_at;
-        if (a.probs) a.probs[row] = top <= kKeyNone ? 0.f : 1.f;
+        const bool none = !(lmax_f > -INFINITY);
+        a.tokens[row] = none ? -1 : top_at;
+        if (a.probs) a.probs[row] = none ? 0.f : 1.f;
     }
     __device__ __forceinline__ void choose(const SampleArgs& a, int i, uint64_t w, uint64_t total) const {
         a.tokens[row] = i;
@@ -206,94 +221,79 @@ struct Row {
     }
 };
 
-// Thresholds of `n` logits, key(i) of the i-th: the whole workgroup calls it.  BY_WEIGHT: the sums are of
-// weights, otherwise of ones, each with `above` in front of them; the lowest key whose larger ones sum to less than
-// `limit`, and what they sum to.  With weights, keys below floor_key do not count and those of floor_key weigh
-// floor_sum together.
-template <bool BY_WEIGHT, class Key>
-__device__ __forceinline__ uint32_t threshold(const Row& R, Shared& sh, int n, const Key& key_at, double limit, uint32_t floor_key,
-                                              uint64_t floor_sum, uint64_t& above) {
+// A threshold over the row in memory, by the whole workgroup: the lowest key whose larger ones sum to less than `limit`,
+// and in `above` what they sum to.  BY_WEIGHT: of weights, otherwise of ones.  With weights, keys below floor_key do not
+// count and those of floor_key weigh floor_sum together.
+template <int DT, bool BY_WEIGHT>
+__device__ __forceinline__ uint32_t threshold(const Row& R, Shared& sh, double limit, uint32_t floor_key, uint64_t floor_sum,
+                                              uint64_t& above) {
     uint32_t prefix = 0;
+    above = 0;
     for (int level = 0; level < 3; ++level) {
         const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
         __syncthreads();
         for (int i = threadIdx.x; i < kDigits; i += kSampleThreads) sh.hist[i] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kSampleThreads) {
-            const uint32_t key = key_at(i);
+        for (int i = threadIdx.x; i < R.V; i += kSampleThreads) {
+            const float l = logit<DT>(R.z, i);
+            const uint32_t key = key_of(l);
             if (key <= kKeyNone || (level > 0 && (key >> (shift + bits)) != prefix)) continue;
             uint64_t v = 1;
-            if (BY_WEIGHT) v = key > floor_key ? R.weight_of(key, sh.frac) : 0;
+            if (BY_WEIGHT) v = key > floor_key ? R.weight_of(l, sh.frac) : 0;
             if (v) atomicAdd(&sh.hist[(key >> shift) & ((1u << bits) - 1)], (unsigned long long)v);
         }
         if (BY_WEIGHT && threadIdx.x == 0 && floor_sum && (level == 0 || (floor_key >> (shift + bits)) == prefix))
             atomicAdd(&sh.hist[(floor_key >> shift) & ((1u << bits) - 1)], (unsigned long long)floor_sum);
         __syncthreads();
         find_digit(above, limit, sh);
-        if (sh.digit >= kDigits) return kKeyNone;      // (nothing that weighs)
         prefix = prefix << bits | sh.digit;
         above = sh.above;
     }
     return prefix;
 }
 
-// Both thresholds over `n` logits that hold everything the filters leave open: kept are keys above
-// tkey, and of those equal the first `share`.  all, below: of Cut, with `outside` logits' weights in
-// them that are not among the n (0 and 0 if the n are the whole row).
-template <class Key>
-__device__ __forceinline__ void thresholds(const Row& R, Shared& sh, int n, const Key& key_at, bool has_k, uint64_t all, uint64_t below,
-                                           uint32_t& tkey, uint32_t& share) {
-    tkey = kKeyNone;
-    share = 0;
-    if (has_k) {
-        uint64_t above = 0;
-        tkey = threshold<false>(R, sh, n, key_at, (double)R.k, 0, 0, above);
+// The row from memory by one workgroup, however it is.
+template <int DT>
+__device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shared& sh) {
+    const int t = threadIdx.x, l = t & 63, w = t >> 6, V = R.V;
+    auto weight_at = [&](uint32_t key) { return R.weight_of(logit_of(key), sh.frac); };
+    auto key_at = [&](int i) { return key_of(logit<DT>(R.z, i)); };
+    // kept are keys above tkey, and of those equal the first `share`
+    uint32_t tkey = kKeyNone, share = 0;
+    if (R.has_k) {
+        uint64_t above;
+        tkey = threshold<DT, false>(R, sh, (double)R.k, 0, 0, above);
         share = (uint32_t)(R.k - above);   // (at least 1; more than there are if few logits are left)
     }
-    if (!R.has_p) return;
-    if (!(R.p > 0.f)) {
-        tkey = R.top;
+    if (R.has_p && !(R.p > 0.f)) {
+        tkey = key_of(R.lmax_f);
         share = 1;
-        return;
-    }
-    uint64_t floor_sum = 0;
-    if (has_k || !all) {                   // the sum over K
-        uint64_t sum = 0, ties = 0;
-        for (int i = threadIdx.x; i < n; i += kSampleThreads) {
+    } else if (R.has_p) {
+        uint64_t sum = 0, ties = 0;        // over K
+        for (int i = t; i < V; i += kSampleThreads) {
             const uint32_t key = key_at(i);
             if (key <= kKeyNone) continue;
-            if (key > tkey) sum += R.weight_of(key, sh.frac);
+            if (key > tkey) sum += weight_at(key);
             else if (key == tkey) ++ties;
         }
         sum = block_sum(sum, sh);
         ties = block_sum(ties, sh);
-        if (tkey > kKeyNone) floor_sum = min((uint64_t)share, ties) * R.weight_of(tkey, sh.frac);
-        all = sum + floor_sum;
+        const uint64_t floor_sum = tkey > kKeyNone ? min((uint64_t)share, ties) * weight_at(tkey) : 0;
+        const double limit = (double)R.p * (double)(sum + floor_sum);
+        uint64_t above;
+        const uint32_t key = threshold<DT, true>(R, sh, limit, tkey, floor_sum, above);
+        const uint64_t each = weight_at(key);
+        // the first `few` of the equal ones begin below the limit
+        uint32_t few = 1, most = key == tkey ? share : (uint32_t)V;
+        while (few < most) {
+            const uint32_t mid = few + (most - few + 1) / 2;
+            if ((double)(above + (mid - 1) * each) < limit) few = mid;
+            else most = mid - 1;
+        }
+        tkey = key;
+        share = few;
     }
-    const double limit = (double)R.p * (double)all;
-    uint64_t above = below;
-    const uint32_t key = threshold<true>(R, sh, n, key_at, limit, tkey, floor_sum, above);
-    if (key <= kKeyNone) return;
-    const uint64_t each = R.weight_of(key, sh.frac);
-    // the first `few` of the equal ones begin below the limit
-    uint32_t few = 1, most = key == tkey ? share : (uint32_t)R.V;
-    while (few < most) {
-        const uint32_t mid = few + (most - few + 1) / 2;
-        if ((double)(above + (mid - 1) * each) < limit) few = mid;
-        else most = mid - 1;
-    }
-    tkey = key;
-    share = few;
-}
-
-// The row from memory by one workgroup, however it is.
-template <int DT>
-__device__ __noinline__ void slow_row(const SampleArgs& a, const Row& R, Shared& sh) {
-    const int t = threadIdx.x, l = t & 63, w = t >> 6, V = R.V;
-    auto key_at = [&](int i) { return key_of(logit<DT>(R.z, i)); };
-    uint32_t tkey, share;
-    thresholds(R, sh, V, key_at, R.has_k, 0, 0, tkey, share);
-    const uint64_t tie_weight = tkey > kKeyNone ? R.kept(R.weight_of(tkey, sh.frac)) : 0;
+    const uint64_t tie_weight = tkey > kKeyNone ? R.kept(weight_at(tkey)) : 0;
     // weights and ties of each wave's part of the row, in the order of the indices
     const int per = ((V + kWaves - 1) / kWaves + 63) & ~63;
     const int i0 = min(w * per, V), i1 = min(i0 + per, V);
@@ -301,7 +301,7 @@ __device__ __noinline__ void slow_row(const SampleArgs& a, const Row& R, Shared&
     for (int i = i0 + l; i < i1; i += 64) {
         const uint32_t key = key_at(i);
         if (key <= kKeyNone) continue;
-        if (key > tkey) sum += R.kept(R.weight_of(key, sh.frac));
+        if (key > tkey) sum += R.kept(weight_at(key));
         else if (key == tkey) ++ties;
     }
 #pragma unroll
@@ -332,7 +332,7 @@ __device__ __noinline__ void slow_row(const SampleArgs& a, const Row& R, Shared&
         const bool tie = key == tkey && key > kKeyNone;
         const uint64_t ballot = __ballot(tie);
         const uint64_t rank = ties_before + __popcll(ballot & ((1ull << l) - 1));
-        uint64_t v = key > kKeyNone && key > tkey ? R.kept(R.weight_of(key, sh.frac)) : tie && rank < share ? tie_weight : 0;
+        uint64_t v = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
         const uint64_t own = v;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -346,474 +346,803 @@ __device__ __noinline__ void slow_row(const SampleArgs& a, const Row& R, Shared&
     }
 }
 
-// A slice of a row in registers: wave w holds 64 EPT consecutive logits, lane l every 64th of them.
-template <int DT, int EPT>
-struct Slice {
-    uint32_t key[EPT];                     // 0 past the row
-    int i0;                                // this lane's first
-    __device__ __forceinline__ Slice(const Row& R, int slice) {
-        i0 = (slice * kWaves + (threadIdx.x >> 6)) * 64 * EPT + (threadIdx.x & 63);
-        float v[EPT];
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) v[e] = i0 + 64 * e < R.V ? logit<DT>(R.z, i0 + 64 * e) : 0.f;
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) key[e] = i0 + 64 * e < R.V ? key_of(v[e]) : 0u;
+// f(logits, index of the first) for the logits of segment `seg`, by one wave, whose lanes hold kVec consecutive ones each,
+// lane by lane and step by step in the order of the indices.  NaN is as -infinity, and so is what lies past the
+// segment.  (16 bytes a lane and load, at whatever alignment the row has; two loads on their way together.)
+template <int DT>
+struct Vec {
+    static constexpr int kVec = DT == LORA_F32 ? 4 : 8;
+    u32x4 w;
+    __device__ __forceinline__ void load(const Row& R, int i) {
+        __builtin_memcpy(&w, (const unsigned char*)R.z + (int64_t)i * (DT == LORA_F32 ? 4 : 2), 16);
     }
-    // Largest key and, complemented, the lowest of its indices: in every thread of the workgroup.
-    __device__ __forceinline__ uint64_t best(Shared& sh) const {
-        uint32_t k = 0;
-        int at = i0;
-#pragma unroll
-        for (int e = 0; e < EPT; ++e)
-            if (key[e] > k) {
-                k = key[e];
-                at = i0 + 64 * e;
-            }
-        uint64_t b = (uint64_t)k << 32 | (0xffffffffu - (uint32_t)at);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) b = max(b, shfl_xor64(b, d));
-        if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = b;
-        __syncthreads();
-        for (int i = 0; i < kWaves; ++i) b = max(b, sh.part[i]);
-        return b;
+    __device__ __forceinline__ float get(int e) const {
+        const uint32_t x = DT == LORA_F32 ? w[e & 3] : w[(e >> 1) & 3] >> (16 * (e & 1)) & 0xffffu;
+        const float l = DT == LORA_F32 ? __uint_as_float(x) : DT == LORA_F16 ? FmtF16::to_f32(x) : FmtBF16::to_f32(x);
+        return l == l ? l : -INFINITY;
     }
 };
+template <int DT, class F>
+__device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, int seg, const F& f) {
+    constexpr int kVec = Vec<DT>::kVec, kStep = 64 * kVec;
+    const int l = threadIdx.x & 63, end = min(R.V, (seg + 1) * a.seg);
+    int c = seg * a.seg;
+    float v[kVec];
+    for (; c + 2 * kStep <= end; c += 2 * kStep) {
+        Vec<DT> x[2];
+        x[0].load(R, c + kVec * l);
+        x[1].load(R, c + kStep + kVec * l);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] = x[q].get(e);
+            f(v, c + kStep * q + kVec * l);
+        }
+    }
+    for (; c < end; c += kStep) {
+        if (c + kStep <= end) {
+            Vec<DT> x;
+            x.load(R, c + kVec * l);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] = x.get(e);
+            f(v, c + kVec * l);
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            const int i = c + kVec * l + e;
+            v[e] = i < end ? logit<DT>(R.z, i) : -INFINITY;
+            v[e] = v[e] == v[e] ? v[e] : -INFINITY;
+        }
+        f(v, c + kVec * l);
+    }
+}
 
-// Whether the histogram has to hold weights: not where the list will be the top_k's.
-__device__ __forceinline__ bool needs_mass(const Row& R) { return !(R.has_k && R.k <= kList); }
+// ranked() of a slice's largest logit, in every thread of the workgroup; `most`: this thread's largest.
+template <int DT>
+__device__ __forceinline__ uint64_t best_of(const SampleArgs& a, const Row& R, Shared& sh, int slice, float& most) {
+    float top = -INFINITY;
+    int at = 0;
+    constexpr int kVec = Vec<DT>::kVec;
+    for_segment<DT>(a, R, slice * kWaves + (threadIdx.x >> 6), [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+            at = v[e] > top ? i + e : at;
+            top = fmaxf(top, v[e]);
+        }
+    });
+    most = top;
+    uint64_t b = ranked(top, at);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) b = max(b, shfl_xor64(b, d));
+    if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = b;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) b = max(b, sh.part[i]);
+    return b;
+}
 
-template <class S, int EPT>
-__device__ __forceinline__ void fill_bins(const Row& R, Shared& sh, const S& s) {
+__device__ __forceinline__ void clear_bins(Shared& sh) {
     for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
         sh.count[i] = 0;
         sh.mass[i] = 0;
     }
     __syncthreads();
-    const bool mass = needs_mass(R);
+}
+
+// A slice's histogram into sh.count and sh.mass, or that of the threads' largest.
+template <int DT>
+__device__ __forceinline__ void fill_bins(const SampleArgs& a, const Row& R, Shared& sh, int slice, float most) {
+    clear_bins(sh);
+    if (R.small_k()) {
+        const int b = R.bin_of(most);
+        if (b < kBins - 1) atomicAdd(&sh.count[b], 1u);
+    } else {
+        constexpr int kVec = Vec<DT>::kVec;
+        for_segment<DT>(a, R, slice * kWaves + (threadIdx.x >> 6), [&](const float (&v)[kVec], int) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-        const uint32_t key = s.key[e];
-        const int b = R.bin_of(key);
-        if (key > kKeyNone && b < kBins - 1) {
-            atomicAdd(&sh.count[b], 1u);
-            if (mass) atomicAdd(&sh.mass[b], (unsigned long long)R.weight_of(key, sh.frac));
-        }
+            for (int e = 0; e < kVec; ++e) {
+                const int b = R.bin_of(v[e]);
+                if (b < kBins - 1) {
+                    atomicAdd(&sh.count[b], 1u);
+                    atomicAdd(&sh.mass[b], (unsigned long long)R.weight_of(v[e], sh.frac));
+                }
+            }
+        });
     }
     __syncthreads();
 }
 
-// Step 2's decision from the row's histogram in sh.count and sh.mass; into sh.cut.
-__device__ __forceinline__ void decide(const Row& R, Shared& sh) {
-    const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    // running sums up to and with bin t
-    uint64_t c = t < kBins ? sh.count[t] : 0, m = t < kBins ? sh.mass[t] : 0;
-    const uint64_t own_m = m;
+// Running sums of the histogram in sh.count and sh.mass, by one wave, 8 bins a lane.
+struct BinSums {
+    static constexpr int kPer = kBins / 64;
+    uint64_t c[kPer], m[kPer], all;        // up to and with each bin; all: of the weights
+    __device__ __forceinline__ BinSums(const Shared& sh) {
+        const int l = threadIdx.x & 63;
+        uint64_t cs = 0, ms = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t oc = shfl_up64(c, d), om = shfl_up64(m, d);
-        if (l >= d) {
-            c += oc;
-            m += om;
+        for (int j = 0; j < kPer; ++j) {
+            cs += sh.count[kPer * l + j];
+            ms += sh.mass[kPer * l + j];
+            c[j] = cs;
+            m[j] = ms;
         }
-    }
-    if (l == 63) {
-        sh.parts[w] = m;
-        sh.ties[w] = c;
-    }
-    __syncthreads();
-    uint64_t all = 0;
-    for (int i = 0; i < kBins / 64; ++i) {
-        if (i < w) {
-            m += sh.parts[i];
-            c += sh.ties[i];
-        }
-        all += sh.parts[i];
-    }
-    // the bin of the top_k-th logit, and the weights up to it, which K's are not above
-    if (t == 0) {
-        sh.digit = kBins - 1;
-        sh.above = all;
-    }
-    __syncthreads();
-    const uint64_t before = c - (t < kBins ? sh.count[t] : 0);
-    if (R.has_k && t < kBins - 1 && before < (uint64_t)R.k && c >= (uint64_t)R.k) {
-        sh.digit = t;
-        sh.above = m;
-    }
-    __syncthreads();
-    const int kb = sh.digit;
-    const double limit = (double)R.p * (double)sh.above;
-    __syncthreads();
-    // the last bin that begins below top_p's limit (or, with K's sum smaller, later than that)
-    if (t == 0) sh.digit = R.has_p && !(R.p > 0.f) ? 0 : kBins - 2;
-    __syncthreads();
-    const bool by_p = R.has_p && R.p > 0.f && needs_mass(R);
-    if (by_p && t < kBins - 1 && own_m && (double)(m - own_m) < limit && (double)m >= limit) sh.digit = t;
-    __syncthreads();
-    const int pb = sh.digit;
-    __syncthreads();
-    // bins in which min_p may cut, with a bin to spare on either side for the roundings
-    int m0 = kBins - 1, m1 = kBins - 2;
-    if (R.least > 0) {
-        const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
-        // (weights of a few units are rounded by up to ln 2)
-        const int spare = R.least < 256 ? 12 : 1;
-        if (f < (float)(kBins - 2)) {
-            m0 = max((int)f - spare, 0);
-            m1 = (int)f + spare;
-        }
-    }
-    const bool k_cuts = R.has_k && kb < kBins - 1;
-    // (top_p needs the sum over K: all of it is in the list, if the bins do not have the row's)
-    const bool whole_k = R.has_p && R.p > 0.f && (k_cuts || !needs_mass(R));
-    const int hi = whole_k ? min(kb, kBins - 2) : min(min(kb, pb), min(m1, kBins - 2));
-    if (t == hi) {                         // all of it fits the list, or else ...
-        sh.digit = c <= (uint64_t)kList;
-        sh.cut.n = (int)min(c, (uint64_t)1 << 30);
-    }
-    __syncthreads();
-    int lo = 0;
-    if (!sh.digit) lo = !R.has_p && R.least <= 0 ? kBins - 1 : min(pb < kBins - 2 || by_p ? pb : kBins - 1, m0);
-    if (t == 0) {
-        sh.cut.lo = lo;
-        sh.cut.hi = hi;
-        sh.cut.all = needs_mass(R) && !k_cuts ? all : 0;
-        sh.cut.below = 0;
-        sh.cut.mode = kListed;
-        sh.cut.k_cuts = k_cuts;
-        if (!sh.digit && (lo == 0 || k_cuts || !needs_mass(R))) sh.cut.mode = kSlow;
-        if (lo > hi) sh.cut.n = 0;
-    }
-    __syncthreads();
-    if (lo > 0) {                          // ... its last bins, with what is kept below them
-        if (t == lo - 1) {
-            sh.cut.below = m;
-            sh.above = c;
-        }
-        __syncthreads();
-        if (t == hi && lo <= hi) {
-            const uint64_t n = c - sh.above;
-            sh.cut.n = (int)min(n, (uint64_t)1 << 30);
-            if (n > (uint64_t)kList) sh.cut.mode = kSlow;
-        }
-    }
-    __syncthreads();
-}
-
-// Step 3 for a slice: its logits of the cut's bins into `list`, from entry `first` on in the order of their indices,
-// and, where lo is not 0, each wave's sum of weights below it into segs.
-template <class S, int EPT>
-__device__ __forceinline__ void collect(const Row& R, Shared& sh, const S& s, int first, uint64_t* list, uint64_t* segs) {
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int lo = sh.cut.lo, hi = sh.cut.hi;
-    int mine = 0;
-    uint64_t sum = 0;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-        const uint32_t key = s.key[e];
-        const int b = key > kKeyNone ? R.bin_of(key) : kBins;
-        mine += __popcll(__ballot(b >= lo && b <= hi));
-        if (lo > 0 && b < lo && b <= hi) sum += R.weight_of(key, sh.frac);
-    }
-    if (lo > 0) {
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += shfl_xor64(sum, d);
-        if (l == 0) segs[w] = sum;
-    }
-    __syncthreads();
-    if (l == 0) sh.ties[w] = mine;
-    __syncthreads();
-    for (int i = 0; i < w; ++i) first += (int)sh.ties[i];
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-        const uint32_t key = s.key[e];
-        const int b = key > kKeyNone ? R.bin_of(key) : kBins;
-        const bool in = b >= lo && b <= hi;
-        const uint64_t ballot = __ballot(in);
-        const int at = first + __popcll(ballot & ((1ull << l) - 1));
-        if (in && at < kList) list[at] = (uint64_t)key << 32 | (uint32_t)(s.i0 + 64 * e);
-        first += __popcll(ballot);
-    }
-    __syncthreads();
-}
-
-// Step 4, from the list and the segments' sums in sh.  EPT: the slices' (a segment is a wave's share of a slice).
-template <int DT, int EPT>
-__device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& sh) {
-    const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    constexpr int kSeg = 64 * EPT, kEach = kList / kSampleThreads;
-    const Cut cut = sh.cut;
-    const int n = cut.n;
-    auto key_at = [&](int i) { return (uint32_t)(sh.list[i] >> 32); };
-    uint32_t tkey = kKeyNone, share = 0;
-    if (n > 0) thresholds(R, sh, n, key_at, cut.k_cuts, cut.all, cut.below, tkey, share);
-    const uint64_t tie_weight = tkey > kKeyNone ? R.kept(R.weight_of(tkey, sh.frac)) : 0;
-    // thread t: entries kEach t ..; ranks of equal ones, then kept weights, then their running sums
-    uint64_t v[kEach], ties = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int i = kEach * t + j;
-        const uint32_t key = i < n ? key_at(i) : 0;
-        v[j] = key > tkey && key > kKeyNone ? R.kept(R.weight_of(key, sh.frac)) : 0;
-        ties += key == tkey && key > kKeyNone;
-    }
-    auto scan = [&](uint64_t x) {          // exclusive, over the workgroup; sh.above: the sum
-        uint64_t s = x;
+        uint64_t co = cs, mo = ms;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t o = shfl_up64(s, d);
-            if (l >= d) s += o;
+            const uint64_t oc = shfl_up64(co, d), om = shfl_up64(mo, d);
+            if (l >= d) {
+                co += oc;
+                mo += om;
+            }
         }
-        __syncthreads();
-        if (l == 63) sh.parts[w] = s;
-        __syncthreads();
-        uint64_t before = 0, all = 0;
-        for (int i = 0; i < kWaves; ++i) {
-            if (i < w) before += sh.parts[i];
-            all += sh.parts[i];
+        all = __shfl((unsigned long long)mo, 63, 64);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            c[j] += co - cs;
+            m[j] += mo - ms;
         }
-        if (t == 0) sh.above = all;
-        return before + s - x;
+    }
+    // the first bin whose running sum satisfies `ok`, or the last bin; a running sum at a bin (0 in front of the first)
+    template <class Ok>
+    __device__ __forceinline__ int first(const Ok& ok) const {
+        int b = kBins;
+#pragma unroll
+        for (int j = kPer - 1; j >= 0; --j) b = ok(j) ? kPer * (int)(threadIdx.x & 63) + j : b;
+        const uint64_t has = __ballot(b < kBins);
+        return has ? min(__shfl(b, __ffsll((unsigned long long)has) - 1, 64), kBins - 1) : kBins - 1;
+    }
+    static __device__ __forceinline__ uint64_t at(const uint64_t (&x)[kPer], int b) {
+        uint64_t v = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v = j == (b & (kPer - 1)) ? x[j] : v;
+        v = __shfl((unsigned long long)v, max(b, 0) / kPer, 64);
+        return b < 0 ? 0 : v;
+    }
+};
+
+// Step 2's decision from the row's histogram in sh.count and sh.mass, into sh.cut.
+__device__ __forceinline__ void decide(const Row& R, Shared& sh) {
+    const int l = threadIdx.x;
+    if (l < 64) {
+        const BinSums S(sh);
+        const uint64_t all = S.all;
+        // the bin of the top_k-th logit, and the weights up to it, which K's are not above
+        const bool small = R.small_k();
+        const int kb = R.has_k ? S.first([&](int j) { return S.c[j] >= (uint64_t)R.k; }) : kBins - 1;
+        const bool k_cuts = R.has_k && (small || kb < kBins - 1);
+        // the last bin that begins below top_p's limit (or, with K's sum smaller, later than that)
+        int pb = kBins - 2;
+        const bool by_p = R.has_p && R.p > 0.f && !small;
+        if (R.has_p && !(R.p > 0.f)) pb = 0;
+        if (by_p) {
+            const double limit = (double)R.p * (double)(kb < kBins - 1 ? S.at(S.m, kb) : all);
+            pb = min(pb, S.first([&](int j) { return (double)S.m[j] >= limit; }));
+        }
+        // bins in which min_p may cut, with some to spare on either side for the roundings (weights of a few units
+        // are rounded by up to ln 2)
+        int m0 = kBins - 1, m1 = kBins - 2;
+        if (R.least > 0) {
+            const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
+            const int spare = R.least < 256 ? 12 : 1;
+            if (f < (float)(kBins - 2)) {
+                m0 = max((int)f - spare, 0);
+                m1 = min((int)f + spare, kBins - 2);
+            }
+        }
+        // (top_p needs the sum over K: all of it is in the list, if the bins do not have the row's)
+        const bool whole_k = R.has_p && R.p > 0.f && k_cuts;
+        const int hi = whole_k ? min(kb, kBins - 2) : min(min(min(kb, pb), m1), kBins - 2);
+        int lo = 0, slow = 0;
+        const uint64_t upto = S.at(S.c, hi);
+        if (!small && upto > (uint64_t)kList) {        // not all of it fits the list: its last bins
+            lo = !R.has_p && R.least <= 0 ? kBins - 1 : min(by_p ? pb : kBins - 1, m0);
+            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kList);
+        }
+        const uint64_t below = S.at(S.m, lo - 1);
+        if (l == 0) {
+            sh.cut.all = k_cuts ? 0 : all;
+            sh.cut.below = below;
+            sh.cut.lo = lo;
+            sh.cut.hi = hi;
+            sh.cut.k_cuts = k_cuts;
+            sh.cut.slow = slow;
+        }
+    }
+    __syncthreads();
+}
+
+// Step 3 for segment `seg`, by one wave: its logits of the cut's bins into `list` of kWaveList, in the order of their
+// indices, and, where lo is not 0, the sum of weights below it into `sum`.  Their number, which may be more than the room.
+template <int DT>
+__device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, Shared& sh, int seg, uint64_t* list, uint64_t& sum) {
+    const int l = threadIdx.x & 63;
+    const int lo = sh.cut.lo, hi = sh.cut.hi;
+    constexpr int kVec = Vec<DT>::kVec;
+    uint32_t n = 0;
+    // a lane's logits of one step that are in, bit by bit; lanes in order
+    auto add = [&](uint32_t in, const float (&v)[kVec], int i) __attribute__((always_inline)) {
+        if (!__any(in)) return;
+        uint32_t at = __popc(in);
+        const uint32_t own = at;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(at, d, 64);
+            if (l >= d) at += o;
+        }
+        const uint32_t all = __shfl(at, 63, 64);
+        at += n - own;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+            if (in >> e & 1) {
+                if (at < (uint32_t)kWaveList) list[at] = ranked(v[e], i + e);
+                ++at;
+            }
+        n += all;
     };
-    uint64_t rank = scan(ties);
-    uint64_t mine = 0;
+    sum = 0;
+    if (lo == 0) {
+        for_segment<DT>(a, R, seg, [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) in |= (uint32_t)(R.bin_of(v[e]) <= hi) << e;
+            add(in, v, i);
+        });
+    } else {
+        for_segment<DT>(a, R, seg, [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const int b = R.bin_of(v[e]);
+                in |= (uint32_t)(b >= lo && b <= hi) << e;
+                if (b < min(lo, hi + 1)) sum += R.weight_of(v[e], sh.frac);
+            }
+            add(in, v, i);
+        });
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum += shfl_xor64(sum, d);
+    }
+    return n;
+}
+
+// Running sum in front of x over the workgroup's threads; `all` gets the whole.
+__device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) {
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint64_t s = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t o = shfl_up64(s, d);
+        if (l >= d) s += o;
+    }
+    __syncthreads();
+    if (l == 63) sh.parts[w] = s;
+    __syncthreads();
+    uint64_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < w) before += sh.parts[i];
+        all += sh.parts[i];
+    }
+    return before + s - x;
+}
+
+// What top_k and top_p keep of a list (n logits, 4 entries a thread in `mine`): ranked() of the last.  A finer histogram
+// of the list's bins leads to the one bin in which each of the two ends, whose few logits are compared with one another.
+// False if they are not few.
+__device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut, const uint64_t (&mine)[kList / kSampleThreads], int n,
+                                       uint64_t& last) {
+    constexpr int kEach = kList / kSampleThreads;
+    const int t = threadIdx.x;
+    const float scale = (float)kBins / (float)(cut.hi + 1 - cut.lo);
+    int fine[kEach];
+    clear_bins(sh);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        const int i = kEach * t + j;
-        const uint32_t key = i < n ? key_at(i) : 0;
-        if (key == tkey && key > kKeyNone) {
-            if (rank < share) v[j] = tie_weight;
-            ++rank;
+        const float l = logit_of((uint32_t)(mine[j] >> 32));
+        const float f = __builtin_amdgcn_fmed3f((R.bin_top - l) * R.bin_rate, 0.f, (float)(kBins - 1));
+        fine[j] = mine[j] ? (int)__builtin_amdgcn_fmed3f((f - (float)cut.lo) * scale, 0.f, (float)(kBins - 1)) : kBins;
+        if (fine[j] < kBins) {
+            atomicAdd(&sh.count[fine[j]], 1u);
+            if (R.has_p) atomicAdd(&sh.mass[fine[j]], (unsigned long long)R.weight_of(l, sh.frac));
         }
-        mine += v[j];
     }
-    if (cut.lo == 0) {
-        const uint64_t at = scan(mine);
+    __syncthreads();
+    // a bin's logits, one a thread, with their rank in it and the weights in front of them in it; false if too many
+    uint64_t own = 0, weight = 0, before = 0;
+    int rank = 0;
+    auto compare = [&](int bin) __attribute__((always_inline)) {
         __syncthreads();
-        const uint64_t total = sh.above, target = R.target(total);
-        uint64_t run = at;
+        const int m = (int)sh.count[bin];
+        if (m > kRanked) return false;
+        if (t == 0) sh.digit = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (fine[j] == bin) sh.hist[atomicAdd(&sh.digit, 1u)] = mine[j];
+        __syncthreads();
+        own = t < m ? sh.hist[t] : 0;
+        weight = t < m ? R.weight_of(logit_of((uint32_t)(own >> 32)), sh.frac) : 0;
+        if (t < m) sh.weights[t] = weight;
+        __syncthreads();
+        rank = 0;
+        before = 0;
+        if (t < m)
+            for (int i = 0; i < m; ++i) {
+                const bool larger = sh.hist[i] > own;
+                rank += larger;
+                before += larger ? sh.weights[i] : 0;
+            }
+        return true;
+    };
+    last = 0;
+    uint64_t sum = cut.all;
+    if (cut.k_cuts) {
+        if (t < 64) {
+            const BinSums S(sh);
+            const int b = S.first([&](int j) { return S.c[j] >= (uint64_t)R.k; });
+            const uint64_t c0 = S.at(S.c, b - 1), m0 = S.at(S.m, b - 1);
+            if (t == 0) {
+                sh.part[0] = (uint64_t)b;
+                sh.part[1] = c0;
+                sh.part[2] = m0;
+                sh.part[3] = S.all;
+            }
+        }
+        __syncthreads();
+        const int b = (int)sh.part[0], c0 = (int)sh.part[1];
+        sum = sh.part[3];
+        if (n > R.k) {
+            const uint64_t m0 = sh.part[2];
+            if (!compare(b)) return false;
+            if (own && c0 + rank == R.k - 1) {
+                sh.part[4] = own;
+                sh.part[5] = m0 + before + weight;
+            }
+            __syncthreads();
+            last = sh.part[4];
+            sum = sh.part[5];
+        }
+        __syncthreads();
+    }
+    if (R.has_p) {
+        const double limit = (double)R.p * (double)sum;
+        if (t < 64) {
+            const BinSums S(sh);
+            const int b = R.p > 0.f ? S.first([&](int j) { return (double)(cut.below + S.m[j]) >= limit; }) : S.first([&](int j) { return S.c[j] > 0; });
+            const uint64_t m0 = S.at(S.m, b - 1);
+            if (t == 0) {
+                sh.part[0] = (uint64_t)b;
+                sh.part[1] = cut.below + m0;
+                sh.part[2] = 0;
+            }
+        }
+        __syncthreads();
+        const int b = (int)sh.part[0];
+        const uint64_t m0 = sh.part[1];
+        if (!compare(b)) return false;
+        // the last of the bin that begins below the limit (none: what lies in front of the bin is all)
+        const bool in = own && ((double)(m0 + before) < limit || (!(R.p > 0.f) && rank == 0));
+        if (t == 0) sh.digit = 0;
+        __syncthreads();
+        if (in) atomicMax(&sh.digit, (uint32_t)rank + 1);
+        __syncthreads();
+        if (in && (uint32_t)rank + 1 == sh.digit) sh.part[2] = own;
+        __syncthreads();
+        // (the weights of all bins may stay below the limit: then nothing is cut here)
+        if (sh.digit > 0) last = max(last, sh.part[2]);
+        __syncthreads();
+    }
+    return true;
+}
+
+// sh.list[0 .. n) falling, by compare and exchange in the order of a bitonic sort; from n on zeros.  Exchanges over
+// less than 128 stay inside a wave's 128 entries, whose reads and writes are in order.
+__device__ __forceinline__ void sort_list(Shared& sh, int n) {
+    int size = 256;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sh.list[i] = 0;
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            if (j >= 128 || k == 2) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int t = threadIdx.x; t < size / 2; t += kSampleThreads) {
+                const int i = 2 * t - (t & (j - 1)), o = i + j;
+                const uint64_t x = sh.list[i], y = sh.list[o];
+                if ((x < y) == ((i & k) == 0)) {
+                    sh.list[i] = y;
+                    sh.list[o] = x;
+                }
+            }
+            if (j == 128) __syncthreads();
+        }
+    __syncthreads();
+}
+
+// Step 4, from the list (n logits in the order of their indices) and the segments' sums in sh.
+template <int DT>
+__device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& sh, int n) {
+    const int t = threadIdx.x;
+    constexpr int kEach = kList / kSampleThreads;
+    const Cut cut = sh.cut;
+    auto weight_at = [&](uint64_t r) __attribute__((always_inline)) { return R.weight_of(logit_of((uint32_t)(r >> 32)), sh.frac); };
+    const bool cuts = n > 0 && (cut.k_cuts || R.has_p);
+    const int most = cut.k_cuts ? min(R.k, n) : n;
+    uint64_t all, last = 0;                // last: the last that top_k and top_p keep
+    if (n <= kRanked) {
+        // one entry a thread: its rank and the weights in front of it, from a comparison with every other
+        const uint64_t mine = t < n ? sh.list[t] : 0;
+        uint64_t w = t < n ? weight_at(mine) : 0;
+        if (cuts) {
+            if (t < kRanked) sh.weights[t] = w;
+            __syncthreads();
+            uint64_t before = 0;
+            int rank = 0;
+            if (t < n)
+                for (int i = 0; i < n; ++i) {
+                    const bool larger = sh.list[i] > mine;
+                    rank += larger;
+                    before += larger ? sh.weights[i] : 0;
+                }
+            bool in = t < n && rank < most;
+            if (R.has_p) {
+                all = cut.all;
+                if (cut.k_cuts) scan(sh, in ? w : 0, all);
+                in &= rank == 0 || (double)(cut.below + before) < (double)R.p * (double)all;
+            }
+            if (!in) w = 0;
+            if (cut.lo > 0) {              // (the segment's search asks for the last)
+                if (t == 0) sh.digit = 0;
+                __syncthreads();
+                if (in) atomicMax(&sh.digit, (uint32_t)rank);
+                __syncthreads();
+                if (in && (uint32_t)rank == sh.digit) sh.part[1] = mine;
+                __syncthreads();
+                last = sh.part[1];
+            }
+        }
+        w = R.kept(w);
+        if (cut.lo == 0) {
+            const uint64_t run = scan(sh, w, all), target = R.target(all);
+            if (w && run <= target && target < run + w) R.choose(a, index_of(mine), w, all);
+            return;
+        }
+        if (w) atomicAdd((unsigned long long*)&sh.segs[index_of(mine) / a.seg], (unsigned long long)w);
+    } else {
+        // thread t: entries kEach t ..
+        uint64_t mine[kEach], v[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) mine[j] = kEach * t + j < n ? sh.list[kEach * t + j] : 0;
+        if (cuts && !select(R, sh, cut, mine, n, last)) {
+            __syncthreads();
+            sort_list(sh, n);
+            int kept = most;
+            if (R.has_p) {
+                uint64_t sum = 0;
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    v[j] = kEach * t + j < kept ? weight_at(sh.list[kEach * t + j]) : 0;
+                    sum += v[j];
+                }
+                uint64_t before = cut.below + scan(sh, sum, all);
+                const double limit = (double)R.p * (double)(cut.k_cuts ? all : cut.all);
+                int end = 1;               // (running sums: the kept ones are the first)
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    if (kEach * t + j < kept && (double)before < limit) end = kEach * t + j + 1;
+                    before += v[j];
+                }
+                if (t == 0) sh.digit = 1;
+                __syncthreads();
+                if (end > 1) atomicMax(&sh.digit, (uint32_t)end);
+                __syncthreads();
+                kept = (int)sh.digit;
+            }
+            last = sh.list[kept - 1];
+        }
+        uint64_t sum = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            if (v[j] && run <= target && target < run + v[j]) R.choose(a, (int)(uint32_t)sh.list[kEach * t + j], v[j], total);
-            run += v[j];
+            v[j] = mine[j] && mine[j] >= last ? R.kept(weight_at(mine[j])) : 0;
+            sum += v[j];
         }
-        return;
-    }
-    // the list's kept weights into their segments; the first of equal ones that is not kept, in tie_end
-    const int n_segs = a.slices * kWaves;
-    if (t == 0) sh.digit = 0x7fffffff;
-    __syncthreads();
+        if (cut.lo == 0) {
+            uint64_t run = scan(sh, sum, all);
+            const uint64_t target = R.target(all);
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int i = kEach * t + j;
-        if (v[j]) atomicAdd((unsigned long long*)&sh.segs[(uint32_t)sh.list[i] / kSeg], (unsigned long long)v[j]);
-        else if (i < n && key_at(i) == tkey) atomicMin(&sh.digit, (uint32_t)sh.list[i]);
+            for (int j = 0; j < kEach; ++j) {
+                if (v[j] && run <= target && target < run + v[j]) R.choose(a, index_of(mine[j]), v[j], all);
+                run += v[j];
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (v[j]) atomicAdd((unsigned long long*)&sh.segs[index_of(mine[j]) / a.seg], (unsigned long long)v[j]);
     }
+    // the segment in which the target lies, and the segment again
     __syncthreads();
-    const uint32_t tie_end = sh.digit;
-    const uint64_t s = t < n_segs ? sh.segs[t] : 0;
-    const uint64_t at = scan(s);
-    __syncthreads();
-    const uint64_t total = sh.above, target = R.target(total);
+    const uint64_t s = t < a.slices * kWaves ? sh.segs[t] : 0;
+    const uint64_t at = scan(sh, s, all);
+    const uint64_t total = all, target = R.target(total);
     if (s && at <= target && target < at + s) {
         sh.digit = t;
         sh.part[0] = at;
     }
     __syncthreads();
-    // the segment again
-    const int seg = sh.digit;
-    const uint64_t begin = sh.part[0];
-    constexpr int kOf = EPT >= 16 ? EPT / 16 : 1;      // consecutive logits of a thread
-    uint64_t x[kOf], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kOf; ++j) {
-        const int o = t * kOf + j, i = seg * kSeg + o;
-        const uint32_t key = o < kSeg && i < R.V ? key_of(logit<DT>(R.z, i)) : 0;
-        const int b = key > kKeyNone ? R.bin_of(key) : kBins;
-        x[j] = 0;
-        if (b <= cut.hi && key >= tkey && (key != tkey || (uint32_t)i < tie_end)) x[j] = R.weight_of(key, sh.frac);
-        if (b >= cut.lo) x[j] = R.kept(x[j]);
-        sum += x[j];
-    }
-    uint64_t run = begin + scan(sum);
-#pragma unroll
-    for (int j = 0; j < kOf; ++j) {
-        if (x[j] && run <= target && target < run + x[j]) R.choose(a, seg * kSeg + t * kOf + j, x[j], total);
-        run += x[j];
+    const int first = (int)sh.digit * a.seg, end = min(R.V, first + a.seg);
+    uint64_t run = sh.part[0];
+    for (int i = first + t; i - t < end && run <= target; i += kSampleThreads) {
+        float l = i < end ? logit<DT>(R.z, i) : -INFINITY;
+        l = l == l ? l : -INFINITY;
+        const int b = R.bin_of(l);
+        uint64_t x = 0;
+        if (b < min(cut.lo, cut.hi + 1)) x = R.weight_of(l, sh.frac);
+        else if (b <= cut.hi && ranked(l, i) >= last) x = R.kept(R.weight_of(l, sh.frac));
+        const uint64_t mine = run + scan(sh, x, all);
+        if (x && mine <= target && target < mine + x) R.choose(a, i, x, total);
+        run += all;
     }
 }
 
-__device__ __forceinline__ void fill_fractions(Shared& sh) {
-    if (threadIdx.x < 64) sh.frac[threadIdx.x] = exp2(threadIdx.x / 64.0);
-}
-
-// Rows that one workgroup holds.
-template <int DT, int EPT>
-__global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleArgs a) {
-    __shared__ Shared sh;
-    Row R(a, blockIdx.x, DT);
-    using S = Slice<DT, EPT>;
-    S s(R, 0);
-    fill_fractions(sh);
-    R.set_top(s.best(sh));
-    if (R.done) {
-        if (threadIdx.x == 0) R.finish(a);
-        return;
+// The waves' lists, from[kWaveList g ..] for wave g, one behind the other in sh.list (which `from` may be itself, of one
+// slice); numbers in sh.seg_n[0 .. segs).  False if one did not fit or all do not.
+__device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int segs, int& n) {
+    const int t = threadIdx.x, l = t & 63, w = t >> 6;
+    const uint32_t mine = t < segs ? sh.seg_n[t] : 0;
+    uint64_t all;
+    const uint32_t first = (uint32_t)scan(sh, mine, all);
+    n = (int)all;
+    if (__syncthreads_or(mine > (uint32_t)kWaveList) || all > (uint64_t)kList) return false;
+    if (t < segs) sh.segs[t] = first;      // (for a moment)
+    __syncthreads();
+    if (segs == kWaves) {
+        constexpr int kPer = kWaveList / 64;
+        uint64_t r[kPer];
+        const int of = (int)sh.seg_n[w], to = (int)sh.segs[w];
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) r[q] = l + 64 * q < of ? from[w * kWaveList + l + 64 * q] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+            if (l + 64 * q < of) sh.list[to + l + 64 * q] = r[q];
+    } else {
+        for (int g = w; g < segs; g += kWaves) {
+            const int of = (int)sh.seg_n[g], to = (int)sh.segs[g];
+            for (int i = l; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
+        }
     }
     __syncthreads();
-    fill_bins<S, EPT>(R, sh, s);
-    decide(R, sh);
-    if (sh.cut.mode == kSlow) {
-        slow_row<DT>(a, R, sh);
-        return;
-    }
-    collect<S, EPT>(R, sh, s, 0, sh.list, sh.segs);
-    pick<DT, EPT>(a, R, sh);
+    return true;
 }
 
-// Rows of several slices, a launch for each of the four steps.  A row's workspace: every slice's best, counts and
-// weights per bin, segment sums; the list; the cut.
+// 2^(i / 64), as sqrt 2 e^x with x = (i - 32) / 64 ln 2 and the series of e^x up to x^13 (the next term is below 5e-18).  (From
+// a table in memory, which no launch has in a cache, they would take 4 us.)
+__device__ __forceinline__ void fill_fractions(Shared& sh) {
+    const int i = threadIdx.x;
+    if (i >= 64) return;
+    const double x = (i - 32) * 0x1.62e42fefa39efp-7;
+    double p = 1.0 / 6227020800.0;
+#pragma unroll
+    for (int n = 12; n >= 0; --n) {
+        constexpr double kInverse[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
+                                         1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
+        p = fma(p, x, kInverse[n]);
+    }
+    sh.frac[i] = p * 0x1.6a09e667f3bcdp+0;
+}
+
+// A row's workspace: the cut; every slice's best; of every wave the number of listed logits, its sum and its list; of
+// every slice counts and weights per bin, or its threads' largest logits.
 struct RowSpace {
-    uint64_t *best, *mass, *segs, *list;
-    uint32_t* count;
     Cut* cut;
-    __host__ __device__ RowSpace(unsigned char* p, int slices) {
+    uint64_t *best, *mass, *segs, *list;
+    uint32_t *count, *n;
+    float* most;
+    static constexpr int64_t kHead = 64 + 8 * kMaxSlices;
+    static constexpr int64_t kSlice = kWaves * (8 + 4 + 8 * kWaveList) + 12 * kBins + 4 * kSampleThreads;
+    __device__ RowSpace(unsigned char* p, int slices) {
         cut = (Cut*)p;
         best = (uint64_t*)(p + 64);
         mass = best + kMaxSlices;
         segs = mass + (int64_t)slices * kBins;
         list = segs + (int64_t)slices * kWaves;
-        count = (uint32_t*)(list + kList);
+        n = (uint32_t*)(list + (int64_t)slices * kWaves * kWaveList);
+        count = n + (int64_t)slices * kWaves;
+        most = (float*)(count + (int64_t)slices * kBins);
     }
-    static int64_t bytes(int slices) { return 64 + 8ll * (kMaxSlices + slices * (kBins + kWaves) + kList) + 4ll * slices * kBins; }
+    static int64_t bytes(int slices) { return kHead + slices * kSlice; }
 };
+static_assert((sizeof(Cut) & (sizeof(Cut) - 1)) == 0 && sizeof(Cut) <= 64 && RowSpace::kHead % 16 == 0 && RowSpace::kSlice % 16 == 0, "rows' workspaces");
 
-__device__ __forceinline__ uint64_t row_best(const RowSpace& ws, int slices) {
-    uint64_t b = 0;
-    for (int i = 0; i < slices; ++i) b = max(b, ws.best[i]);
+template <int DT>
+__global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int t = threadIdx.x, w = t >> 6;
+    Row R(a, blockIdx.x, DT);
+    fill_fractions(sh);
+    float most;
+    R.set_top(best_of<DT>(a, R, sh, 0, most));
+    if (R.done) {
+        if (t == 0) R.finish(a);
+        return;
+    }
+    fill_bins<DT>(a, R, sh, 0, most);
+    decide(R, sh);
+    int n = 0;
+    bool fits = !sh.cut.slow;
+    if (fits) {
+        uint64_t sum;
+        const uint32_t of = collect<DT>(a, R, sh, w, sh.list + w * kWaveList, sum);
+        if ((t & 63) == 0) sh.seg_n[w] = of;
+        __syncthreads();
+        fits = gather(sh, sh.list, kWaves, n);
+        __syncthreads();
+        if ((t & 63) == 0) sh.segs[w] = sum;
+        __syncthreads();
+    }
+    if (!fits) {
+        slow_row<DT>(a, R, sh);
+        return;
+    }
+    pick<DT>(a, R, sh, n);
+}
+
+// The row's best of its slices', which lanes hold.
+__device__ __forceinline__ uint64_t largest(uint64_t b, int slices) {
+    if ((threadIdx.x & (kMaxSlices - 1)) >= (unsigned)slices) b = 0;
+#pragma unroll
+    for (int d = kMaxSlices / 2; d >= 1; d >>= 1) b = max(b, shfl_xor64(b, d));
     return b;
 }
 
-template <int DT, int EPT>
+template <int DT>
 __global__ void __launch_bounds__(kSampleThreads) lora_sample_best_kernel(SampleArgs a) {
     __shared__ Shared sh;
+    const RowSpace ws(a.ws + blockIdx.y * a.ws_row, a.slices);
     const Row R(a, blockIdx.y, DT);
-    const Slice<DT, EPT> s(R, blockIdx.x);
-    const uint64_t b = s.best(sh);
-    if (threadIdx.x == 0) RowSpace(a.ws + blockIdx.y * a.ws_row, a.slices).best[blockIdx.x] = b;
+    float most;
+    const uint64_t b = best_of<DT>(a, R, sh, blockIdx.x, most);
+    if (threadIdx.x == 0) ws.best[blockIdx.x] = b;
+    if (R.small_k()) ws.most[blockIdx.x * kSampleThreads + threadIdx.x] = most;
 }
 
-template <int DT, int EPT>
+template <int DT>
 __global__ void __launch_bounds__(kSampleThreads) lora_sample_bins_kernel(SampleArgs a) {
     __shared__ Shared sh;
     const RowSpace ws(a.ws + blockIdx.y * a.ws_row, a.slices);
+    const uint64_t bests = ws.best[threadIdx.x & (kMaxSlices - 1)];
     Row R(a, blockIdx.y, DT);
-    using S = Slice<DT, EPT>;
-    const S s(R, blockIdx.x);
+    if (R.small_k()) return;
     fill_fractions(sh);
-    R.set_top(row_best(ws, a.slices));
+    R.set_top(largest(bests, a.slices));
     if (R.done) return;
-    __syncthreads();
-    fill_bins<S, EPT>(R, sh, s);
+    fill_bins<DT>(a, R, sh, blockIdx.x, 0.f);
     for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
         ws.count[blockIdx.x * kBins + i] = sh.count[i];
         ws.mass[blockIdx.x * kBins + i] = sh.mass[i];
     }
 }
 
-template <int DT, int EPT>
+template <int DT>
 __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(SampleArgs a) {
     __shared__ Shared sh;
+    const int t = threadIdx.x, seg = blockIdx.x * kWaves + (t >> 6);
     const RowSpace ws(a.ws + blockIdx.y * a.ws_row, a.slices);
+    const uint64_t bests = ws.best[t & (kMaxSlices - 1)];
     Row R(a, blockIdx.y, DT);
-    using S = Slice<DT, EPT>;
-    const S s(R, blockIdx.x);
     fill_fractions(sh);
-    R.set_top(row_best(ws, a.slices));
-    if (R.done) return;
-    for (int i = threadIdx.x; i < kBins; i += kSampleThreads) {
-        uint32_t c = 0, before = 0;
-        uint64_t m = 0;
-        for (int j = 0; j < a.slices; ++j) {
-            if (j == (int)blockIdx.x) before = c;
-            c += ws.count[j * kBins + i];
-            m += ws.mass[j * kBins + i];
+    // (slices past the last are read as the last again and not counted: all loads at once)
+    if (R.small_k()) {
+        float most[kMaxSlices];
+#pragma unroll
+        for (int j = 0; j < kMaxSlices; ++j) most[j] = ws.most[min(j, a.slices - 1) * kSampleThreads + t];
+        R.set_top(largest(bests, a.slices));
+        if (R.done) return;
+        clear_bins(sh);
+#pragma unroll
+        for (int j = 0; j < kMaxSlices; ++j) {
+            const int b = R.bin_of(most[j]);
+            if (j < a.slices && b < kBins - 1) atomicAdd(&sh.count[b], 1u);
         }
-        sh.count[i] = c;
-        sh.before[i] = before;
-        sh.mass[i] = m;
+    } else {
+        uint32_t c[kMaxSlices];
+        uint64_t m[kMaxSlices];
+#pragma unroll
+        for (int j = 0; j < kMaxSlices; ++j) {
+            c[j] = ws.count[min(j, a.slices - 1) * kBins + (t & (kBins - 1))];
+            m[j] = ws.mass[min(j, a.slices - 1) * kBins + (t & (kBins - 1))];
+        }
+        R.set_top(largest(bests, a.slices));
+        if (R.done) return;
+#pragma unroll
+        for (int j = 1; j < kMaxSlices; ++j) {
+            c[0] += j < a.slices ? c[j] : 0;
+            m[0] += j < a.slices ? m[j] : 0;
+        }
+        if (t < kBins) {
+            sh.count[t] = c[0];
+            sh.mass[t] = m[0];
+        }
     }
     __syncthreads();
     decide(R, sh);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ws.cut = sh.cut;
-    if (sh.cut.mode == kSlow) return;
-    const int t = threadIdx.x;
-    const int first = (int)block_sum(t < kBins && t >= sh.cut.lo && t <= sh.cut.hi ? sh.before[t] : 0, sh);
-    collect<S, EPT>(R, sh, s, first, ws.list, ws.segs + blockIdx.x * kWaves);
-}
-
-template <int DT, int EPT>
-__global__ void __launch_bounds__(kSampleThreads) lora_sample_pick_kernel(SampleArgs a) {
-    __shared__ Shared sh;
-    const RowSpace ws(a.ws + blockIdx.x * a.ws_row, a.slices);
-    Row R(a, blockIdx.x, DT);
-    fill_fractions(sh);
-    R.set_top(row_best(ws, a.slices));
-    if (R.done) {
-        if (threadIdx.x == 0) R.finish(a);
-        return;
+    if (blockIdx.x == 0 && t == 0) *ws.cut = sh.cut;
+    if (sh.cut.slow) return;
+    uint64_t sum;
+    const uint32_t n = collect<DT>(a, R, sh, seg, ws.list + (int64_t)seg * kWaveList, sum);
+    if ((t & 63) == 0) {
+        ws.n[seg] = n;
+        ws.segs[seg] = sum;
     }
-    if (threadIdx.x == 0) sh.cut = *ws.cut;
-    __syncthreads();
-    if (sh.cut.mode == kSlow) {
-        slow_row<DT>(a, R, sh);
-        return;
-    }
-    for (int i = threadIdx.x; i < sh.cut.n; i += kSampleThreads) sh.list[i] = ws.list[i];
-    if (sh.cut.lo > 0)
-        for (int i = threadIdx.x; i < a.slices * kWaves; i += kSampleThreads) sh.segs[i] = ws.segs[i];
-    __syncthreads();
-    pick<DT, EPT>(a, R, sh);
-}
-
-// Slices of a row: kSampleThreads * ept logits each.
-struct SamplePlan {
-    int ept, slices;
-};
-
-SamplePlan plan_sample(int n_rows, int n_vocab) {
-    SamplePlan p{};
-    for (p.ept = 8; p.ept < 32; p.ept *= 2) {
-        const int64_t per = (int64_t)kSampleThreads * p.ept;
-        p.slices = (int)((n_vocab + per - 1) / per);
-        if (p.slices <= kMaxSlices && (int64_t)n_rows * p.slices <= 512) break;
-    }
-    p.slices = (int)((n_vocab + (int64_t)kSampleThreads * p.ept - 1) / ((int64_t)kSampleThreads * p.ept));
-#ifdef MX_PROBE
-    if (const char* e = getenv("SA_EPT")) { p.ept = atoi(e); p.slices = (int)((n_vocab + (int64_t)kSampleThreads * p.ept - 1) / ((int64_t)kSampleThreads * p.ept)); }
-#endif
-    return p;
-}
-
-template <int DT, int EPT>
-void launch_sample(const SampleArgs& a, int n_rows, hipStream_t st) {
-    const dim3 block(kSampleThreads);
-    if (a.slices == 1) {
-        hipLaunchKernelGGL((lora_sample_row_kernel<DT, EPT>), dim3(n_rows), block, 0, st, a);
-        return;
-    }
-    const dim3 grid(a.slices, n_rows);
-    hipLaunchKernelGGL((lora_sample_best_kernel<DT, EPT>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((lora_sample_bins_kernel<DT, EPT>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((lora_sample_list_kernel<DT, EPT>), grid, block, 0, st, a);
-    hipLaunchKernelGGL((lora_sample_pick_kernel<DT, EPT>), dim3(n_rows), block, 0, st, a);
 }
 
 template <int DT>
-void launch_sample(const SampleArgs& a, int ept, int n_rows, hipStream_t st) {
-    if (ept == 8) launch_sample<DT, 8>(a, n_rows, st);
-    else if (ept == 16) launch_sample<DT, 16>(a, n_rows, st);
-    else launch_sample<DT, 32>(a, n_rows, st);
+__global__ void __launch_bounds__(kSampleThreads) lora_sample_pick_kernel(SampleArgs a) {
+    __shared__ Shared sh;
+    const int t = threadIdx.x, segs = a.slices * kWaves;
+    const RowSpace ws(a.ws + blockIdx.x * a.ws_row, a.slices);
+    // (all that is read from the workspace, at once)
+    constexpr int kCutWords = sizeof(Cut) / 8;
+    const uint64_t cut = ((const uint64_t*)ws.cut)[t & (kCutWords - 1)];
+    const uint32_t listed = ws.n[min(t, segs - 1)];
+    const uint64_t sum = ws.segs[min(t, segs - 1)];
+    const uint64_t bests = ws.best[t & (kMaxSlices - 1)];
+    Row R(a, blockIdx.x, DT);
+    fill_fractions(sh);
+    if (t < kCutWords) ((uint64_t*)&sh.cut)[t] = cut;
+    if (t < segs) sh.seg_n[t] = listed;
+    const uint64_t best = largest(bests, a.slices);
+    R.set_top(best);
+    if (R.done) {
+        if (t == 0) R.finish(a);
+        return;
+    }
+    __syncthreads();
+    int n = 0;
+    bool fits = !sh.cut.slow;
+    if (fits) {
+        fits = gather(sh, ws.list, segs, n);
+        __syncthreads();
+        if (t < segs) sh.segs[t] = sum;
+        __syncthreads();
+    }
+    if (!fits) {
+        slow_row<DT>(a, R, sh);
+        return;
+    }
+    pick<DT>(a, R, sh, n);
+}
+
+struct SamplePlan {
+    int slices, seg;
+};
+
+// A slice has 4096 logits at least, and all slices together are no more than two workgroups a compute unit.
+SamplePlan plan_sample(int n_rows, int n_vocab) {
+    int64_t slices = std::min<int64_t>({kMaxSlices, (n_vocab + 4095) / 4096, 512 / std::max(1, n_rows)});
+#ifdef MX_PROBE
+    if (const char* e = getenv("SA_S")) slices = std::min(atoi(e), kMaxSlices);
+#endif
+    slices = std::max<int64_t>(1, slices);
+    SamplePlan p;
+    p.seg = (int)((n_vocab + slices * kWaves * 256 - 1) / (slices * kWaves * 256)) * 256;
+    p.slices = (n_vocab + p.seg * kWaves - 1) / (p.seg * kWaves);
+    return p;
+}
+
+template <int DT>
+void launch_sample(const SampleArgs& a, int n_rows, hipStream_t st) {
+    const dim3 block(kSampleThreads);
+    if (a.slices == 1) {
+        hipLaunchKernelGGL(lora_sample_row_kernel<DT>, dim3(n_rows), block, 0, st, a);
+        return;
+    }
+    const dim3 grid(a.slices, n_rows);
+    hipLaunchKernelGGL(lora_sample_best_kernel<DT>, grid, block, 0, st, a);
+    hipLaunchKernelGGL(lora_sample_bins_kernel<DT>, grid, block, 0, st, a);
+    hipLaunchKernelGGL(lora_sample_list_kernel<DT>, grid, block, 0, st, a);
+    hipLaunchKernelGGL(lora_sample_pick_kernel<DT>, dim3(n_rows), block, 0, st, a);
 }
 
 }  // namespace
@@ -877,10 +1206,11 @@ int lora_sample(const void* logits, int64_t ld, int32_t dtype, int32_t n_rows, i
     a.ws = (unsigned char*)ws;
     const SamplePlan p = plan_sample(n_rows, n_vocab);
     a.slices = p.slices;
+    a.seg = p.seg;
     a.ws_row = RowSpace::bytes(p.slices);
-    if (dtype == LORA_F16) launch_sample<LORA_F16>(a, p.ept, n_rows, st);
-    else if (dtype == LORA_BF16) launch_sample<LORA_BF16>(a, p.ept, n_rows, st);
-    else launch_sample<LORA_F32>(a, p.ept, n_rows, st);
+    if (dtype == LORA_F16) launch_sample<LORA_F16>(a, n_rows, st);
+    else if (dtype == LORA_BF16) launch_sample<LORA_BF16>(a, n_rows, st);
+    else launch_sample<LORA_F32>(a, n_rows, st);
     return check_launch("lora_sample");
 }
 
