@@ -134,11 +134,13 @@ struct NormArgs {
     int64_t ldx, ldr, ldt, ldy;            // bytes
     int64_t ld_codes, ld_scales;
     int n_rows, chunks, format;            // chunks of a row
-    float eps, h;
+    float eps;
+    double inv_h;
 };
 
 // A row by TPR threads (a wave, or a workgroup of 256 or 1024), CH chunks each, which stay in
-// registers between the sum of squares and the outputs: x and the residual are read once.
+// registers between the sum of squares and the outputs: x and the residual are read once.  HBM bounds many rows (8437 x
+// 5120 with all outputs 73-76 us, 5.1-5.3 TB/s), the launch and the chain of load, sum and barrier a few (3.5 us).
 // Every output of a row is written after all of its inputs are read where that is asked
 // for: y depends on the whole row, and total[i] only on x[i] and residual[i].
 template <class Fmt, int CH, int TPR>
@@ -161,7 +163,8 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
             if (a.weight) g[i].load(a.weight + 16 * c);
         }
     }
-    float s[CH][8], sum = 0.f;
+    float s[CH][8];
+    double sum = 0.;                       // (the squares of a chunk in float32, chunks in binary64)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         float r[8];
@@ -179,14 +182,19 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
     if constexpr (TPR > 64) {
-        __shared__ float part[TPR / 64];
+        __shared__ double part[TPR / 64];
         if ((t & 63) == 0) part[t >> 6] = sum;
         __syncthreads();
-        sum = 0.f;
+        sum = 0.;
 #pragma unroll
         for (int i = 0; i < TPR / 64; ++i) sum += part[i];
     }
-    const float rstd = 1.f / sqrtf(sum / a.h + a.eps);
+    // 1 / sqrt in binary64 (an estimate and one Newton step), as a float32 and what it leaves: with them the product
+    // s rstd w below is off by little more than its last rounding, and 8-bit codes hardly ever by that
+    const double ms = sum * a.inv_h + (double)a.eps;
+    double r64 = __builtin_amdgcn_rsq(ms);
+    r64 = ms < INFINITY ? r64 * (1.5 - 0.5 * ms * r64 * r64) : r64;    // (0 for infinity, NaN for NaN)
+    const float rstd = (float)r64, rest = (float)(r64 - (double)rstd);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * TPR + t;
@@ -194,8 +202,9 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
         g[i].get(w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s[i][e] *= rstd;
-            if (a.weight) s[i][e] *= w[e];
+            const float hi = s[i][e] * rstd, lo = fmaf(s[i][e], rest, fmaf(s[i][e], rstd, -hi));
+            const float by = a.weight ? w[e] : 1.f;    // (one form: hi + lo could be contracted to other bits)
+            s[i][e] = fmaf(hi, by, lo * by);
         }
         if (a.y && c < a.chunks) Chunk<Fmt>::put(a.y + row * a.ldy + 16 * c, s[i]);
         if (a.codes && i * TPR < a.chunks) {
@@ -223,7 +232,10 @@ void launch_norm_tpr(const NormArgs& a, int tpr, hipStream_t st) {
 
 template <class Fmt>
 void launch_norm(const NormArgs& a, hipStream_t st) {
-    int tpr = a.n_rows >= 1024 && a.chunks <= 256 ? 64 : a.chunks <= 1024 ? 256 : 1024;
+    // many short rows: a wave each, without barriers; few long ones: as many threads as there are chunks, for the sake of
+    // the loads on their way (us with 256 against 1024 threads, h 8192: 64 rows 5.3 against 4.4, 256 rows 6.6 against
+    // 6.2; past that the barriers of 16 waves cost more: 1024 rows 14.3 against 15.3, 8437 x 5120 75.2 against 80.5)
+    const int tpr = a.n_rows >= 1024 && a.chunks <= 256 ? 64 : a.chunks <= (a.n_rows <= 512 ? 512 : 1024) ? 256 : 1024;
     const int ch = (a.chunks + tpr - 1) / tpr;
     if (ch <= 1) launch_norm_tpr<Fmt, 1>(a, tpr, st);
     else if (ch <= 2) launch_norm_tpr<Fmt, 2>(a, tpr, st);
@@ -417,7 +429,7 @@ int lora_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, con
     a.chunks = h / 8;
     a.format = q ? q->format : 0;
     a.eps = eps;
-    a.h = (float)h;
+    a.inv_h = 1.0 / h;
     if (dtype == LORA_F16) launch_norm<FmtF16>(a, st);
     else launch_norm<FmtBF16>(a, st);
     return check_launch("lora_norm");

@@ -19,6 +19,11 @@
 //
 // Sums are whole numbers, so neither the order of atomic additions nor the division of a row over workgroups changes
 // a bit.
+//
+// What bounds it: a few rows, the four launches (3 to 9 us each in a trace, most of it the way of the first loads and of
+// barriers of sixteen waves); many rows with top_p and no small top_k, the weights of all logits, about 25 binary64
+// operations each, twice where the list does not hold all that is kept, and their atomic additions; many rows with
+// a small top_k, two readings of the logits (256 x 50257 in float32: 29 us, 51 MB).
 #include <cmath>
 
 #include <algorithm>
@@ -79,11 +84,12 @@ __device__ __forceinline__ int index_of(uint64_t r) { return (int)(0xffffffffu -
 
 // The weight 2^43 exp((l - max) / T), rounded: exp(d / T) = 2^(k / 64) e^r, k = round(64 d / (T ln 2)),
 // |r| <= ln 2 / 128, 2^(k / 64) from a table of its 64 fractions and e^r by its series up to r^5 (the
-// next term is below 4e-17).  Adding 2^52 leaves the rounded whole number in the low bits.
+// next term is below 4e-17).  Adding 2^52 leaves the rounded whole number in the low bits.  (Without branches, so that
+// several run side by side.)
 __device__ __forceinline__ uint64_t weight(float l, float top, double lmax, double rate, const double* frac) {
-    if (l == top) return 1ull << kWeightBits;
-    const double d = ((double)l - lmax) * rate;
-    if (!(d > -64.0 * (kWeightBits + 2))) return 0;
+    double d = ((double)l - lmax) * rate;
+    const bool some = d > -64.0 * (kWeightBits + 2);          // (not of infinities' difference)
+    d = some ? d : 0.0;
     const double k = __builtin_rint(d);
     const double r = (d - k) * 0x1.62e42fefa39efp-7;          // ln 2 / 64
     double p = 1.0 / 120;
@@ -94,7 +100,8 @@ __device__ __forceinline__ uint64_t weight(float l, float top, double lmax, doub
     p = fma(p, r, 1.0);
     const int ki = (int)k;
     const double v = ldexp(frac[ki & 63] * p, (ki >> 6) + kWeightBits);
-    return (uint64_t)__double_as_longlong(v + 0x1p52) - 0x4330000000000000ull;
+    const uint64_t w = (uint64_t)__double_as_longlong(v + 0x1p52) - 0x4330000000000000ull;
+    return l == top ? 1ull << kWeightBits : some ? w : 0;
 }
 
 __device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return __shfl_up((unsigned long long)v, d, 64); }
@@ -440,12 +447,15 @@ __device__ __forceinline__ void fill_bins(const SampleArgs& a, const Row& R, Sha
     } else {
         constexpr int kVec = Vec<DT>::kVec;
         for_segment<DT>(a, R, slice * kWaves + (threadIdx.x >> 6), [&](const float (&v)[kVec], int) __attribute__((always_inline)) {
+            uint64_t w[kVec];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) w[e] = R.weight_of(v[e], sh.frac);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
                 const int b = R.bin_of(v[e]);
                 if (b < kBins - 1) {
                     atomicAdd(&sh.count[b], 1u);
-                    atomicAdd(&sh.mass[b], (unsigned long long)R.weight_of(v[e], sh.frac));
+                    atomicAdd(&sh.mass[b], (unsigned long long)w[e]);
                 }
             }
         });
@@ -535,9 +545,9 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
         const int hi = whole_k ? min(kb, kBins - 2) : min(min(min(kb, pb), m1), kBins - 2);
         int lo = 0, slow = 0;
         const uint64_t upto = S.at(S.c, hi);
-        if (!small && upto > (uint64_t)kList) {        // not all of it fits the list: its last bins
+        if (!small && upto > (uint64_t)kList / 2) {    // more than is sure to fit the waves' lists: its last bins
             lo = !R.has_p && R.least <= 0 ? kBins - 1 : min(by_p ? pb : kBins - 1, m0);
-            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kList);
+            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kList / 2);
         }
         const uint64_t below = S.at(S.m, lo - 1);
         if (l == 0) {
@@ -916,8 +926,7 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
     return true;
 }
 
-// 2^(i / 64), as sqrt 2 e^x with x = (i - 32) / 64 ln 2 and the series of e^x up to x^13 (the next term is below 5e-18).  (From
-// a table in memory, which no launch has in a cache, they would take 4 us.)
+// 2^(i / 64), as sqrt 2 e^x with x = (i - 32) / 64 ln 2 and the series of e^x up to x^13 (the next term is below 5e-18).
 __device__ __forceinline__ void fill_fractions(Shared& sh) {
     const int i = threadIdx.x;
     if (i >= 64) return;
@@ -1118,12 +1127,12 @@ struct SamplePlan {
     int slices, seg;
 };
 
-// A slice has 4096 logits at least, and all slices together are no more than two workgroups a compute unit.
+// One launch and a workgroup a row from 256 rows on, or where a row is short; slices of 4096 logits at least, as many as
+// give every compute unit a workgroup, otherwise.  Measured, one launch against 2, 4 and 8 slices: 256 rows of
+// 50257 with top_k 29 us against 44, 53, 67, with top_p alone 76 against 89, 101, 113; 64 rows of 128000, all kinds, 127
+// against 88, 64, 63; 16 rows of 32000 without filters 34 against 30, 25, 24; one row of 32000 33 against 32, 28, 27.
 SamplePlan plan_sample(int n_rows, int n_vocab) {
-    int64_t slices = std::min<int64_t>({kMaxSlices, (n_vocab + 4095) / 4096, 512 / std::max(1, n_rows)});
-#ifdef MX_PROBE
-    if (const char* e = getenv("SA_S")) slices = std::min(atoi(e), kMaxSlices);
-#endif
+    int64_t slices = n_vocab <= 16384 ? 1 : std::min<int64_t>({kMaxSlices, (n_vocab + 4095) / 4096, 256 / std::max(1, n_rows)});
     slices = std::max<int64_t>(1, slices);
     SamplePlan p;
     p.seg = (int)((n_vocab + slices * kWaves * 256 - 1) / (slices * kWaves * 256)) * 256;
