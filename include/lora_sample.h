@@ -17,7 +17,8 @@
  * however the work is divided.  The weight of a token less likely than the likeliest by
  * 2^44 is zero.  Sums are compared in binary64.
  *
- *   - T not above 0 (or NaN): the largest logit, prob 1.
+ *   - T below 2^-100 (0, less and NaN too): the largest logit, prob 1.  T above 2^100 is read as
+ *     2^100.
  *   - top_k below 1 or not below V: all.  top_p not below 1 (or NaN): all; not above 0: one
  *     logit.  min_p not above 0 (or NaN): all; 1 and more: those of weight 2^43.
  *   - u outside [0, 1) (or NaN) is read as 0 below and as the last token that is left above.

@@ -34,6 +34,7 @@ int check_mx(const char* name, const lora_mx_t* q) {
 namespace {
 
 constexpr int kNormMax = 65536;            // elements of a row: 1024 threads of 8 chunks
+constexpr int kNormRows = 1 << 20;         // of one launch: its threads stay below 2^32
 
 // 32-bit rows in memory, beside FmtF16 and FmtBF16.
 struct FmtF32 {};
@@ -313,6 +314,7 @@ constexpr uint32_t kLaunchChunks = 1u << 30;   // of one launch, at most (or one
 
 template <bool BACK>
 int enqueue_blocks(const char* name, const lora_mx_t* q, const void* values, int64_t ld, int32_t dtype, void* stream) {
+    if (q->n_rows == 0) return LORA_OK;
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
     if (!g.ok) return set_error(LORA_E_HIP, std::string(name) + ": no device for the stream");
@@ -425,14 +427,25 @@ int lora_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, con
     a.ldy = 2 * ldy;
     a.ld_codes = q ? q->ld_codes : 0;
     a.ld_scales = q ? q->ld_scales : 0;
-    a.n_rows = n_rows;
     a.chunks = h / 8;
     a.format = q ? q->format : 0;
     a.eps = eps;
     a.inv_h = 1.0 / h;
-    if (dtype == LORA_F16) launch_norm<FmtF16>(a, st);
-    else launch_norm<FmtBF16>(a, st);
-    return check_launch("lora_norm");
+    for (int left = n_rows; left > 0; left -= kNormRows) {
+        a.n_rows = std::min(left, kNormRows);
+        if (dtype == LORA_F16) launch_norm<FmtF16>(a, st);
+        else launch_norm<FmtBF16>(a, st);
+        if (int rc = check_launch("lora_norm")) return rc;
+        a.x += kNormRows * a.ldx;
+        if (a.residual) a.residual += kNormRows * a.ldr;
+        if (a.total) a.total += kNormRows * a.ldt;
+        if (a.y) a.y += kNormRows * a.ldy;
+        if (a.codes) {
+            a.codes += kNormRows * a.ld_codes;
+            a.scales += kNormRows * a.ld_scales;
+        }
+    }
+    return LORA_OK;
 }
 
 int lora_mx_quantize(const void* x, int64_t ldx, int32_t dtype, const lora_mx_t* q, void* stream) {

@@ -44,6 +44,8 @@ constexpr int kRanked = 256;               // up to which a list is ranked by co
 constexpr int kSmallK = 512;               // top_k up to which threads' largest logits bound it
 constexpr int kMaxSlices = 16;
 constexpr int kMaxVocab = 1 << 19;
+constexpr int kLaunchRows = 1 << 20;       // of one launch: its threads stay below 2^32
+constexpr float kLeastT = 0x1p-100f, kMostT = 0x1p100f;   // within which bins and logits' differences stay in range
 constexpr int kWeightBits = 43;            // sums of 2^19 weights stay below 2^62 (and exact)
 constexpr double kOne = 8796093022208.0;   // 2^43
 constexpr uint32_t kKeyNone = 0x007fffffu; // the key of -infinity
@@ -186,7 +188,7 @@ struct Row {
         const float t = *((a.temperature ? a.temperature : a.u) + r), q = *((a.top_p ? a.top_p : a.u) + r),
                     n = *((a.min_p ? a.min_p : a.u) + r);
         const int i = *((a.top_k ? a.top_k : (const int32_t*)a.u) + r);
-        T = a.temperature ? t : 1.f;
+        T = !a.temperature ? 1.f : t > kMostT ? kMostT : t;
         p = a.top_p ? q : 1.f;
         m = a.min_p ? n : 0.f;
         k = a.top_k ? i : 0;
@@ -198,11 +200,10 @@ struct Row {
     __device__ __forceinline__ void set_top(uint64_t best) {
         lmax_f = logit_of((uint32_t)(best >> 32));
         top_at = index_of(best);
-        done = (uint32_t)(best >> 32) <= kKeyNone || !(T > 0.f);
+        done = (uint32_t)(best >> 32) <= kKeyNone || !(T >= kLeastT);
         lmax = lmax_f;
         rate = 64 * 1.4426950408889634 / (double)T;
-        // (finite and not 0, so that only the difference decides where it is infinite)
-        bin_rate = fminf(fmaxf((float)kBinsPerNat / T, 1e-37f), 1e38f);
+        bin_rate = (float)kBinsPerNat / T;
         bin_top = fminf(lmax_f, 3.402823466e38f);
     }
     // top_k is small: the histogram is of threads' largest logits, and K's weights are summed in the list
@@ -1202,25 +1203,29 @@ int lora_sample(const void* logits, int64_t ld, int32_t dtype, int32_t n_rows, i
     StreamDevice g(st);
     if (!g.ok) return set_error(LORA_E_HIP, "lora_sample: no device for the stream");
     SampleArgs a;
-    a.logits = logits;
     a.ld = ld;
-    a.temperature = params->temperature;
-    a.top_p = params->top_p;
-    a.min_p = params->min_p;
-    a.u = u;
-    a.top_k = params->top_k;
-    a.tokens = tokens;
-    a.probs = probs;
     a.n_vocab = n_vocab;
     a.ws = (unsigned char*)ws;
     const SamplePlan p = plan_sample(n_rows, n_vocab);
     a.slices = p.slices;
     a.seg = p.seg;
     a.ws_row = RowSpace::bytes(p.slices);
-    if (dtype == LORA_F16) launch_sample<LORA_F16>(a, n_rows, st);
-    else if (dtype == LORA_BF16) launch_sample<LORA_BF16>(a, n_rows, st);
-    else launch_sample<LORA_F32>(a, n_rows, st);
-    return check_launch("lora_sample");
+    for (int r = 0, n; r < n_rows; r += n) {
+        n = std::min(n_rows - r, kLaunchRows);
+        a.logits = (const unsigned char*)logits + r * ld * e;
+        a.temperature = params->temperature ? params->temperature + r : nullptr;
+        a.top_k = params->top_k ? params->top_k + r : nullptr;
+        a.top_p = params->top_p ? params->top_p + r : nullptr;
+        a.min_p = params->min_p ? params->min_p + r : nullptr;
+        a.u = u + r;
+        a.tokens = tokens + r;
+        a.probs = probs ? probs + r : nullptr;
+        if (dtype == LORA_F16) launch_sample<LORA_F16>(a, n, st);
+        else if (dtype == LORA_BF16) launch_sample<LORA_BF16>(a, n, st);
+        else launch_sample<LORA_F32>(a, n, st);
+        if (int rc = check_launch("lora_sample")) return rc;
+    }
+    return LORA_OK;
 }
 
 }  // extern "C"

@@ -2,7 +2,8 @@
 
 Marshalling only, with the C functions' names.  ``Rows`` describes torch tensors of codes and
 scales to the library and keeps them alive; the calls take device buffers and streams as the
-rest of the package does.
+rest of the package does.  Rows that are not on one GPU, and workspaces given as tensors that are too
+short or on another device, are refused before anything is enqueued (``ValueError``).
 """
 from __future__ import annotations
 
@@ -47,6 +48,7 @@ class Rows:
             raise ValueError(f"a row of {h} elements takes {code_bytes(h, fmt)} bytes and {-(-h // 32)} scales, not "
                              f"{codes.shape[1]} and {scales.shape[1]}")
         self.codes, self.scales, self.fmt, self.h, self.device = codes, scales, fmt, h, codes.device
+        self.gpu = codes.get_device() if codes.is_cuda else -1
         self.n_rows = int(codes.shape[0])
         # (torch gives the stride of a single row any value)
         ldc, lds = ((codes.stride(0), scales.stride(0)) if self.n_rows > 1 else
@@ -97,17 +99,38 @@ def _addr(p) -> int:
         return 0 if p is None else int(p)
 
 
+def _on_gpu(*rows: Rows) -> None:
+    for r in rows:
+        if r.gpu != rows[0].gpu or r.gpu < 0:
+            raise ValueError(f"rows in blocks on {rows[0].device} and {r.device}: device tensors of one GPU are needed")
+
+
+def _space(t, n: int, device) -> int:
+    """The address of a workspace of at least n bytes."""
+    try:
+        p = t.data_ptr()
+    except AttributeError:
+        return 0 if t is None else int(t)
+    if t.numel() * t.element_size() < n or (device is not None and t.device != device) or not t.is_contiguous():
+        raise ValueError(f"ws: a contiguous tensor of {n} bytes or more on {device} is needed")
+    return p
+
+
 def lora_norm(x, ldx: int, residual, ldr: int, weight, eps: float, n_rows: int, h: int, dtype: int, total, ldt: int,
               y, ldy: int, q: Rows = None, stream=None) -> None:
+    if q is not None:
+        _on_gpu(q)
     _check(_lib().lora_norm(_addr(x), ldx, _addr(residual), ldr, _addr(weight), eps, n_rows, h, dtype, _addr(total), ldt,
                             _addr(y), ldy, q.c if q is not None else None, _stream(stream)))
 
 
 def lora_mx_quantize(x, ldx: int, dtype: int, q: Rows, stream=None) -> None:
+    _on_gpu(q)
     _check(_lib().lora_mx_quantize(_addr(x), ldx, dtype, q.c, _stream(stream)))
 
 
 def lora_mx_dequantize(q: Rows, y, ldy: int, dtype: int, stream=None) -> None:
+    _on_gpu(q)
     _check(_lib().lora_mx_dequantize(q.c, _addr(y), ldy, dtype, _stream(stream)))
 
 
@@ -118,4 +141,5 @@ def lora_mx_workspace_bytes(x: Rows, w: Rows) -> int:
 
 
 def lora_mx_apply(x: Rows, w: Rows, y, ldy: int, dtype: int, ws, ws_bytes: int, stream=None) -> None:
-    _check(_lib().lora_mx_apply(x.c, w.c, _addr(y), ldy, dtype, _addr(ws), ws_bytes, _stream(stream)))
+    _on_gpu(x, w)
+    _check(_lib().lora_mx_apply(x.c, w.c, _addr(y), ldy, dtype, _space(ws, ws_bytes, x.device), ws_bytes, _stream(stream)))

@@ -81,8 +81,9 @@ def sample(z, temperature, top_k, top_p, min_p, u):
     if len(order) == 0:
         return -1, 0, 1
     top = z[order[0]]
-    if not temperature > 0:
+    if not temperature >= 2.0 ** -100:
         return int(order[0]), 1, 1
+    temperature = min(temperature, 2.0 ** 100)
     with np.errstate(invalid="ignore", over="ignore", under="ignore"):
         d = np.where(z == top, 0.0, (z - top) / np.float64(temperature))
         w = np.rint(np.exp(np.where(np.isnan(d), -np.inf, d)) * ONE).astype(np.int64)

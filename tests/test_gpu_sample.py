@@ -156,6 +156,22 @@ def test_parameters_outside_their_ranges(dtype):
               u.astype(np.float32), dtype)
 
 
+@pytest.mark.parametrize("dtype", [R.BF16, R.F32], ids=NAMES.get)
+@pytest.mark.parametrize("v", [900, 70000])
+def test_temperatures_at_the_ends_of_their_range(v, dtype):
+    """Logits as far apart as the temperature, up to the type's whole range and down to its subnormal
+    numbers; past the ends of 2^-100 .. 2^100 the temperature does not matter any more."""
+    rng = np.random.default_rng([8, v])
+    t, scale = zip(*[(2.0 ** 100, 1e30), (1e38, 1e30), (np.inf, 1e30), (2.0 ** 100, 1e38), (1e30, 3e37), (1.1e30, 2e30),
+                     (2.0 ** -100, 1e-30), (7.8e-31, 1e-30), (1e-30, 1e-30), (1e-30, 1e-38), (1e-38, 1e-38), (1, 1e-40)])
+    rows = len(t)
+    z = torch.from_numpy(rng.standard_normal((rows, v)) * np.array(scale)[:, None]).to(DEV).to(TYPE[dtype])
+    for k, p, m in ((0, 1, 0), (0, 0.7, 0), (0, 1, 0.2), (40, 0.9, 0.05), (v - 1, 0.9, 0.01)):
+        full = lambda x, d: np.full(rows, x, d)  # noqa: E731
+        check(z, np.array(t, np.float32), full(k, np.int32), full(p, np.float32), full(m, np.float32),
+              rng.random(rows).astype(np.float32), dtype)
+
+
 def test_frequencies_follow_the_probabilities():
     """u in even steps meets every token as often as its share: counts are off by at most 1 on
     either side of its stretch, and by the rounding of u."""
