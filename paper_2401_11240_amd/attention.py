@@ -1,5 +1,5 @@
 """Adapted self-attention of a layer over the paged key-value cache: the calls of
-``lora`` and ``kv`` in the order in which a serving step makes them.
+``lora``, ``kv``, ``mx`` and ``sample`` in the order in which a serving step makes them.
 
 For the rows of a step (Section 2.2: one row per decoding request, a segment
 of rows per prompt), with x [n_rows, hidden]:
@@ -11,9 +11,21 @@ of rows per prompt), with x [n_rows, hidden]:
 
 Position encodings belong between the first two lines and are the caller's: a
 model that rotates q and k does it on ``q`` and ``k`` between ``project`` and
-``attend``.  Run as a command on a GPU, the module serves a small random stack
-of layers (prompts, branches, decode steps in a HIP graph, a window's pages given
-back, compaction) and prints what each part took.
+``attend``.
+
+A layer may have a norm in front of it, whose weight it holds; a step of such layers keeps
+the sum of its input and of what the layers gave (``total``), and a layer reads
+
+    total  += what the layer before gave       (in 16 bits)
+    h       = norm(total)
+
+as its x.  A base weight may be in 4-bit blocks (``mx.Rows``).  Then x goes into 8-bit blocks for it,
+y is rounded to 16 bits once behind the product and once behind the adapters' delta, which reads the
+16-bit x.  A ``Head`` behind the last layer leads from a sequence's last row to its next token.
+
+Run as a command on a GPU, the module serves two small random stacks of layers, of 16-bit weights
+(prompts, branches, decode steps in a HIP graph, a window's pages given back, compaction) and of
+4-bit weights with norms and a head (prompts, tokens in a HIP graph), and prints what each part took.
 """
 from __future__ import annotations
 
@@ -24,26 +36,44 @@ import numpy as np
 
 from . import kv as KV
 from . import lora as L
+from . import mx as MX
+from . import sample as SA
 
 
 @dataclass
 class Projection:
-    """A base weight, transposed ([h_out, h_in], as a linear layer keeps it), and
-    the table of its adapters."""
+    """A base weight, transposed ([h_out, h_in], as a linear layer keeps it; a tensor, or
+    ``mx.Rows`` of 4-bit blocks), and the table of its adapters."""
     table: int
     wt: object
 
     @property
+    def in_blocks(self):
+        return isinstance(self.wt, MX.Rows)
+
+    @property
     def shape(self):
+        if self.in_blocks:
+            return self.wt.h, self.wt.n_rows
         return int(self.wt.shape[1]), int(self.wt.shape[0])
 
 
 @dataclass
 class Layer:
+    """``norm``: the weight [hidden] of the norm in front of q, k and v, or None for no norm."""
     q: Projection
     k: Projection
     v: Projection
     o: Projection
+    norm: object = None
+
+
+@dataclass
+class Head:
+    """The last norm's weight [hidden] and the weight of the vocabulary, ``mx.Rows`` of 4-bit
+    blocks [n_vocab, hidden]."""
+    norm: object
+    wt: MX.Rows
 
 
 def _ordered(stream, device):
@@ -61,7 +91,7 @@ class Step:
     recorded in a HIP graph."""
 
     def __init__(self, layers: Sequence[Layer], cache: KV.Cache, seg_lens: Sequence[int], seg_adapter: Sequence[int],
-                 n_heads: int, window: int = 0, n_sinks: int = 0, stream=None):
+                 n_heads: int, window: int = 0, n_sinks: int = 0, stream=None, head: Head = None, eps: float = 1e-5):
         import torch
         self.layers, self.cache, self.n_heads, self.window, self.n_sinks = list(layers), cache, n_heads, window, n_sinks
         head_dim = int(cache.k.shape[4])
@@ -78,6 +108,10 @@ class Step:
             for name, p, side, n in want:
                 if p.shape[side] != n:
                     raise ValueError(f"layer {i}: the {name} projection is {p.shape}, the heads take {n}")
+        self.head, self.eps = head, eps
+        self.normed = any(layer.norm is not None for layer in self.layers)
+        if any((layer.norm is not None) != self.normed for layer in self.layers) or (head and not self.normed):
+            raise ValueError("a norm in front of every layer or of none is needed, and of every one with a head")
         self.single = all(n == 1 for n in seg_lens)      # one row per sequence: the decode form
         self.batch = L.Batch(offset, np.asarray(seg_adapter, np.int32), self.n_rows)
         dev, dt = cache.k.device, cache.k.dtype
@@ -87,6 +121,7 @@ class Step:
             self.k = torch.empty((self.n_rows, self.kv_width), dtype=dt, device=dev)
             self.v = torch.empty_like(self.k)
             self.a = torch.empty_like(self.q)
+            self._make_blocks(seg_lens)
         self._plans, self._plan_of = [], {}              # plans with their shapes; a table's plan
         try:
             for layer in self.layers:
@@ -96,31 +131,90 @@ class Step:
             self.release()
             raise
 
+    def _make_blocks(self, seg_lens):
+        """What norms, weights in blocks and a head need beside q, k, v and a."""
+        import torch
+        dev, dt = self.q.device, self.q.dtype
+        self.code = L.LORA_F16 if dt == torch.float16 else L.LORA_BF16
+        self.hidden = self.layers[0].q.shape[0] if self.layers else 0
+        self.total = self.h = self.hq = self.aq = self.last = None
+        for i, layer in enumerate(self.layers):
+            if self.normed and (layer.q.shape[0] != self.hidden or layer.o.shape[1] != self.hidden):
+                raise ValueError(f"layer {i}: norms need layers of one width, {self.hidden}")
+            if self.normed:
+                self._check_weight(f"layer {i}", layer.norm)
+            for p in (layer.q, layer.k, layer.v, layer.o):
+                if p.in_blocks and (p.wt.fmt != MX.LORA_E2M1 or p.wt.device != dev):
+                    raise ValueError(f"layer {i}: weights in blocks are LORA_E2M1, on {dev}")
+        if self.normed:
+            self.total = torch.empty((self.n_rows, self.hidden), dtype=dt, device=dev)
+            self.h = torch.empty_like(self.total)
+        need = [0]
+        rows = {}
+        for layer in self.layers:
+            for p, name in ((layer.q, "hq"), (layer.k, "hq"), (layer.v, "hq"), (layer.o, "aq")):
+                if p.in_blocks:
+                    key = name, p.shape[0]
+                    if key not in rows:
+                        rows[key] = MX.empty_rows(self.n_rows, p.shape[0], MX.LORA_E4M3, dev)
+                    need.append(MX.lora_mx_workspace_bytes(rows[key], p.wt))
+        self._rows = rows                                # x and a in blocks, by width
+        if self.head:
+            self._check_weight("head", self.head.norm)
+            wt, n = self.head.wt, self.n_segments
+            if wt.fmt != MX.LORA_E2M1 or wt.device != dev or wt.h != self.hidden:
+                raise ValueError(f"head: a weight in LORA_E2M1 blocks of {self.hidden} on {dev} is needed")
+            ends = np.cumsum(seg_lens) - 1
+            self.empty = torch.from_numpy(np.asarray(seg_lens) == 0).to(dev) if min(seg_lens, default=1) == 0 else None
+            # (a segment of no rows takes some other row, and no token)
+            self.last = None if self.single else torch.from_numpy(np.maximum(ends, 0).astype(np.int64)).to(dev)
+            self.last_rows = [torch.zeros((n, self.hidden), dtype=dt, device=dev) for _ in range(2)]
+            self.last_q = MX.empty_rows(n, self.hidden, MX.LORA_E4M3, dev)
+            self.logits = torch.empty((n, wt.n_rows), dtype=torch.float32, device=dev)
+            need.append(MX.lora_mx_workspace_bytes(self.last_q, wt))
+            need.append(SA.lora_sample_workspace_bytes(n, wt.n_rows, SA.LORA_F32))
+        self.ws_bytes = max(need)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+
+    def _check_weight(self, what: str, w):
+        if w.shape != (self.hidden,) or w.dtype != self.q.dtype or w.device != self.q.device or not w.is_contiguous():
+            raise ValueError(f"{what}: a norm's weight is {self.q.dtype} [{self.hidden}] on {self.q.device}, contiguous")
+
     def _plan_for(self, p: Projection, stream):
         """One plan serves all tables of a shape whose adapters agree in rank."""
         if p.table in self._plan_of:
             return
-        for shape, plan in self._plans:
-            if shape == p.shape and self._fits(plan, p):
+        for kind, plan in self._plans:
+            if kind == (p.shape, p.in_blocks) and self._fits(plan, p):
                 break
         else:
-            plan = L.lora_base_plan_create(p.table, self.batch, stream)
-            self._plans.append((p.shape, plan))
+            plan = (L.lora_plan_create if p.in_blocks else L.lora_base_plan_create)(p.table, self.batch, stream)
+            self._plans.append(((p.shape, p.in_blocks), plan))
         self._plan_of[p.table] = plan
 
     @staticmethod
     def _fits(plan: int, p: Projection) -> bool:
         # (a call without operands enqueues nothing: it is refused for the table where that does not
-        # fit the plan, for the missing x where it does; a plan of no rows takes it)
+        # fit the plan, for the missing x where it does; a plan of no rows takes it.  The delta's plan looks for
+        # missing operands first: there it is an x that no call may have)
         try:
-            L.lora_base_plan_apply(plan, p.table, None, p.shape[0], None, p.shape[0], None, p.shape[1])
+            if p.in_blocks:
+                L.lora_plan_apply(plan, p.table, 1, p.shape[0], 1, p.shape[1])
+            else:
+                L.lora_base_plan_apply(plan, p.table, None, p.shape[0], None, p.shape[0], None, p.shape[1])
         except L.LoraError as e:
-            return e.code == L.LORA_E_ARG
+            return e.code == (L.LORA_E_ALIGN if p.in_blocks else L.LORA_E_ARG)
         return True
 
-    def _apply(self, p: Projection, x, y, stream):
-        L.lora_base_plan_apply(self._plan_of[p.table], p.table, x, x.stride(0), p.wt, p.wt.stride(0), y, y.stride(0),
-                               stream)
+    def _apply(self, p: Projection, x, y, stream, rows=None):
+        """``rows``: x in blocks, for a weight in blocks."""
+        plan = self._plan_of[p.table]
+        if p.in_blocks:
+            MX.lora_mx_apply(rows, p.wt, y, y.stride(0), self.code, self.ws, self.ws_bytes, stream)
+            if self.n_rows:                  # (without rows x and y have no memory, which the call refuses)
+                L.lora_plan_apply(plan, p.table, x, x.stride(0), y, y.stride(0), stream)
+        else:
+            L.lora_base_plan_apply(plan, p.table, x, x.stride(0), p.wt, p.wt.stride(0), y, y.stride(0), stream)
 
     def _check_seqs(self, seqs: KV.Seqs):
         # (the launches read an offset per sequence)
@@ -136,11 +230,22 @@ class Step:
                              f"in the last dimension, is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def project(self, layer: int, x, stream=None) -> None:
-        """q, k and v of the step's rows, into ``self.q``, ``self.k`` and ``self.v``."""
+        """q, k and v of the step's rows, into ``self.q``, ``self.k`` and ``self.v``.  With norms x
+        begins ``total`` at layer 0 and is added to it at the others."""
         w = self.layers[layer]
         self._check_rows("x", x, w.q.shape[0])
+        if self.normed:
+            rows = self._rows.get(("hq", self.hidden)) if any(p.in_blocks for p in (w.q, w.k, w.v)) else None
+            MX.lora_norm(x, x.stride(0), self.total if layer else None, self.hidden, w.norm, self.eps, self.n_rows, self.hidden,
+                         self.code, self.total, self.hidden, self.h, self.hidden, rows, stream)
+            x = self.h
+        done = {self.hidden} if self.normed else set()   # widths of x that are in blocks already
         for p, y in ((w.q, self.q), (w.k, self.k), (w.v, self.v)):
-            self._apply(p, x, y, stream)
+            rows = self._rows.get(("hq", p.shape[0])) if p.in_blocks else None
+            if rows is not None and p.shape[0] not in done:
+                MX.lora_mx_quantize(x, x.stride(0), self.code, rows, stream)
+                done.add(p.shape[0])
+            self._apply(p, x, y, stream, rows)
 
     def attend(self, attn: int, layer: int, seqs: KV.Seqs, y, stream=None) -> None:
         """The rows' keys and values into the cache, attention, the o projection."""
@@ -154,10 +259,15 @@ class Step:
             KV.lora_attn_decode(attn, self.cache, layer, seqs, *rows)
         else:
             KV.lora_attn_prompt(attn, self.cache, layer, seqs, self.seg_offset, self.n_rows, *rows)
-        self._apply(self.layers[layer].o, self.a, y, stream)
+        o = self.layers[layer].o
+        rows = self._rows[("aq", self.width)] if o.in_blocks else None
+        if rows is not None:
+            MX.lora_mx_quantize(self.a, self.width, self.code, rows, stream)
+        self._apply(o, self.a, y, stream, rows)
 
     def run(self, attn: int, seqs: KV.Seqs, x, y, stream=None) -> None:
-        """Every layer: the first reads x, the others what the one before wrote to y."""
+        """Every layer: the first reads x, the others what the one before wrote to y (which with norms they add
+        to ``total``; the last one's is left to the head)."""
         self._check_seqs(seqs)
         if self.layers:
             self._check_rows("y", y, self.layers[0].o.shape[1])
@@ -165,10 +275,36 @@ class Step:
             self.project(i, x if i == 0 else y, stream)
             self.attend(attn, i, seqs, y, stream)
 
+    def choose(self, y, params, u, tokens, probs=None, stream=None) -> None:
+        """The next token of every sequence from its last row of ``total`` + y, y what ``run`` left: ``tokens``
+        (int32 [n_segments]) and, unless None, ``probs``; -1 and 0 for a sequence without rows.
+        ``params`` (``sample.Params`` or None) and ``u`` as ``lora_sample`` takes them."""
+        import torch
+        head, n, v = self.head, self.n_segments, self.head.wt.n_rows if self.head else 0
+        if head is None:
+            raise ValueError("a step without a head has no tokens")
+        self._check_rows("y", y, self.hidden)
+        x, total, ldy = y, self.total, y.stride(0)
+        if self.last is not None and self.n_rows:
+            with _ordered(stream, self.q.device):
+                for src, dst in ((y[:, :self.hidden], self.last_rows[0]), (self.total, self.last_rows[1])):
+                    torch.index_select(src, 0, self.last, out=dst)
+        if self.last is not None:
+            (x, total), ldy = self.last_rows, self.hidden
+        MX.lora_norm(x, ldy, total, self.hidden, head.norm, self.eps, n, self.hidden, self.code, None, 0, None, 0, self.last_q,
+                     stream)
+        MX.lora_mx_apply(self.last_q, head.wt, self.logits, v, MX.LORA_F32, self.ws, self.ws_bytes, stream)
+        SA.lora_sample(self.logits, v, SA.LORA_F32, n, v, params, u, tokens, probs, self.ws, self.ws_bytes, stream)
+        if self.empty is not None:
+            with _ordered(stream, self.q.device):
+                tokens[:n].masked_fill_(self.empty, -1)
+                if probs is not None:
+                    probs[:n].masked_fill_(self.empty, 0.)
+
     def release(self) -> None:
         """Frees the plans: no launch, recorded or enqueued, may still use them."""
-        for _, plan in self._plans:
-            L.lora_base_plan_destroy(plan)
+        for (_, in_blocks), plan in self._plans:
+            (L.lora_plan_destroy if in_blocks else L.lora_base_plan_destroy)(plan)
         self._plans, self._plan_of = [], {}
 
 
@@ -228,9 +364,10 @@ class Server:
 
 
 def random_layers(n_layers: int, hidden: int, n_heads: int, n_kv_heads: int, head_dim: int, dtype, ranks, device,
-                  seed: int = 0, stream=None):
+                  seed: int = 0, stream=None, in_blocks: bool = False):
     """Layers of random weights and adapters (scales 16 / r), and the tensors that
-    the tables point at (keep them while the tables live)."""
+    the tables point at (keep them while the tables live).  ``in_blocks``: weights in 4-bit
+    blocks, and a norm in front of every layer."""
     import torch
     gen = torch.Generator(device=device).manual_seed(seed)
 
@@ -242,7 +379,7 @@ def random_layers(n_layers: int, hidden: int, n_heads: int, n_kv_heads: int, hea
     kept = []
 
     def projection(h_in, h_out):
-        wt = draw(h_out, h_in)
+        wt = in_4_bits(draw(h_out, h_in), stream) if in_blocks else draw(h_out, h_in)
         A = [draw(r, h_in).t().contiguous() for r in ranks]
         B = [(draw(h_out, r) * 0.25).t().contiguous() for r in ranks]
         scales = [16.0 / r for r in ranks]
@@ -253,9 +390,22 @@ def random_layers(n_layers: int, hidden: int, n_heads: int, n_kv_heads: int, hea
         return Projection(table, wt)
 
     w, kw = n_heads * head_dim, n_kv_heads * head_dim
-    layers = [Layer(projection(hidden, w), projection(hidden, kw), projection(hidden, kw), projection(w, hidden))
+    layers = [Layer(projection(hidden, w), projection(hidden, kw), projection(hidden, kw), projection(w, hidden),
+                    1 + draw(hidden) if in_blocks else None)
               for _ in range(n_layers)]
     return layers, kept
+
+
+def in_4_bits(wt, stream=None) -> MX.Rows:
+    """A 16-bit device tensor [h_out, h_in] in 4-bit blocks."""
+    import torch
+    code = L.LORA_F16 if wt.dtype == torch.float16 else L.LORA_BF16
+    if stream is None:
+        stream = torch.cuda.current_stream(wt.device)
+    with _ordered(stream, wt.device):
+        rows = MX.empty_rows(wt.shape[0], wt.shape[1], MX.LORA_E2M1, wt.device)
+    MX.lora_mx_quantize(wt, wt.stride(0) if wt.shape[0] > 1 else wt.shape[1], code, rows, stream)
+    return rows
 
 
 def main() -> None:
@@ -310,6 +460,66 @@ def main() -> None:
         timed("compaction", srv.compact)
         print("pages in use, pages moved:", srv.info.tolist(), "of", shape[1], flush=True)
         timed("a token after compaction", graph.replay)
+        st.synchronize()
+        del graph
+        step.release()
+        decode.release()
+        srv.release()
+        for layer in layers:
+            for p in (layer.q, layer.k, layer.v, layer.o):
+                L.lora_release_adapters(p.table)
+        del kept
+
+        # weights in 4 bits, norms, and every sequence's token the input of its next step
+        n_vocab, max_new = 32000, 100
+        layers, kept = random_layers(n_layers, hidden, heads, kv_heads, dim, dt, [8, 16, 32, 64], dev, 1, st, in_blocks=True)
+        embed = torch.randn((n_vocab, hidden), device=dev).to(dt)
+        head = Head(torch.ones(hidden, device=dev, dtype=dt), in_4_bits((torch.randn_like(embed) * hidden ** -0.5).to(dt), st))
+        prompts = [203, 512, 64, 1000, 17, 300, 128, 700] * 3
+        shape = (n_layers, sum((p + max_new + 16) // 16 + 1 for p in prompts), kv_heads, 16, dim)
+        cache = KV.Cache(torch.zeros(shape, dtype=dt, device=dev), torch.zeros(shape, dtype=dt, device=dev))
+        srv = Server(cache, n_seqs, max_len, st)
+        tokens = torch.zeros(n_seqs, dtype=torch.int32, device=dev)
+        chosen = torch.zeros((max_new + 2, n_seqs), dtype=torch.int32, device=dev)
+        at = torch.zeros(1, dtype=torch.int64, device=dev)
+        u = torch.rand(chosen.shape, device=dev)
+        params = SA.Params(torch.full((n_seqs,), 0.8, device=dev), None, torch.full((n_seqs,), 0.95, device=dev))
+        uu = torch.empty(n_seqs, device=dev)
+
+        def choose(s, y):
+            uu.copy_(torch.index_select(u, 0, at)[0])
+            s.choose(y, params, uu, tokens, None, st)
+            chosen.index_copy_(0, at, tokens[None])
+            at.add_(1)
+
+        step = Step(layers, cache, prompts, adapters, heads, window, sinks, st, head)
+        x = torch.index_select(embed, 0, torch.randint(n_vocab, (step.n_rows,), device=dev))
+        y = torch.empty_like(x)
+        srv.grow(torch.tensor(prompts, dtype=torch.int32, device=dev))
+
+        def first():
+            step.run(srv.attn, srv.seqs, x, y, st)
+            choose(step, y)
+
+        first()                                          # (once untimed: code and memory are there from then on)
+        at.zero_()
+        timed(f"4-bit weights: {step.n_rows} prompt rows to {n_seqs} tokens, {n_layers} layers", first)
+        decode = Step(layers, cache, [1] * n_seqs, adapters, heads, window, sinks, st, head)
+
+        def token():
+            srv.grow(ones)
+            torch.index_select(embed, 0, tokens, out=dx)
+            decode.run(srv.attn, srv.seqs, dx, dy, st)
+            choose(decode, dy)
+
+        token()
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            token()
+        timed(f"4-bit weights: a token of {n_seqs} sequences, {n_layers} layers, {n_vocab} logits",
+              lambda: [graph.replay() for _ in range(max_new)], max_new)
+        print("sequence 0:", chosen[:8, 0].tolist(), "...", flush=True)
         st.synchronize()
         del graph
         step.release()
