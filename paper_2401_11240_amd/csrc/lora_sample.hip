@@ -3,7 +3,7 @@
 // The way to the token:
 //
 //   1. the largest logit of the row (weights are relative to it);
-//   2. a histogram over bins of 1/16 in (l_max - l) / T: logits and weights per bin.  From its running sums come a
+//   2. a histogram over bins of 1/32 in (l_max - l) / T: logits and weights per bin.  From its running sums come a
 //      first bin `lo` and a last bin `hi`: logits of bins below lo are kept by all filters, those above hi by none
 //      (what lies past 32 weighs nothing).  Where top_k is small, every thread's largest logit is enough: at
 //      least top_k logits are as large as the top_k-th of those, and not many more;
@@ -37,9 +37,10 @@ namespace {
 
 constexpr int kSampleThreads = 1024, kWaves = kSampleThreads / 64;
 constexpr int kDigits = 2048;
-constexpr int kBins = 512, kBinsPerNat = 16;   // the last bin: 31.9 and more, whose weights are zero
+constexpr int kBins = 1024, kBinsPerNat = 32;  // the last bin: 31.9 and more, whose weights are zero
 constexpr int kList = 4096;                // logits of a list
 constexpr int kWaveList = kList / kWaves;  // of one wave's part of it
+constexpr int kFits = kList * 3 / 4;       // up to which the waves' parts are expected to hold them
 constexpr int kRanked = 256;               // up to which a list is ranked by comparing all with all
 constexpr int kSmallK = 512;               // top_k up to which threads' largest logits bound it
 constexpr int kMaxSlices = 16;
@@ -530,25 +531,22 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
             const double limit = (double)R.p * (double)(kb < kBins - 1 ? S.at(S.m, kb) : all);
             pb = min(pb, S.first([&](int j) { return (double)S.m[j] >= limit; }));
         }
-        // bins in which min_p may cut, with some to spare on either side for the roundings (weights of a few units
+        // the last bin with a logit that min_p keeps, with some to spare for the roundings (weights of a few units
         // are rounded by up to ln 2)
-        int m0 = kBins - 1, m1 = kBins - 2;
+        int m1 = kBins - 2;
         if (R.least > 0) {
             const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
-            const int spare = R.least < 256 ? 12 : 1;
-            if (f < (float)(kBins - 2)) {
-                m0 = max((int)f - spare, 0);
-                m1 = min((int)f + spare, kBins - 2);
-            }
+            const int spare = R.least < 256 ? kBinsPerNat * 3 / 4 : 2;
+            if (f < (float)(kBins - 2)) m1 = min((int)f + spare, kBins - 2);
         }
         // (top_p needs the sum over K: all of it is in the list, if the bins do not have the row's)
         const bool whole_k = R.has_p && R.p > 0.f && k_cuts;
         const int hi = whole_k ? min(kb, kBins - 2) : min(min(min(kb, pb), m1), kBins - 2);
         int lo = 0, slow = 0;
         const uint64_t upto = S.at(S.c, hi);
-        if (!small && upto > (uint64_t)kList / 2) {    // more than is sure to fit the waves' lists: its last bins
-            lo = !R.has_p && R.least <= 0 ? kBins - 1 : min(by_p ? pb : kBins - 1, m0);
-            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kList / 2);
+        if (!small && upto > (uint64_t)kFits) {        // more than a list: top_p's last bin, if it is among them
+            lo = R.has_p && pb <= hi ? pb : hi + 1;
+            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kFits);
         }
         const uint64_t below = S.at(S.m, lo - 1);
         if (l == 0) {
@@ -606,7 +604,7 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
             for (int e = 0; e < kVec; ++e) {
                 const int b = R.bin_of(v[e]);
                 in |= (uint32_t)(b >= lo && b <= hi) << e;
-                if (b < min(lo, hi + 1)) sum += R.weight_of(v[e], sh.frac);
+                if (b < lo) sum += R.kept(R.weight_of(v[e], sh.frac));
             }
             add(in, v, i);
         });
@@ -888,8 +886,7 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
         l = l == l ? l : -INFINITY;
         const int b = R.bin_of(l);
         uint64_t x = 0;
-        if (b < min(cut.lo, cut.hi + 1)) x = R.weight_of(l, sh.frac);
-        else if (b <= cut.hi && ranked(l, i) >= last) x = R.kept(R.weight_of(l, sh.frac));
+        if (b < cut.lo || (b <= cut.hi && ranked(l, i) >= last)) x = R.kept(R.weight_of(l, sh.frac));
         const uint64_t mine = run + scan(sh, x, all);
         if (x && mine <= target && target < mine + x) R.choose(a, i, x, total);
         run += all;
