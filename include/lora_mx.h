@@ -73,12 +73,12 @@ typedef struct {
 } lora_mx_t;
 
 /*
- * For every row, in float32 with one rounding at each output:
+ * For every row, in float32 and more, with one rounding at each output:
  *
  *     s = x + residual          total gets s
  *     y = s * weight / sqrt(mean(s^2) + eps)
  *
- * and q gets y in blocks (from the float32 y).  residual, weight and total may be NULL (no
+ * and q gets y in blocks (from y before its rounding to `dtype`).  residual, weight and total may be NULL (no
  * addition, ones, s not kept); y or q may be NULL, not both.  x, residual, total and y
  * [n_rows, ld] and weight [h] are of `dtype` (LORA_F16 or LORA_BF16), q of LORA_E4M3 or
  * LORA_E2M1 with n_rows rows.  total may be x or residual itself, and y may be x or residual itself

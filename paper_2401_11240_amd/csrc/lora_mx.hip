@@ -8,6 +8,7 @@
 #include <cmath>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lora_device.h"
 #include "lora_mx_internal.h"
@@ -139,9 +140,16 @@ struct NormArgs {
     double inv_h;
 };
 
+// The float32 y with a rest of the exact value beyond it, moved by its last bit towards the rest.
+__device__ __forceinline__ float towards(float y, float rest) {
+    const uint32_t b = __float_as_uint(y);
+    constexpr int kFinite = 0x198;         // normal and subnormal, of either sign: not zero, infinity or NaN
+    return __builtin_amdgcn_classf(rest, kFinite) ? __uint_as_float(b + ((int)(b ^ __float_as_uint(rest)) >> 31 | 1)) : y;
+}
+
 // A row by TPR threads (a wave, or a workgroup of 256 or 1024), CH chunks each, which stay in
 // registers between the sum of squares and the outputs: x and the residual are read once.  HBM bounds many rows (8437 x
-// 5120 with all outputs 73-76 us, 5.1-5.3 TB/s), the launch and the chain of load, sum and barrier a few (3.5 us).
+// 5120 with all outputs 73-76 us, 5.1-5.3 TB/s), the launch and the chain of load, sum and barrier a few (one row of 4096: 3.7 us).
 // Every output of a row is written after all of its inputs are read where that is asked
 // for: y depends on the whole row, and total[i] only on x[i] and residual[i].
 template <class Fmt, int CH, int TPR>
@@ -151,13 +159,14 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
     const int row = blockIdx.x * kRows + threadIdx.x / TPR;
     if (row >= a.n_rows) return;           // (a whole wave: without a barrier below)
     const unsigned char* x = a.x + row * a.ldx;
-    Chunk<Fmt> in[CH], res[CH], g[CH];
+    constexpr uint32_t kOnes = std::is_same<Fmt, FmtF16>::value ? 0x3c003c00u : 0x3f803f80u;
+    Chunk<Fmt> in[CH], res[CH], g[CH];       // (zeros and ones for a residual and a weight that are not there)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * TPR + t;
         in[i].clear();
         res[i].clear();
-        g[i].clear();
+        g[i].w = u32x4{kOnes, kOnes, kOnes, kOnes};
         if (c < a.chunks) {
             in[i].load(x + 16 * c);
             if (a.residual) res[i].load(a.residual + row * a.ldr + 16 * c);
@@ -174,7 +183,7 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
         float q = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (a.residual) s[i][e] += r[e];
+            s[i][e] += r[e];
             q = fmaf(s[i][e], s[i][e], q);
         }
         sum += q;
@@ -191,7 +200,10 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
         for (int i = 0; i < TPR / 64; ++i) sum += part[i];
     }
     // 1 / sqrt in binary64 (an estimate and one Newton step), as a float32 and what it leaves: with them the product
-    // s rstd w below is off by little more than its last rounding, and 8-bit codes hardly ever by that
+    // s rstd w below is off by little more than its rounding to float32.  That one matters to the outputs' only where it
+    // ends half way between two of their values: there the rest decides.  (Without that about one of 2 million 8-bit
+    // codes comes out next to the right one; with the rest carried through every product 8437 x 5120 takes 82.7 us, so
+    // 73.7.)
     const double ms = sum * a.inv_h + (double)a.eps;
     double r64 = __builtin_amdgcn_rsq(ms);
     r64 = ms < INFINITY ? r64 * (1.5 - 0.5 * ms * r64 * r64) : r64;    // (0 for infinity, NaN for NaN)
@@ -199,22 +211,38 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * TPR + t;
-        float w[8];
+        constexpr uint32_t kHalfWay = std::is_same<Fmt, FmtF16>::value ? 0xfff : 0x7fff;
+        float w[8], v[8];
         g[i].get(w);
+        uint32_t half_way = ~0u;           // 0 if one of the chunk may lie half way between two values of an output
+        auto product = [&](int e, float& lo_by) __attribute__((always_inline)) {
+            const float hi = s[i][e] * rstd, lo = fmaf(s[i][e], rest, fmaf(s[i][e], rstd, -hi));
+            lo_by = lo * w[e];
+            return hi;
+        };
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float hi = s[i][e] * rstd, lo = fmaf(s[i][e], rest, fmaf(s[i][e], rstd, -hi));
-            const float by = a.weight ? w[e] : 1.f;    // (one form: hi + lo could be contracted to other bits)
-            s[i][e] = fmaf(hi, by, lo * by);
+            float lo_by;
+            const float hi = product(e, lo_by);
+            v[e] = fmaf(hi, w[e], lo_by);
+            half_way = min(half_way, __float_as_uint(v[e]) & kHalfWay);
         }
-        if (a.y && c < a.chunks) Chunk<Fmt>::put(a.y + row * a.ldy + 16 * c, s[i]);
+        if (__builtin_expect(__any(half_way == 0 && c < a.chunks), 0)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float lo_by;
+                const float hi = product(e, lo_by);
+                if ((__float_as_uint(v[e]) & kHalfWay) == 0) v[e] = towards(v[e], fmaf(hi, w[e], -v[e]) + lo_by);
+            }
+        }
+        if (a.y && c < a.chunks) Chunk<Fmt>::put(a.y + row * a.ldy + 16 * c, v);
         if (a.codes && i * TPR < a.chunks) {
             if (c >= a.chunks) {           // (rows of zeros may not be: 0 times infinity)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[i][e] = 0.f;
+                for (int e = 0; e < 8; ++e) v[e] = 0.f;
             }
             u32x2 codes;
-            const uint32_t scale = encode(s[i], a.format, codes);
+            const uint32_t scale = encode(v, a.format, codes);
             if (c < ((a.chunks + 3) & ~3))
                 put_codes(a.codes + row * a.ld_codes, a.scales + row * a.ld_scales, c, a.format, codes, scale);
         }
