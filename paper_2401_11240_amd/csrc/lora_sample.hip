@@ -20,9 +20,10 @@
 // Sums are whole numbers, so neither the order of atomic additions nor the division of a row over workgroups changes
 // a bit.
 //
-// What bounds it: a few rows, the four launches (3 to 9 us each in a trace, most of it the way of the first loads and of
+// What bounds it: a few rows, the four launches (3 to 10 us each in a trace; one row of 32000: 27 us, most of it the way of the first loads and of
 // barriers of sixteen waves); many rows with top_p and no small top_k, the weights of all logits, about 25 binary64
-// operations each, twice where the list does not hold all that is kept, and their atomic additions; many rows with
+// operations each, twice where the list does not hold all that is kept, and their atomic additions (64 rows of 128000 in
+// bfloat16: 67-70 us; with one of them done by slow_row 365); many rows with
 // a small top_k, two readings of the logits (256 x 50257 in float32: 29 us, 51 MB).
 #include <cmath>
 
