@@ -71,9 +71,16 @@ class Layer:
 @dataclass
 class Head:
     """The last norm's weight [hidden] and the weight of the vocabulary, ``mx.Rows`` of 4-bit
-    blocks [n_vocab, hidden]."""
+    blocks [n_vocab, hidden].  ``n_vocab``: the tokens, where the weight has more rows than those (the product
+    takes a multiple of 8)."""
     norm: object
     wt: MX.Rows
+    n_vocab: int = 0
+
+    def __post_init__(self):
+        self.n_vocab = self.n_vocab or self.wt.n_rows
+        if not 0 < self.n_vocab <= self.wt.n_rows:
+            raise ValueError(f"n_vocab is {self.n_vocab}, the weight has {self.wt.n_rows} rows")
 
 
 def _ordered(stream, device):
@@ -172,7 +179,7 @@ class Step:
             self.last_q = MX.empty_rows(n, self.hidden, MX.LORA_E4M3, dev)
             self.logits = torch.empty((n, wt.n_rows), dtype=torch.float32, device=dev)
             need.append(MX.lora_mx_workspace_bytes(self.last_q, wt))
-            need.append(SA.lora_sample_workspace_bytes(n, wt.n_rows, SA.LORA_F32))
+            need.append(SA.lora_sample_workspace_bytes(n, self.head.n_vocab, SA.LORA_F32))
         self.ws_bytes = max(need)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
 
@@ -277,7 +284,8 @@ class Step:
 
     def choose(self, y, params, u, tokens, probs=None, stream=None) -> None:
         """The next token of every sequence from its last row of ``total`` + y, y what ``run`` left: ``tokens``
-        (int32 [n_segments]) and, unless None, ``probs``; -1 and 0 for a sequence without rows.
+        (int32 [n_segments]) and, unless None, ``probs``; -1 and 0 for a segment of no rows.  (Only the device
+        knows which sequences did not fit, ``Server.step_lens`` is 0 for those: their tokens mean nothing.)
         ``params`` (``sample.Params`` or None) and ``u`` as ``lora_sample`` takes them."""
         import torch
         head, n, v = self.head, self.n_segments, self.head.wt.n_rows if self.head else 0
@@ -294,7 +302,7 @@ class Step:
         MX.lora_norm(x, ldy, total, self.hidden, head.norm, self.eps, n, self.hidden, self.code, None, 0, None, 0, self.last_q,
                      stream)
         MX.lora_mx_apply(self.last_q, head.wt, self.logits, v, MX.LORA_F32, self.ws, self.ws_bytes, stream)
-        SA.lora_sample(self.logits, v, SA.LORA_F32, n, v, params, u, tokens, probs, self.ws, self.ws_bytes, stream)
+        SA.lora_sample(self.logits, v, SA.LORA_F32, n, head.n_vocab, params, u, tokens, probs, self.ws, self.ws_bytes, stream)
         if self.empty is not None:
             with _ordered(stream, self.q.device):
                 tokens[:n].masked_fill_(self.empty, -1)
@@ -379,7 +387,7 @@ def random_layers(n_layers: int, hidden: int, n_heads: int, n_kv_heads: int, hea
     kept = []
 
     def projection(h_in, h_out):
-        wt = in_4_bits(draw(h_out, h_in), stream) if in_blocks else draw(h_out, h_in)
+        wt = in_4_bits(draw(h_out, h_in)) if in_blocks else draw(h_out, h_in)
         A = [draw(r, h_in).t().contiguous() for r in ranks]
         B = [(draw(h_out, r) * 0.25).t().contiguous() for r in ranks]
         scales = [16.0 / r for r in ranks]
@@ -396,15 +404,12 @@ def random_layers(n_layers: int, hidden: int, n_heads: int, n_kv_heads: int, hea
     return layers, kept
 
 
-def in_4_bits(wt, stream=None) -> MX.Rows:
-    """A 16-bit device tensor [h_out, h_in] in 4-bit blocks."""
+def in_4_bits(wt) -> MX.Rows:
+    """A 16-bit device tensor [h_out, h_in] in 4-bit blocks, on torch's current stream."""
     import torch
     code = L.LORA_F16 if wt.dtype == torch.float16 else L.LORA_BF16
-    if stream is None:
-        stream = torch.cuda.current_stream(wt.device)
-    with _ordered(stream, wt.device):
-        rows = MX.empty_rows(wt.shape[0], wt.shape[1], MX.LORA_E2M1, wt.device)
-    MX.lora_mx_quantize(wt, wt.stride(0) if wt.shape[0] > 1 else wt.shape[1], code, rows, stream)
+    rows = MX.empty_rows(wt.shape[0], wt.shape[1], MX.LORA_E2M1, wt.device)
+    MX.lora_mx_quantize(wt, wt.stride(0) if wt.shape[0] > 1 else wt.shape[1], code, rows, torch.cuda.current_stream(wt.device))
     return rows
 
 
@@ -474,7 +479,7 @@ def main() -> None:
         n_vocab, max_new = 32000, 100
         layers, kept = random_layers(n_layers, hidden, heads, kv_heads, dim, dt, [8, 16, 32, 64], dev, 1, st, in_blocks=True)
         embed = torch.randn((n_vocab, hidden), device=dev).to(dt)
-        head = Head(torch.ones(hidden, device=dev, dtype=dt), in_4_bits((torch.randn_like(embed) * hidden ** -0.5).to(dt), st))
+        head = Head(torch.ones(hidden, device=dev, dtype=dt), in_4_bits((torch.randn_like(embed) * hidden ** -0.5).to(dt)))
         prompts = [203, 512, 64, 1000, 17, 300, 128, 700] * 3
         shape = (n_layers, sum((p + max_new + 16) // 16 + 1 for p in prompts), kv_heads, 16, dim)
         cache = KV.Cache(torch.zeros(shape, dtype=dt, device=dev), torch.zeros(shape, dtype=dt, device=dev))

@@ -58,7 +58,7 @@ class Stack:
         gen = torch.Generator().manual_seed(9)
         self.embed = torch.randn((VOCAB, HIDDEN), generator=gen).to(dt).to(DEV)
         out = (torch.randn((VOCAB, HIDDEN), generator=gen) * 0.2).to(dt).to(DEV)
-        self.head = T.Head((1 + 0.1 * torch.randn(HIDDEN, generator=gen)).to(dt).to(DEV), T.in_4_bits(out, self.st))
+        self.head = T.Head((1 + 0.1 * torch.randn(HIDDEN, generator=gen)).to(dt).to(DEV), T.in_4_bits(out), VOCAB - 5)
         nan = float("nan")
         self.cache = KV.Cache(*(torch.full((LAYERS, 60, KV_HEADS, 16, DIM), nan, dtype=dt, device=DEV) for _ in range(2)))
         self.srv = T.Server(self.cache, N_SEQS, MAX_LEN, self.st)
@@ -167,7 +167,7 @@ class Stack:
             if not seg_lens[s]:
                 assert tokens[s].item() == -1 and probs[s].item() == 0
                 continue
-            token, own, total = R.sample(logits[s], t[s], int(k[s]), p[s], m[s], np.float32(u[s].item()))
+            token, own, total = R.sample(logits[s][:VOCAB - 5], t[s], int(k[s]), p[s], m[s], np.float32(u[s].item()))
             assert tokens[s].item() == token
             assert abs(probs[s].item() - own / total) <= own / total * (2.0 ** -24 + 2.0 ** -50)
 
@@ -275,6 +275,9 @@ def test_weights_in_blocks_without_norms_and_beside_others():
             T.Step(s.layers, s.cache, seg_lens, ADAPTERS, HEADS, 0, 0, s.st, T.Head(s.head.norm, blocks.o.wt))
         for p in (plain[0].q, plain[0].k, plain[0].v, plain[0].o):
             L.lora_release_adapters(p.table)
+        for n in (-8, VOCAB + 1):             # tokens that the weight has not
+            with pytest.raises(ValueError):
+                T.Head(s.head.norm, s.head.wt, n)
         empty = s.step([0] * N_SEQS)          # a step without rows
         s.grow([0] * N_SEQS)
         y = torch.empty((0, HIDDEN), dtype=s.dt, device=DEV)
@@ -283,4 +286,40 @@ def test_weights_in_blocks_without_norms_and_beside_others():
         empty.choose(y, None, torch.zeros(N_SEQS, device=DEV), tokens, None, s.st)
         assert tokens.tolist() == [-1] * N_SEQS
     finally:
+        s.close()
+
+
+def test_norms_in_front_of_16_bit_weights():
+    """The stages are the calls by themselves, bit for bit."""
+    s = Stack(torch.bfloat16)
+    plain, kept = T.random_layers(2, HIDDEN, HEADS, KV_HEADS, DIM, s.dt, RANKS, DEV, 6, s.st)
+    seg_lens, steps = [3, 0, 2, 1, 4], []
+    try:
+        layers = [T.Layer(p.q, p.k, p.v, p.o, b.norm) for p, b in zip(plain, s.layers)]
+        step = T.Step(layers, s.cache, seg_lens, ADAPTERS, HEADS, 0, 0, s.st, s.head, EPS)
+        bare = T.Step(plain, s.cache, seg_lens, ADAPTERS, HEADS, 0, 0, s.st)
+        steps += [step, bare]
+        n = sum(seg_lens)
+        x = s.embed[:n].contiguous()
+        s.grow(seg_lens)
+        y, want = torch.empty_like(x), torch.empty_like(x)
+        step.run(s.srv.attn, s.srv.seqs, x, y, s.st)
+        total, h, src = torch.empty_like(x), torch.empty_like(x), x
+        for i in range(2):
+            MX.lora_norm(src, HIDDEN, total if i else None, HIDDEN, layers[i].norm, EPS, n, HIDDEN, L.LORA_BF16, total, HIDDEN,
+                         h, HIDDEN, None, s.st)
+            bare.project(i, h, s.st)
+            bare.attend(s.srv.attn, i, s.srv.seqs, want, s.st)
+            src = want
+        assert torch.equal(y, want) and torch.equal(step.total, total) and torch.equal(step.h, h)
+        tokens, probs = torch.zeros(N_SEQS, dtype=torch.int32, device=DEV), torch.zeros(N_SEQS, device=DEV)
+        step.choose(y, None, torch.zeros(N_SEQS, device=DEV), tokens, probs, s.st)
+        assert tokens[1] == -1 and (tokens[[0, 2, 3, 4]] >= 0).all() and (probs[[0, 2, 3, 4]] > 0).all()
+    finally:
+        torch.cuda.synchronize()
+        for t in steps:
+            t.release()
+        for layer in plain:
+            for p in (layer.q, layer.k, layer.v, layer.o):
+                L.lora_release_adapters(p.table)
         s.close()
