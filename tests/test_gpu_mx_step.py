@@ -323,3 +323,34 @@ def test_norms_in_front_of_16_bit_weights():
             for p in (layer.q, layer.k, layer.v, layer.o):
                 L.lora_release_adapters(p.table)
         s.close()
+
+
+def test_layers_of_other_ranks():
+    """q, k and v share a launch where their adapters agree in rank, layers a plan where theirs do; every
+    delta is its own table's either way."""
+    s = Stack(torch.float16)
+    others, kept = T.random_layers(2, HIDDEN, HEADS, KV_HEADS, DIM, s.dt, [7, 24, 40], DEV, 6, s.st, in_blocks=True)
+    seg_lens, step = [3, 0, 2, 1, 4], None
+    try:
+        a, b = s.layers[0], others[0]
+        mixed = T.Layer(a.q, b.k, a.v, b.o, a.norm)
+        layers = [a, b, s.layers[1], others[1], mixed]
+        cache = KV.Cache(*(torch.zeros((5, 60, KV_HEADS, 16, DIM), dtype=s.dt, device=DEV) for _ in range(2)))
+        step = T.Step(layers, cache, seg_lens, ADAPTERS, HEADS, 0, 0, s.st)
+        # a plan of three and one for o for either ranks; q, k and v of the mixed layer on their own (k and v are of one shape)
+        assert len(step._plans) == 4 + 3
+        x = s.embed[:sum(seg_lens)].contiguous()
+        s.kept = [s.kept[0], s.kept[1], s.kept[2], s.kept[3], *kept[:4], *s.kept[4:], *kept[4:], s.kept[0], kept[1], s.kept[2], kept[3]]
+        for i, layer in enumerate(layers):
+            step.project(i, x, s.st)
+            torch.cuda.synchronize()
+            for name, got in (("q", step.q), ("k", step.k), ("v", step.v)):
+                s.check_projection(name, i, getattr(layer, name), seg_lens, step.h, step._rows["hq", HIDDEN], got)
+    finally:
+        torch.cuda.synchronize()
+        if step:
+            step.release()
+        for layer in others:
+            for p in (layer.q, layer.k, layer.v, layer.o):
+                L.lora_release_adapters(p.table)
+        s.close()
