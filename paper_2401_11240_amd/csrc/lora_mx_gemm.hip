@@ -590,7 +590,7 @@ int check_product(const lora_mx_t* x, const lora_mx_t* w) {
     if (w->n_rows < 8 || w->n_rows % 8) return set_error(LORA_E_SHAPE, "w: n_rows must be a positive multiple of 8");
     for (const lora_mx_t* q : {x, w})
         if (std::max(q->ld_codes, q->ld_scales) * kTileSpan > (int64_t)kMaxSpan)
-            return set_error(LORA_E_SHAPE, "256 rows of x or w span more than 2 GiB");
+            return set_error(LORA_E_SHAPE, "256 rows of x or w span more than 0x7fff0000 bytes");
     return LORA_OK;
 }
 

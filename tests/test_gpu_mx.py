@@ -420,3 +420,107 @@ def test_calls_allocate_nothing():
     torch.cuda.synchronize()
     assert torch.cuda.mem_get_info(DEV)[0] == free
     assert L.lora_abi_version() == 4
+
+
+# -- offsets past 32 bits ------------------------------------------------------
+
+def far(rows, width, ld, dtype):
+    """Rows `ld` elements apart in memory that is not touched between them."""
+    buf = torch.empty((rows - 1) * ld + width, dtype=dtype, device=DEV)
+    return buf.as_strided((rows, width), (ld, 1))
+
+
+def test_rows_more_than_4_gib_apart():
+    rng = np.random.default_rng(20)
+    h, ld = 264, (1 << 31) + 24
+    x, r, t, y = (far(2, h, ld, torch.bfloat16) for _ in range(4))
+    for m in (x, r):
+        m.copy_(torch.from_numpy(rng.standard_normal((2, h))).to(DEV))
+    q = MX.Rows(far(2, MX.code_bytes(h, R.E4M3), (1 << 32) + 32, torch.uint8), far(2, MX.scale_bytes(h), (1 << 32) + 12, torch.uint8),
+                R.E4M3, h)
+    near = lambda: torch.empty((2, h), dtype=torch.bfloat16, device=DEV)  # noqa: E731
+    xn, rn, tn, yn, qn = x.contiguous(), r.contiguous(), near(), near(), rows_of(2, h, R.E4M3)
+    MX.lora_norm(x, ld, r, ld, None, 1e-5, 2, h, R.BF16, t, ld, y, ld, q, stream())
+    MX.lora_norm(xn, h, rn, h, None, 1e-5, 2, h, R.BF16, tn, h, yn, h, qn, stream())
+    assert torch.equal(t, tn) and torch.equal(y, yn)
+    n = R.blocks(h)
+    assert torch.equal(q.codes, qn.codes) and torch.equal(q.scales[:, :n], qn.scales[:, :n])
+    MX.lora_mx_quantize(x, ld, R.BF16, q, stream())
+    MX.lora_mx_quantize(xn, h, R.BF16, qn, stream())
+    assert torch.equal(q.codes, qn.codes) and torch.equal(q.scales[:, :n], qn.scales[:, :n])
+    MX.lora_mx_dequantize(q, y, ld, R.BF16, stream())
+    MX.lora_mx_dequantize(qn, yn, h, R.BF16, stream())
+    assert torch.equal(y, yn)
+
+
+@pytest.mark.parametrize("rows,h_out,far_of", [(600, 40, "x"), (20, 8712, "w"), (600, 520, "x"), (300, 8712, "w"), (2, 40, "y"), (70, 264, "y")])
+def test_products_over_more_than_4_gib(rows, h_out, far_of):
+    """Rows of x or w 8 MiB or 512 KiB apart (256 of them within 0x7fff0000 bytes, as the call asks), rows of y far apart: the bits of the
+    call on dense rows."""
+    rng = np.random.default_rng([21, rows, h_out])
+    h = 264
+    x, w = random_rows(rng, rows, h, R.E4M3), random_rows(rng, h_out, h, R.E2M1)
+    want = apply(x, w, R.F16)
+
+    def spread(q, ld):
+        f = MX.Rows(far(q.n_rows, q.codes.shape[1], ld, torch.uint8), q.scales, q.fmt, h)
+        f.codes.copy_(q.codes)
+        return f
+
+    if far_of == "x":
+        x = spread(x, (1 << 23) - 256)
+    if far_of == "w":
+        w = spread(w, 1 << 19)
+    assert far_of == "y" or (x if far_of == "x" else w).codes.stride(0) * (rows if far_of == "x" else h_out) > 1 << 32
+    y = far(rows, h_out, (1 << 32) // rows + 8 & ~7, torch.float16) if far_of == "y" else torch.empty((rows, h_out), dtype=torch.float16, device=DEV)
+    n = MX.lora_mx_workspace_bytes(x, w)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    MX.lora_mx_apply(x, w, y, y.stride(0), R.F16, ws, n, stream())
+    assert torch.equal(y, want)
+
+
+def test_more_rows_than_a_launch_has():
+    """The norm's rows past 2^20 and the blocks' chunks past 2^30 go to launches of their own."""
+    rng = np.random.default_rng(22)
+    rows, h = (1 << 20) + 37, 8
+    gen = torch.Generator(device=DEV).manual_seed(22)
+    x, r = (torch.randn((rows, h), generator=gen, device=DEV).half() for _ in range(2))
+    t, y, q = torch.empty_like(x), torch.empty_like(x), rows_of(rows, h, R.E4M3)
+    MX.lora_norm(x, h, r, h, None, 1e-5, rows, h, R.F16, t, h, y, h, q, stream())
+    for at in (slice(0, 100), slice((1 << 20) - 50, rows)):
+        n = at.stop - at.start
+        ts, ys, qs = torch.empty((n, h), dtype=torch.float16, device=DEV), torch.empty((n, h), dtype=torch.float16, device=DEV), rows_of(n, h, R.E4M3)
+        MX.lora_norm(x[at], h, r[at], h, None, 1e-5, n, h, R.F16, ts, h, ys, h, qs, stream())
+        assert torch.equal(t[at], ts) and torch.equal(y[at], ys)
+        assert torch.equal(q.codes[at], qs.codes) and torch.equal(q.scales[at, :1], qs.scales[:, :1])
+    del x, r, t, y, q
+    rows, h = (1 << 22) + 3, 2048
+    x, q = torch.empty((rows, h), dtype=torch.float16, device=DEV), rows_of(rows, h, R.E2M1)
+    at = torch.tensor([0, 1, (1 << 22) - 1, 1 << 22, rows - 1], device=DEV)
+    v = torch.from_numpy(rng.standard_normal((len(at), h))).to(DEV).half()
+    x[at] = v
+    MX.lora_mx_quantize(x, h, R.F16, q, stream())
+    codes, scales = R.quantize(f64(v), R.E2M1)
+    assert np.array_equal(q.codes[at].cpu().numpy(), codes) and np.array_equal(q.scales[at].cpu().numpy(), scales)
+    x.zero_()
+    MX.lora_mx_dequantize(q, x, h, R.F16, stream())
+    assert np.array_equal(f64(x[at]), R.values(codes, scales, R.E2M1, h))
+
+
+def test_two_streams_at_once():
+    """Calls with workspaces of their own do not disturb each other."""
+    rng = np.random.default_rng(23)
+    jobs = []
+    for rows, h, h_out in ((24, 8192, 128), (300, 1032, 264)):
+        x, w = random_rows(rng, rows, h, R.E4M3), random_rows(rng, h_out, h, R.E2M1)
+        n = MX.lora_mx_workspace_bytes(x, w)
+        jobs.append((x, w, torch.empty(n, dtype=torch.uint8, device=DEV), apply(x, w, R.F32, 0), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    ys = [[torch.empty((j[0].n_rows, j[1].n_rows), device=DEV) for _ in range(20)] for j in jobs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for (x, w, ws, _, st), y in zip(jobs, ys):
+            MX.lora_mx_apply(x, w, y[i], w.n_rows, R.F32, ws, ws.numel(), st)
+    torch.cuda.synchronize()
+    for (_, _, _, want, _), y in zip(jobs, ys):
+        assert all(torch.equal(a, want) for a in y)

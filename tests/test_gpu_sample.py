@@ -222,3 +222,30 @@ def test_no_rows():
     z = torch.zeros((0, 100), device=DEV)
     tokens, probs = choose(z, None, np.zeros(0), R.F32)
     assert tokens.size == 0
+
+
+@pytest.mark.parametrize("v", [700, 40000])
+def test_rows_more_than_4_gib_apart(v):
+    rng = np.random.default_rng([9, v])
+    ld = (1 << 32) + 3
+    z = torch.empty(ld + v, dtype=torch.float16, device=DEV).as_strided((2, v), (ld, 1))
+    z.copy_(logits(rng, 2, v, R.F16))
+    check(z, *mixed(rng, 2, v), rng.random(2).astype(np.float32), R.F16)
+
+
+def test_more_rows_than_a_launch_has():
+    """Rows past 2^20 go to launches of their own."""
+    rows, v = (1 << 20) + 37, 9
+    rng = np.random.default_rng(10)
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    z = torch.randn((rows, v), generator=gen, device=DEV).half()
+    t, k, p, m = mixed(rng, rows, v)
+    u = rng.random(rows).astype(np.float32)
+    params = SA.Params(device(t, np.float32), device(k, np.int32), device(p, np.float32), device(m, np.float32))
+    tokens, probs = choose(z, params, u, R.F16)
+    at = np.concatenate([np.arange(300), np.arange((1 << 20) - 50, rows)])
+    zz = z[torch.from_numpy(at).to(DEV)].double().cpu().numpy()
+    for i, r in enumerate(at):
+        want, own, total = R.sample(zz[i], t[r], int(k[r]), p[r], m[r], u[r])
+        assert tokens[r] == want, r
+        assert abs(probs[r] - own / total) <= own / total * (2.0 ** -24 + 2.0 ** -50), r
