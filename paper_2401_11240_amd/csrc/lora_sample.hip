@@ -28,6 +28,7 @@
 #include <cmath>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lora_device.h"
 #include "lora_mx_internal.h"
@@ -110,6 +111,21 @@ __device__ __forceinline__ uint64_t weight(float l, float top, double lmax, doub
 
 __device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return __shfl_up((unsigned long long)v, d, 64); }
 __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) { return __shfl_xor((unsigned long long)v, d, 64); }
+
+// Sums over the four lanes of a quad, in all four.
+__device__ __forceinline__ int quad_sum(int v) {
+    v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);        // lanes 1 0 3 2
+    return v + __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);  // lanes 2 3 0 1
+}
+__device__ __forceinline__ uint64_t quad_sum(uint64_t v) {
+    auto moved = [](uint64_t x, auto dpp) __attribute__((always_inline)) {
+        const int lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)x, decltype(dpp)::value, 0xf, 0xf, true);
+        const int hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(x >> 32), decltype(dpp)::value, 0xf, 0xf, true);
+        return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
+    };
+    v += moved(v, std::integral_constant<int, 0xB1>{});
+    return v + moved(v, std::integral_constant<int, 0x4E>{});
+}
 
 // What the filters leave open (step 2).
 struct Cut {                               // (read as whole words)
@@ -637,6 +653,24 @@ __device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) 
     return before + s - x;
 }
 
+// How many of list[0 .. n) are larger than `mine`, and their weights' sum, by the quad that holds `mine` (0 for none).
+__device__ __forceinline__ void rank_among(const uint64_t* list, const uint64_t* weights, int n, uint64_t mine, int& rank,
+                                           uint64_t& before) {
+    rank = 0;
+    before = 0;
+    if (mine) {
+#pragma unroll 4
+        for (int i = threadIdx.x & 3; i < n; i += 4) {
+            const bool larger = list[i] > mine;
+            const uint64_t w = weights[i];
+            rank += larger;
+            before += larger ? w : 0;
+        }
+    }
+    rank = quad_sum(rank);
+    before = quad_sum(before);
+}
+
 // What top_k and top_p keep of a list (n logits, 4 entries a thread in `mine`): ranked() of the last.  A finer histogram
 // of the list's bins leads to the one bin in which each of the two ends, whose few logits are compared with one another.
 // False if they are not few.
@@ -658,7 +692,8 @@ __device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut,
         }
     }
     __syncthreads();
-    // a bin's logits, one a thread, with their rank in it and the weights in front of them in it; false if too many
+    // a bin's logits, one a quad (and in its first lane), with their rank in it and the weights in front of them in it;
+    // false if too many
     uint64_t own = 0, weight = 0, before = 0;
     int rank = 0;
     auto compare = [&](int bin) __attribute__((always_inline)) {
@@ -671,18 +706,12 @@ __device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut,
         for (int j = 0; j < kEach; ++j)
             if (fine[j] == bin) sh.hist[atomicAdd(&sh.digit, 1u)] = mine[j];
         __syncthreads();
-        own = t < m ? sh.hist[t] : 0;
-        weight = t < m ? R.weight_of(logit_of((uint32_t)(own >> 32)), sh.frac) : 0;
-        if (t < m) sh.weights[t] = weight;
+        own = t >> 2 < m ? sh.hist[t >> 2] : 0;
+        weight = own ? R.weight_of(logit_of((uint32_t)(own >> 32)), sh.frac) : 0;
+        if (own) sh.weights[t >> 2] = weight;
         __syncthreads();
-        rank = 0;
-        before = 0;
-        if (t < m)
-            for (int i = 0; i < m; ++i) {
-                const bool larger = sh.hist[i] > own;
-                rank += larger;
-                before += larger ? sh.weights[i] : 0;
-            }
+        rank_among((const uint64_t*)sh.hist, sh.weights, m, own, rank, before);
+        if (t & 3) own = 0;
         return true;
     };
     last = 0;
@@ -780,21 +809,17 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
     const int most = cut.k_cuts ? min(R.k, n) : n;
     uint64_t all, last = 0;                // last: the last that top_k and top_p keep
     if (n <= kRanked) {
-        // one entry a thread: its rank and the weights in front of it, from a comparison with every other
-        const uint64_t mine = t < n ? sh.list[t] : 0;
-        uint64_t w = t < n ? weight_at(mine) : 0;
+        // one entry a quad: its rank and the weights in front of it, from a comparison with every other, which the four
+        // lanes share; from then on it is the first lane's
+        const uint64_t mine = t >> 2 < n ? sh.list[t >> 2] : 0;
+        uint64_t w = mine ? weight_at(mine) : 0;
         if (cuts) {
-            if (t < kRanked) sh.weights[t] = w;
+            if (mine) sh.weights[t >> 2] = w;
             __syncthreads();
-            uint64_t before = 0;
-            int rank = 0;
-            if (t < n)
-                for (int i = 0; i < n; ++i) {
-                    const bool larger = sh.list[i] > mine;
-                    rank += larger;
-                    before += larger ? sh.weights[i] : 0;
-                }
-            bool in = t < n && rank < most;
+            uint64_t before;
+            int rank;
+            rank_among(sh.list, sh.weights, n, mine, rank, before);
+            bool in = mine && (t & 3) == 0 && rank < most;
             if (R.has_p) {
                 all = cut.all;
                 if (cut.k_cuts) scan(sh, in ? w : 0, all);
@@ -811,7 +836,7 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
                 last = sh.part[1];
             }
         }
-        w = R.kept(w);
+        w = (t & 3) == 0 ? R.kept(w) : 0;
         if (cut.lo == 0) {
             const uint64_t run = scan(sh, w, all), target = R.target(all);
             if (w && run <= target && target < run + w) R.choose(a, index_of(mine), w, all);
@@ -916,9 +941,20 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
         for (int q = 0; q < kPer; ++q)
             if (l + 64 * q < of) sh.list[to + l + 64 * q] = r[q];
     } else {
-        for (int g = w; g < segs; g += kWaves) {
+        // the first 64 of all of the wave's parts at once, more where there are
+        uint64_t r[kMaxSlices];
+#pragma unroll
+        for (int j = 0; j < kMaxSlices; ++j) {
+            const int g = w + kWaves * j;
+            r[j] = g < segs && l < (int)sh.seg_n[g] ? from[(int64_t)g * kWaveList + l] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kMaxSlices; ++j) {
+            const int g = w + kWaves * j;
+            if (g >= segs) break;
             const int of = (int)sh.seg_n[g], to = (int)sh.segs[g];
-            for (int i = l; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
+            if (l < of) sh.list[to + l] = r[j];
+            for (int i = l + 64; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
         }
     }
     __syncthreads();
@@ -961,6 +997,7 @@ struct RowSpace {
     }
     static int64_t bytes(int slices) { return kHead + slices * kSlice; }
 };
+static_assert(4 * kRanked == kSampleThreads, "a quad for each of a ranked list");
 static_assert((sizeof(Cut) & (sizeof(Cut) - 1)) == 0 && sizeof(Cut) <= 64 && RowSpace::kHead % 16 == 0 && RowSpace::kSlice % 16 == 0, "rows' workspaces");
 
 template <int DT>
@@ -1126,7 +1163,7 @@ struct SamplePlan {
     int slices, seg;
 };
 
-// One launch and a workgroup a row from 256 rows on, or where a row is short; slices of 4096 logits at least, as many as
+// One launch and a workgroup a row from 129 rows on, or where a row is short; slices of 4096 logits at least, as many as
 // give every compute unit a workgroup, otherwise.  Measured, one launch against 2, 4 and 8 slices: 256 rows of
 // 50257 with top_k 29 us against 44, 53, 67, with top_p alone 76 against 89, 101, 113; 64 rows of 128000, all kinds, 127
 // against 88, 64, 63; 16 rows of 32000 without filters 34 against 30, 25, 24; one row of 32000 33 against 32, 28, 27.

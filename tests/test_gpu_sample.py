@@ -114,6 +114,19 @@ def test_equal_logits_go_to_the_lowest_indices(v, dtype):
 
 
 @dtypes
+@pytest.mark.parametrize("scale", [0.02, 0.3, 3.0])
+@pytest.mark.parametrize("v", [5000, 40000])
+def test_filters_that_end_among_many(v, scale, dtype):
+    """Few, hundreds and thousands of logits before and at the places where top_k and top_p end."""
+    rng = np.random.default_rng([4, v, int(100 * scale), dtype])
+    k = np.array([0, 2, 64, 255, 256, 257, 511, 512, 513, 1000, 2500, 4000] * 3, np.int32)
+    p = np.repeat(np.array([1, 0.9, 0.03], np.float32), 12)
+    m = np.where(np.arange(36) % 5 == 0, 0.6, 0).astype(np.float32)
+    z = torch.from_numpy(rng.standard_normal((36, v)) * scale).to(DEV).to(TYPE[dtype])
+    check(z, np.ones(36, np.float32), k, p, m, rng.random(36).astype(np.float32), dtype)
+
+
+@dtypes
 @pytest.mark.parametrize("v", [9, 3000, 90000])
 def test_masked_infinite_and_nan_logits(v, dtype):
     rng = np.random.default_rng([4, v])
