@@ -28,7 +28,6 @@
 #include <cmath>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "lora_device.h"
 #include "lora_mx_internal.h"
@@ -109,22 +108,43 @@ __device__ __forceinline__ uint64_t weight(float l, float top, double lmax, doub
     return l == top ? 1ull << kWeightBits : some ? w : 0;
 }
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return __shfl_up((unsigned long long)v, d, 64); }
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int d) { return __shfl_xor((unsigned long long)v, d, 64); }
-
-// Sums over the four lanes of a quad, in all four.
-__device__ __forceinline__ int quad_sum(int v) {
-    v += __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);        // lanes 1 0 3 2
-    return v + __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);  // lanes 2 3 0 1
+// The value of the lane that the DPP control names, in the rows of ROWS; 0 elsewhere and where there is none.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ uint64_t quad_sum(uint64_t v) {
-    auto moved = [](uint64_t x, auto dpp) __attribute__((always_inline)) {
-        const int lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)x, decltype(dpp)::value, 0xf, 0xf, true);
-        const int hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(x >> 32), decltype(dpp)::value, 0xf, 0xf, true);
-        return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
-    };
-    v += moved(v, std::integral_constant<int, 0xB1>{});
-    return v + moved(v, std::integral_constant<int, 0x4E>{});
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t moved(uint64_t v) {
+    return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v);
+}
+// Sums over the four lanes of a quad, in all four.
+template <class T>
+__device__ __forceinline__ T quad_sum(T v) {
+    v += moved<0xB1>(v);                   // lanes 1 0 3 2
+    return v + moved<0x4E>(v);             // lanes 2 3 0 1
+}
+// f over the lanes up to and with each of a wave's 64, all of them active (0 must change nothing): over 1, 2, 4 and 8 lanes
+// of a row of 16, then the rows' ends into the rows behind them.
+template <class T, class F>
+__device__ __forceinline__ T wave_scan(T v, const F& f) {
+    v = f(v, moved<0x111>(v));             // 1 lane down
+    v = f(v, moved<0x112>(v));
+    v = f(v, moved<0x114>(v));
+    v = f(v, moved<0x118>(v));
+    v = f(v, moved<0x142, 0xa>(v));        // a row's last lane to rows 1 and 3
+    return f(v, moved<0x143, 0xc>(v));     // lane 31 to rows 2 and 3
+}
+template <class T>
+__device__ __forceinline__ T wave_sums(T v) {
+    return wave_scan(v, [](T a, T b) { return a + b; });
+}
+// The last lane's value, in every lane.
+__device__ __forceinline__ uint32_t of_last(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint64_t of_last(uint64_t v) { return (uint64_t)of_last((uint32_t)(v >> 32)) << 32 | of_last((uint32_t)v); }
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) { return of_last(wave_sums(v)); }
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+    return of_last(wave_scan(v, [](uint64_t a, uint64_t b) { return max(a, b); }));
 }
 
 // What the filters leave open (step 2).
@@ -147,14 +167,14 @@ struct Shared {
     double frac[64];
     uint64_t part[kWaves], parts[kWaves], ties[kWaves];
     uint64_t above;
+    int found[2];
     uint32_t digit;
     Cut cut;
 };
 
 // Sum over the workgroup, in every thread.
 __device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared& sh) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += shfl_xor64(v, d);
+    v = wave_sum(v);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -171,12 +191,7 @@ __device__ __forceinline__ void find_digit(uint64_t above, double limit, Shared&
     // thread t: digits kDigits - 1 - 2 t and the one below, falling
     const int d0 = kDigits - 1 - 2 * t;
     const uint64_t a = sh.hist[d0], b = sh.hist[d0 - 1];
-    uint64_t s = a + b;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = shfl_up64(s, d);
-        if (l >= d) s += o;
-    }
+    const uint64_t s = wave_sums(a + b);
     if (l == 63) sh.parts[w] = s;
     if (t == 0) sh.digit = kDigits;
     __syncthreads();
@@ -330,11 +345,8 @@ __device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shar
         if (key > tkey) sum += R.kept(weight_at(key));
         else if (key == tkey) ++ties;
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-        sum += shfl_xor64(sum, d);
-        ties += shfl_xor64(ties, d);
-    }
+    sum = wave_sum(sum);
+    ties = wave_sum(ties);
     __syncthreads();
     if (l == 0) {
         sh.parts[w] = sum;
@@ -358,15 +370,10 @@ __device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shar
         const bool tie = key == tkey && key > kKeyNone;
         const uint64_t ballot = __ballot(tie);
         const uint64_t rank = ties_before + __popcll(ballot & ((1ull << l) - 1));
-        uint64_t v = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
-        const uint64_t own = v;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t o = shfl_up64(v, d);
-            if (l >= d) v += o;
-        }
+        const uint64_t own = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
+        const uint64_t v = wave_sums(own);
         if (own && at + v > target && at + v - own <= target) R.choose(a, i + l, own, total);
-        at += __shfl((unsigned long long)v, 63, 64);
+        at += of_last(v);
         ties_before += __popcll(ballot);
         if (at > target) break;
     }
@@ -438,9 +445,7 @@ __device__ __forceinline__ uint64_t best_of(const SampleArgs& a, const Row& R, S
         }
     });
     most = top;
-    uint64_t b = ranked(top, at);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) b = max(b, shfl_xor64(b, d));
+    uint64_t b = wave_max(ranked(top, at));
     if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = b;
     __syncthreads();
 #pragma unroll
@@ -482,98 +487,88 @@ __device__ __forceinline__ void fill_bins(const SampleArgs& a, const Row& R, Sha
     __syncthreads();
 }
 
-// Running sums of the histogram in sh.count and sh.mass, by one wave, 8 bins a lane.
+// The histogram in sh.count and sh.mass into its running sums, a bin a thread: up to and with the thread's bin, and
+// in front of it.  Whole workgroup.
 struct BinSums {
-    static constexpr int kPer = kBins / 64;
-    uint64_t c[kPer], m[kPer], all;        // up to and with each bin; all: of the weights
-    __device__ __forceinline__ BinSums(const Shared& sh) {
-        const int l = threadIdx.x & 63;
-        uint64_t cs = 0, ms = 0;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            cs += sh.count[kPer * l + j];
-            ms += sh.mass[kPer * l + j];
-            c[j] = cs;
-            m[j] = ms;
+    uint32_t c, c0;
+    uint64_t m, m0;
+    __device__ __forceinline__ BinSums(Shared& sh) {
+        const int t = threadIdx.x, w = t >> 6;
+        c0 = sh.count[t];
+        m0 = sh.mass[t];
+        c = wave_sums(c0);
+        m = wave_sums(m0);
+        if ((t & 63) == 63) {
+            sh.ties[w] = c;
+            sh.parts[w] = m;
         }
-        uint64_t co = cs, mo = ms;
+        if (t < 2) sh.found[t] = kBins - 1;
+        __syncthreads();
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t oc = shfl_up64(co, d), om = shfl_up64(mo, d);
-            if (l >= d) {
-                co += oc;
-                mo += om;
+        for (int i = 0; i < kWaves - 1; ++i)
+            if (i < w) {
+                c += (uint32_t)sh.ties[i];
+                m += sh.parts[i];
             }
-        }
-        all = __shfl((unsigned long long)mo, 63, 64);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            c[j] += co - cs;
-            m[j] += mo - ms;
-        }
+        sh.count[t] = c;
+        sh.mass[t] = m;
+        c0 = c - c0;
+        m0 = m - m0;
+        __syncthreads();
     }
-    // the first bin whose running sum satisfies `ok`, or the last bin; a running sum at a bin (0 in front of the first)
+    // the first bin at which `ok` of the running sums holds (it holds from there on, and not of 0 and 0), or the last
+    // bin; `i` is 0 or 1, once each
     template <class Ok>
-    __device__ __forceinline__ int first(const Ok& ok) const {
-        int b = kBins;
-#pragma unroll
-        for (int j = kPer - 1; j >= 0; --j) b = ok(j) ? kPer * (int)(threadIdx.x & 63) + j : b;
-        const uint64_t has = __ballot(b < kBins);
-        return has ? min(__shfl(b, __ffsll((unsigned long long)has) - 1, 64), kBins - 1) : kBins - 1;
-    }
-    static __device__ __forceinline__ uint64_t at(const uint64_t (&x)[kPer], int b) {
-        uint64_t v = 0;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) v = j == (b & (kPer - 1)) ? x[j] : v;
-        v = __shfl((unsigned long long)v, max(b, 0) / kPer, 64);
-        return b < 0 ? 0 : v;
+    __device__ __forceinline__ int first(Shared& sh, int i, const Ok& ok) const {
+        if (ok(c, m) && !ok(c0, m0)) sh.found[i] = threadIdx.x;
+        __syncthreads();
+        return sh.found[i];
     }
 };
+static_assert(kBins == kSampleThreads, "a bin a thread");
+template <class T>
+__device__ __forceinline__ T up_to(const T* sums, int b) { return b < 0 ? 0 : sums[b]; }
 
 // Step 2's decision from the row's histogram in sh.count and sh.mass, into sh.cut.
 __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
-    const int l = threadIdx.x;
-    if (l < 64) {
-        const BinSums S(sh);
-        const uint64_t all = S.all;
-        // the bin of the top_k-th logit, and the weights up to it, which K's are not above
-        const bool small = R.small_k();
-        const int kb = R.has_k ? S.first([&](int j) { return S.c[j] >= (uint64_t)R.k; }) : kBins - 1;
-        const bool k_cuts = R.has_k && (small || kb < kBins - 1);
-        // the last bin that begins below top_p's limit (or, with K's sum smaller, later than that)
-        int pb = kBins - 2;
-        const bool by_p = R.has_p && R.p > 0.f && !small;
-        if (R.has_p && !(R.p > 0.f)) pb = 0;
-        if (by_p) {
-            const double limit = (double)R.p * (double)(kb < kBins - 1 ? S.at(S.m, kb) : all);
-            pb = min(pb, S.first([&](int j) { return (double)S.m[j] >= limit; }));
-        }
-        // the last bin with a logit that min_p keeps, with some to spare for the roundings (weights of a few units
-        // are rounded by up to ln 2)
-        int m1 = kBins - 2;
-        if (R.least > 0) {
-            const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
-            const int spare = R.least < 256 ? kBinsPerNat * 3 / 4 : 2;
-            if (f < (float)(kBins - 2)) m1 = min((int)f + spare, kBins - 2);
-        }
-        // (top_p needs the sum over K: all of it is in the list, if the bins do not have the row's)
-        const bool whole_k = R.has_p && R.p > 0.f && k_cuts;
-        const int hi = whole_k ? min(kb, kBins - 2) : min(min(min(kb, pb), m1), kBins - 2);
-        int lo = 0, slow = 0;
-        const uint64_t upto = S.at(S.c, hi);
-        if (!small && upto > (uint64_t)kFits) {        // more than a list: top_p's last bin, if it is among them
-            lo = R.has_p && pb <= hi ? pb : hi + 1;
-            slow = lo == 0 || k_cuts || (lo <= hi && upto - S.at(S.c, lo - 1) > (uint64_t)kFits);
-        }
-        const uint64_t below = S.at(S.m, lo - 1);
-        if (l == 0) {
-            sh.cut.all = k_cuts ? 0 : all;
-            sh.cut.below = below;
-            sh.cut.lo = lo;
-            sh.cut.hi = hi;
-            sh.cut.k_cuts = k_cuts;
-            sh.cut.slow = slow;
-        }
+    const BinSums S(sh);
+    const uint64_t all = sh.mass[kBins - 1];
+    // the bin of the top_k-th logit, and the weights up to it, which K's are not above
+    const bool small = R.small_k();
+    const int kb = R.has_k ? S.first(sh, 0, [&](uint32_t c, uint64_t) { return c >= (uint32_t)R.k; }) : kBins - 1;
+    const bool k_cuts = R.has_k && (small || kb < kBins - 1);
+    // the last bin that begins below top_p's limit (or, with K's sum smaller, later than that)
+    int pb = kBins - 2;
+    const bool by_p = R.has_p && R.p > 0.f && !small;
+    if (R.has_p && !(R.p > 0.f)) pb = 0;
+    if (by_p) {
+        const double limit = (double)R.p * (double)sh.mass[kb];
+        pb = min(pb, S.first(sh, 1, [&](uint32_t, uint64_t m) { return (double)m >= limit; }));
+    }
+    // the last bin with a logit that min_p keeps, with some to spare for the roundings (weights of a few units
+    // are rounded by up to ln 2)
+    int m1 = kBins - 2;
+    if (R.least > 0) {
+        const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
+        const int spare = R.least < 256 ? kBinsPerNat * 3 / 4 : 2;
+        if (f < (float)(kBins - 2)) m1 = min((int)f + spare, kBins - 2);
+    }
+    // (top_p needs the sum over K: all of it is in the list, if the bins do not have the row's)
+    const bool whole_k = R.has_p && R.p > 0.f && k_cuts;
+    const int hi = whole_k ? min(kb, kBins - 2) : min(min(min(kb, pb), m1), kBins - 2);
+    int lo = 0, slow = 0;
+    const uint32_t upto = sh.count[hi];
+    if (!small && upto > (uint32_t)kFits) {            // more than a list: top_p's last bin, if it is among them
+        lo = R.has_p && pb <= hi ? pb : hi + 1;
+        slow = lo == 0 || k_cuts || (lo <= hi && upto - up_to(sh.count, lo - 1) > (uint32_t)kFits);
+    }
+    if (threadIdx.x == 0) {
+        sh.cut.all = k_cuts ? 0 : all;
+        sh.cut.below = up_to(sh.mass, lo - 1);
+        sh.cut.lo = lo;
+        sh.cut.hi = hi;
+        sh.cut.k_cuts = k_cuts;
+        sh.cut.slow = slow;
     }
     __syncthreads();
 }
@@ -582,29 +577,21 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
 // indices, and, where lo is not 0, the sum of weights below it into `sum`.  Their number, which may be more than the room.
 template <int DT>
 __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, Shared& sh, int seg, uint64_t* list, uint64_t& sum) {
-    const int l = threadIdx.x & 63;
     const int lo = sh.cut.lo, hi = sh.cut.hi;
     constexpr int kVec = Vec<DT>::kVec;
     uint32_t n = 0;
     // a lane's logits of one step that are in, bit by bit; lanes in order
     auto add = [&](uint32_t in, const float (&v)[kVec], int i) __attribute__((always_inline)) {
         if (!__any(in)) return;
-        uint32_t at = __popc(in);
-        const uint32_t own = at;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(at, d, 64);
-            if (l >= d) at += o;
-        }
-        const uint32_t all = __shfl(at, 63, 64);
-        at += n - own;
+        const uint32_t own = __popc(in), sums = wave_sums(own);
+        uint32_t at = n + sums - own;
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
             if (in >> e & 1) {
                 if (at < (uint32_t)kWaveList) list[at] = ranked(v[e], i + e);
                 ++at;
             }
-        n += all;
+        n += of_last(sums);
     };
     sum = 0;
     if (lo == 0) {
@@ -625,8 +612,7 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
             }
             add(in, v, i);
         });
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += shfl_xor64(sum, d);
+        sum = wave_sum(sum);
     }
     return n;
 }
@@ -634,12 +620,7 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
 // Running sum in front of x over the workgroup's threads; `all` gets the whole.
 __device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) {
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint64_t s = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = shfl_up64(s, d);
-        if (l >= d) s += o;
-    }
+    const uint64_t s = wave_sums(x);
     __syncthreads();
     if (l == 63) sh.parts[w] = s;
     __syncthreads();
@@ -656,18 +637,18 @@ __device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) 
 // How many of list[0 .. n) are larger than `mine`, and their weights' sum, by the quad that holds `mine` (0 for none).
 __device__ __forceinline__ void rank_among(const uint64_t* list, const uint64_t* weights, int n, uint64_t mine, int& rank,
                                            uint64_t& before) {
-    rank = 0;
+    uint32_t r = 0;
     before = 0;
     if (mine) {
 #pragma unroll 4
         for (int i = threadIdx.x & 3; i < n; i += 4) {
             const bool larger = list[i] > mine;
             const uint64_t w = weights[i];
-            rank += larger;
+            r += larger;
             before += larger ? w : 0;
         }
     }
-    rank = quad_sum(rank);
+    rank = (int)quad_sum(r);
     before = quad_sum(before);
 }
 
@@ -696,9 +677,9 @@ __device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut,
     // false if too many
     uint64_t own = 0, weight = 0, before = 0;
     int rank = 0;
+    const BinSums S(sh);                   // (and the running sums in sh)
     auto compare = [&](int bin) __attribute__((always_inline)) {
-        __syncthreads();
-        const int m = (int)sh.count[bin];
+        const int m = (int)(sh.count[bin] - up_to(sh.count, bin - 1));
         if (m > kRanked) return false;
         if (t == 0) sh.digit = 0;
         __syncthreads();
@@ -717,22 +698,11 @@ __device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut,
     last = 0;
     uint64_t sum = cut.all;
     if (cut.k_cuts) {
-        if (t < 64) {
-            const BinSums S(sh);
-            const int b = S.first([&](int j) { return S.c[j] >= (uint64_t)R.k; });
-            const uint64_t c0 = S.at(S.c, b - 1), m0 = S.at(S.m, b - 1);
-            if (t == 0) {
-                sh.part[0] = (uint64_t)b;
-                sh.part[1] = c0;
-                sh.part[2] = m0;
-                sh.part[3] = S.all;
-            }
-        }
-        __syncthreads();
-        const int b = (int)sh.part[0], c0 = (int)sh.part[1];
-        sum = sh.part[3];
+        sum = sh.mass[kBins - 1];
         if (n > R.k) {
-            const uint64_t m0 = sh.part[2];
+            const int b = S.first(sh, 0, [&](uint32_t c, uint64_t) { return c >= (uint32_t)R.k; });
+            const int c0 = (int)up_to(sh.count, b - 1);
+            const uint64_t m0 = up_to((const uint64_t*)sh.mass, b - 1);
             if (!compare(b)) return false;
             if (own && c0 + rank == R.k - 1) {
                 sh.part[4] = own;
@@ -742,27 +712,15 @@ __device__ __forceinline__ bool select(const Row& R, Shared& sh, const Cut& cut,
             last = sh.part[4];
             sum = sh.part[5];
         }
-        __syncthreads();
     }
     if (R.has_p) {
         const double limit = (double)R.p * (double)sum;
-        if (t < 64) {
-            const BinSums S(sh);
-            const int b = R.p > 0.f ? S.first([&](int j) { return (double)(cut.below + S.m[j]) >= limit; }) : S.first([&](int j) { return S.c[j] > 0; });
-            const uint64_t m0 = S.at(S.m, b - 1);
-            if (t == 0) {
-                sh.part[0] = (uint64_t)b;
-                sh.part[1] = cut.below + m0;
-                sh.part[2] = 0;
-            }
-        }
-        __syncthreads();
-        const int b = (int)sh.part[0];
-        const uint64_t m0 = sh.part[1];
+        const int b = S.first(sh, 1, [&](uint32_t c, uint64_t m) { return R.p > 0.f ? (double)(cut.below + m) >= limit : c > 0; });
+        const uint64_t m0 = cut.below + up_to((const uint64_t*)sh.mass, b - 1);
         if (!compare(b)) return false;
         // the last of the bin that begins below the limit (none: what lies in front of the bin is all)
         const bool in = own && ((double)(m0 + before) < limit || (!(R.p > 0.f) && rank == 0));
-        if (t == 0) sh.digit = 0;
+        if (t == 0) sh.digit = 0, sh.part[2] = 0;
         __syncthreads();
         if (in) atomicMax(&sh.digit, (uint32_t)rank + 1);
         __syncthreads();
@@ -1035,10 +993,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleA
 
 // The row's best of its slices', which lanes hold.
 __device__ __forceinline__ uint64_t largest(uint64_t b, int slices) {
-    if ((threadIdx.x & (kMaxSlices - 1)) >= (unsigned)slices) b = 0;
-#pragma unroll
-    for (int d = kMaxSlices / 2; d >= 1; d >>= 1) b = max(b, shfl_xor64(b, d));
-    return b;
+    return wave_max((threadIdx.x & (kMaxSlices - 1)) < (unsigned)slices ? b : 0);
 }
 
 template <int DT>
@@ -1077,11 +1032,12 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
     const uint64_t bests = ws.best[t & (kMaxSlices - 1)];
     Row R(a, blockIdx.y, DT);
     fill_fractions(sh);
-    // (slices past the last are read as the last again and not counted: all loads at once)
+    // (of four slices at once, those past the last read as the last again and not counted)
     if (R.small_k()) {
-        float most[kMaxSlices];
+        float most[kMaxSlices] = {};
 #pragma unroll
-        for (int j = 0; j < kMaxSlices; ++j) most[j] = ws.most[min(j, a.slices - 1) * kSampleThreads + t];
+        for (int j = 0; j < kMaxSlices; ++j)
+            if ((j & ~3) < a.slices) most[j] = ws.most[min(j, a.slices - 1) * kSampleThreads + t];
         R.set_top(largest(bests, a.slices));
         if (R.done) return;
         clear_bins(sh);
@@ -1095,8 +1051,11 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
         uint64_t m[kMaxSlices];
 #pragma unroll
         for (int j = 0; j < kMaxSlices; ++j) {
-            c[j] = ws.count[min(j, a.slices - 1) * kBins + (t & (kBins - 1))];
-            m[j] = ws.mass[min(j, a.slices - 1) * kBins + (t & (kBins - 1))];
+            c[j] = 0, m[j] = 0;
+            if ((j & ~3) < a.slices) {
+                c[j] = ws.count[min(j, a.slices - 1) * kBins + t];
+                m[j] = ws.mass[min(j, a.slices - 1) * kBins + t];
+            }
         }
         R.set_top(largest(bests, a.slices));
         if (R.done) return;
@@ -1105,10 +1064,8 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
             c[0] += j < a.slices ? c[j] : 0;
             m[0] += j < a.slices ? m[j] : 0;
         }
-        if (t < kBins) {
-            sh.count[t] = c[0];
-            sh.mass[t] = m[0];
-        }
+        sh.count[t] = c[0];
+        sh.mass[t] = m[0];
     }
     __syncthreads();
     decide(R, sh);
