@@ -138,14 +138,29 @@ template <class T>
 __device__ __forceinline__ T wave_sums(T v) {
     return wave_scan(v, [](T a, T b) { return a + b; });
 }
-// The last lane's value, in every lane.
-__device__ __forceinline__ uint32_t of_last(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
-__device__ __forceinline__ uint64_t of_last(uint64_t v) { return (uint64_t)of_last((uint32_t)(v >> 32)) << 32 | of_last((uint32_t)v); }
+// A lane's value, in every lane; l is the same in all.
+__device__ __forceinline__ uint32_t at_lane(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ uint64_t at_lane(uint64_t v, int l) { return (uint64_t)at_lane((uint32_t)(v >> 32), l) << 32 | at_lane((uint32_t)v, l); }
 template <class T>
-__device__ __forceinline__ T wave_sum(T v) { return of_last(wave_sums(v)); }
+__device__ __forceinline__ T wave_sum(T v) { return at_lane(wave_sums(v), 63); }
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-    return of_last(wave_scan(v, [](uint64_t a, uint64_t b) { return max(a, b); }));
+    return at_lane(wave_scan(v, [](uint64_t a, uint64_t b) { return max(a, b); }), 63);
 }
+
+// Of the sums of a workgroup's waves, one behind the other in LDS: what lies in front of this wave's, and their whole.  (By
+// lanes: sixteen conditional additions are four times the code, and a workgroup that runs through code once waits for it.)
+template <class T>
+__device__ __forceinline__ T in_front(const T* sums, T& all) {
+    const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const T own = sums[l & (kWaves - 1)];
+    T v = own + moved<0x111>(own);         // (a row of 16 lanes holds all)
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    v += moved<0x118>(v);
+    all = at_lane(v, kWaves - 1);
+    return at_lane(T(v - own), w);
+}
+static_assert(kWaves == 16, "a lane of a row for each wave");
 
 // What the filters leave open (step 2).
 struct Cut {                               // (read as whole words)
@@ -166,6 +181,7 @@ struct Shared {
     uint32_t seg_n[kMaxSlices * kWaves];
     double frac[64];
     uint64_t part[kWaves], parts[kWaves], ties[kWaves];
+    uint32_t counts[kWaves];
     uint64_t above;
     int found[2];
     uint32_t digit;
@@ -178,9 +194,7 @@ __device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared& sh) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) v += sh.part[i];
+    in_front(sh.part, v);
     return v;
 }
 
@@ -373,7 +387,7 @@ __device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shar
         const uint64_t own = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
         const uint64_t v = wave_sums(own);
         if (own && at + v > target && at + v - own <= target) R.choose(a, i + l, own, total);
-        at += of_last(v);
+        at += at_lane(v, 63);
         ties_before += __popcll(ballot);
         if (at > target) break;
     }
@@ -448,9 +462,7 @@ __device__ __forceinline__ uint64_t best_of(const SampleArgs& a, const Row& R, S
     uint64_t b = wave_max(ranked(top, at));
     if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = b;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) b = max(b, sh.part[i]);
-    return b;
+    return wave_max(sh.part[threadIdx.x & (kWaves - 1)]);
 }
 
 __device__ __forceinline__ void clear_bins(Shared& sh) {
@@ -499,17 +511,15 @@ struct BinSums {
         c = wave_sums(c0);
         m = wave_sums(m0);
         if ((t & 63) == 63) {
-            sh.ties[w] = c;
+            sh.counts[w] = c;
             sh.parts[w] = m;
         }
         if (t < 2) sh.found[t] = kBins - 1;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kWaves - 1; ++i)
-            if (i < w) {
-                c += (uint32_t)sh.ties[i];
-                m += sh.parts[i];
-            }
+        uint32_t n;
+        uint64_t all;
+        c += in_front(sh.counts, n);
+        m += in_front(sh.parts, all);
         sh.count[t] = c;
         sh.mass[t] = m;
         c0 = c - c0;
@@ -591,7 +601,7 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
                 if (at < (uint32_t)kWaveList) list[at] = ranked(v[e], i + e);
                 ++at;
             }
-        n += of_last(sums);
+        n += at_lane(sums, 63);
     };
     sum = 0;
     if (lo == 0) {
@@ -624,14 +634,7 @@ __device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) 
     __syncthreads();
     if (l == 63) sh.parts[w] = s;
     __syncthreads();
-    uint64_t before = 0;
-    all = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < w) before += sh.parts[i];
-        all += sh.parts[i];
-    }
-    return before + s - x;
+    return in_front(sh.parts, all) + s - x;
 }
 
 // How many of list[0 .. n) are larger than `mine`, and their weights' sum, by the quad that holds `mine` (0 for none).
@@ -919,19 +922,23 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
     return true;
 }
 
-// 2^(i / 64), as sqrt 2 e^x with x = (i - 32) / 64 ln 2 and the series of e^x up to x^13 (the next term is below 5e-18).
-__device__ __forceinline__ void fill_fractions(Shared& sh) {
-    const int i = threadIdx.x;
-    if (i >= 64) return;
-    const double x = (i - 32) * 0x1.62e42fefa39efp-7;
-    double p = 1.0 / 6227020800.0;
-#pragma unroll
-    for (int n = 12; n >= 0; --n) {
-        constexpr double kInverse[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
-                                         1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
-        p = fma(p, x, kInverse[n]);
+// 2^(i / 64), by the series of e^x: past x^20 nothing is left of it.
+struct Fractions {
+    double f[64];
+    constexpr Fractions() : f() {
+        for (int i = 0; i < 64; ++i) {
+            const long double x = 0.693147180559945309417232121458176568L * i / 64;
+            long double p = 1;
+            for (int n = 24; n > 0; --n) p = 1 + p * x / n;
+            f[i] = (double)p;
+        }
     }
-    sh.frac[i] = p * 0x1.6a09e667f3bcdp+0;
+};
+__constant__ const Fractions kFractions;
+// (loaded early, needed late)
+__device__ __forceinline__ double fraction() { return kFractions.f[threadIdx.x & 63]; }
+__device__ __forceinline__ void put_fraction(Shared& sh, double f) {
+    if (threadIdx.x < 64) sh.frac[threadIdx.x] = f;
 }
 
 // A row's workspace: the cut; every slice's best; of every wave the number of listed logits, its sum and its list; of
@@ -963,13 +970,14 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleA
     __shared__ Shared sh;
     const int t = threadIdx.x, w = t >> 6;
     Row R(a, blockIdx.x, DT);
-    fill_fractions(sh);
+    const double f = fraction();
     float most;
     R.set_top(best_of<DT>(a, R, sh, 0, most));
     if (R.done) {
         if (t == 0) R.finish(a);
         return;
     }
+    put_fraction(sh, f);
     fill_bins<DT>(a, R, sh, 0, most);
     decide(R, sh);
     int n = 0;
@@ -1014,7 +1022,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_bins_kernel(Sample
     const uint64_t bests = ws.best[threadIdx.x & (kMaxSlices - 1)];
     Row R(a, blockIdx.y, DT);
     if (R.small_k()) return;
-    fill_fractions(sh);
+    put_fraction(sh, fraction());
     R.set_top(largest(bests, a.slices));
     if (R.done) return;
     fill_bins<DT>(a, R, sh, blockIdx.x, 0.f);
@@ -1031,7 +1039,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
     const RowSpace ws(a.ws + blockIdx.y * a.ws_row, a.slices);
     const uint64_t bests = ws.best[t & (kMaxSlices - 1)];
     Row R(a, blockIdx.y, DT);
-    fill_fractions(sh);
+    const double f = fraction();
     // (of four slices at once, those past the last read as the last again and not counted)
     if (R.small_k()) {
         float most[kMaxSlices] = {};
@@ -1067,6 +1075,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
         sh.count[t] = c[0];
         sh.mass[t] = m[0];
     }
+    put_fraction(sh, f);
     __syncthreads();
     decide(R, sh);
     if (blockIdx.x == 0 && t == 0) *ws.cut = sh.cut;
@@ -1091,7 +1100,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_pick_kernel(Sample
     const uint64_t sum = ws.segs[min(t, segs - 1)];
     const uint64_t bests = ws.best[t & (kMaxSlices - 1)];
     Row R(a, blockIdx.x, DT);
-    fill_fractions(sh);
+    put_fraction(sh, fraction());
     if (t < kCutWords) ((uint64_t*)&sh.cut)[t] = cut;
     if (t < segs) sh.seg_n[t] = listed;
     const uint64_t best = largest(bests, a.slices);
