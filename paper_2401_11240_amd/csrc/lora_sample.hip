@@ -86,26 +86,23 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
 __device__ __forceinline__ uint64_t ranked(float l, int i) { return (uint64_t)key_of(l) << 32 | (0xffffffffu - (uint32_t)i); }
 __device__ __forceinline__ int index_of(uint64_t r) { return (int)(0xffffffffu - (uint32_t)r); }
 
-// The weight 2^43 exp((l - max) / T), rounded: exp(d / T) = 2^(k / 64) e^r, k = round(64 d / (T ln 2)),
-// |r| <= ln 2 / 128, 2^(k / 64) from a table of its 64 fractions and e^r by its series up to r^5 (the
-// next term is below 4e-17).  Adding 2^52 leaves the rounded whole number in the low bits.  (Without branches, so that
-// several run side by side.)
-__device__ __forceinline__ uint64_t weight(float l, float top, double lmax, double rate, const double* frac) {
+// The weight 2^43 exp((l - max) / T), rounded: exp(d / T) = 2^(k / 64) 2^(x / 64) with k + x = 64 d / (T ln 2), k whole and
+// |x| at most 1/2.  2^(43 + k / 64) comes from a table of its 64 fractions, 2^(x / 64) from its series in x up to x^5 (the
+// next term is below 4e-17).  Adding 1.5 2^52 leaves the whole number k in the low bits, adding 2^52 the rounded weight.
+// (Without branches, so that several run side by side: their number of instructions is what the histogram costs.)
+__device__ __forceinline__ uint64_t weight(float l, double lmax, double rate, const double* frac) {
+    constexpr double c = 0x1.62e42fefa39efp-7;                // ln 2 / 64
     double d = ((double)l - lmax) * rate;
-    const bool some = d > -64.0 * (kWeightBits + 2);          // (not of infinities' difference)
-    d = some ? d : 0.0;
-    const double k = __builtin_rint(d);
-    const double r = (d - k) * 0x1.62e42fefa39efp-7;          // ln 2 / 64
-    double p = 1.0 / 120;
-    p = fma(p, r, 1.0 / 24);
-    p = fma(p, r, 1.0 / 6);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    const int ki = (int)k;
-    const double v = ldexp(frac[ki & 63] * p, (ki >> 6) + kWeightBits);
-    const uint64_t w = (uint64_t)__double_as_longlong(v + 0x1p52) - 0x4330000000000000ull;
-    return l == top ? 1ull << kWeightBits : some ? w : 0;
+    d = __builtin_fmin(__builtin_fmax(d, -64.0 * (kWeightBits + 2)), 0.0);   // (rounds to nothing; infinities)
+    const double kd = d + 0x1.8p52, x = d - (kd - 0x1.8p52);
+    const int k = (int)(uint32_t)__double_as_longlong(kd);
+    double p = c * c * c * c * c / 120;
+    p = fma(p, x, c * c * c * c / 24);
+    p = fma(p, x, c * c * c / 6);
+    p = fma(p, x, c * c / 2);
+    p = fma(p, x, c);
+    p = fma(p, x, 1.0);
+    return (uint64_t)__double_as_longlong(fma(ldexp(frac[k & 63], k >> 6), p, 0x1p52)) - 0x4330000000000000ull;
 }
 
 // The value of the lane that the DPP control names, in the rows of ROWS; 0 elsewhere and where there is none.
@@ -179,7 +176,7 @@ struct Shared {
     uint64_t weights[kRanked];
     uint64_t segs[kMaxSlices * kWaves];
     uint32_t seg_n[kMaxSlices * kWaves];
-    double frac[64];
+    double frac[64];                       // 2^(43 + i / 64)
     uint64_t part[kWaves], parts[kWaves], ties[kWaves];
     uint32_t counts[kWaves];
     uint64_t above;
@@ -224,7 +221,8 @@ __device__ __forceinline__ void find_digit(uint64_t above, double limit, Shared&
 struct Row {
     const void* z;
     float T, p, m, lmax_f, bin_top, bin_rate;
-    double lmax, rate, least, u;           // least: the weight that min_p asks for
+    double lmax, rate, u;
+    uint64_t least;                        // the weight that min_p asks for
     int row, V, k, top_at;
     bool has_k, has_p, done;               // done: nothing to draw (nothing left, or the largest logit alone)
 
@@ -242,21 +240,21 @@ struct Row {
         u = uf >= 1.f ? 1.0 : uf > 0.f ? (double)uf : 0.0;
         has_k = k > 0 && k < V;
         has_p = p < 1.f;
-        least = m > 0.f ? (double)(m < 1.f ? m : 1.f) * kOne : 0;
+        least = m > 0.f ? (uint64_t)ceil((double)(m < 1.f ? m : 1.f) * kOne) : 0;
     }
     __device__ __forceinline__ void set_top(uint64_t best) {
         lmax_f = logit_of((uint32_t)(best >> 32));
         top_at = index_of(best);
         done = (uint32_t)(best >> 32) <= kKeyNone || !(T >= kLeastT);
-        lmax = lmax_f;
+        lmax = lmax_f < INFINITY ? (double)lmax_f : 0x1p130;   // (infinity weighs 2^43, what is finite nothing)
         rate = 64 * 1.4426950408889634 / (double)T;
         bin_rate = (float)kBinsPerNat / T;
         bin_top = fminf(lmax_f, 3.402823466e38f);
     }
     // top_k is small: the histogram is of threads' largest logits, and K's weights are summed in the list
     __device__ __forceinline__ bool small_k() const { return has_k && k <= kSmallK; }
-    __device__ __forceinline__ uint64_t weight_of(float l, const double* frac) const { return weight(l, lmax_f, lmax, rate, frac); }
-    __device__ __forceinline__ uint64_t kept(uint64_t w) const { return (double)w >= least ? w : 0; }
+    __device__ __forceinline__ uint64_t weight_of(float l, const double* frac) const { return weight(l, lmax, rate, frac); }
+    __device__ __forceinline__ uint64_t kept(uint64_t w) const { return w >= least ? w : 0; }
     // (each step is monotone; what is -infinity or weighs nothing is in the last bin)
     __device__ __forceinline__ int bin_of(float l) const {
         return (int)__builtin_amdgcn_fmed3f((bin_top - l) * bin_rate, 0.f, (float)(kBins - 1));
@@ -559,7 +557,7 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
     // are rounded by up to ln 2)
     int m1 = kBins - 2;
     if (R.least > 0) {
-        const float f = (float)kBinsPerNat * -logf((float)(R.least / kOne));
+        const float f = (float)kBinsPerNat * -logf((float)((double)R.least / kOne));
         const int spare = R.least < 256 ? kBinsPerNat * 3 / 4 : 2;
         if (f < (float)(kBins - 2)) m1 = min((int)f + spare, kBins - 2);
     }
@@ -922,7 +920,7 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
     return true;
 }
 
-// 2^(i / 64), by the series of e^x: past x^20 nothing is left of it.
+// 2^(43 + i / 64), by the series of e^x: past x^20 nothing is left of it.
 struct Fractions {
     double f[64];
     constexpr Fractions() : f() {
@@ -930,7 +928,7 @@ struct Fractions {
             const long double x = 0.693147180559945309417232121458176568L * i / 64;
             long double p = 1;
             for (int n = 24; n > 0; --n) p = 1 + p * x / n;
-            f[i] = (double)p;
+            f[i] = (double)p * kOne;
         }
     }
 };
