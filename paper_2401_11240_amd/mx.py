@@ -2,8 +2,8 @@
 
 Marshalling only, with the C functions' names.  ``Rows`` describes torch tensors of codes and
 scales to the library and keeps them alive; the calls take device buffers and streams as the
-rest of the package does.  Rows that are not on one GPU, and workspaces given as tensors that are too
-short or on another device, are refused before anything is enqueued (``ValueError``).
+rest of the package does.  Rows, and tensors beside them, that are not on one GPU, and workspaces given as
+tensors that are too short or on another device, are refused before anything is enqueued (``ValueError``).
 """
 from __future__ import annotations
 
@@ -99,6 +99,17 @@ def _addr(p) -> int:
         return 0 if p is None else int(p)
 
 
+def _at(name: str, t, gpu: int) -> int:
+    """The address of a tensor on that GPU, or the address that is given."""
+    try:
+        p = t.data_ptr()
+    except AttributeError:
+        return 0 if t is None else int(t)
+    if gpu < 0 or t.get_device() != gpu:
+        raise ValueError(f"{name} is on {t.device}: a tensor on cuda:{max(gpu, 0)} is needed")
+    return p
+
+
 def _on_gpu(*rows: Rows) -> None:
     for r in rows:
         if r.gpu != rows[0].gpu or r.gpu < 0:
@@ -120,18 +131,23 @@ def lora_norm(x, ldx: int, residual, ldr: int, weight, eps: float, n_rows: int, 
               y, ldy: int, q: Rows = None, stream=None) -> None:
     if q is not None:
         _on_gpu(q)
-    _check(_lib().lora_norm(_addr(x), ldx, _addr(residual), ldr, _addr(weight), eps, n_rows, h, dtype, _addr(total), ldt,
-                            _addr(y), ldy, q.c if q is not None else None, _stream(stream)))
+        gpu = q.gpu
+    else:                                  # (outputs are never all missing: one of them says where)
+        on = next((t for t in (y, total, x, weight, residual) if hasattr(t, "get_device")), None)
+        gpu = -1 if on is None else on.get_device()
+    _check(_lib().lora_norm(_at("x", x, gpu), ldx, _at("residual", residual, gpu), ldr, _at("weight", weight, gpu), eps, n_rows,
+                            h, dtype, _at("total", total, gpu), ldt, _at("y", y, gpu), ldy, q.c if q is not None else None,
+                            _stream(stream)))
 
 
 def lora_mx_quantize(x, ldx: int, dtype: int, q: Rows, stream=None) -> None:
     _on_gpu(q)
-    _check(_lib().lora_mx_quantize(_addr(x), ldx, dtype, q.c, _stream(stream)))
+    _check(_lib().lora_mx_quantize(_at("x", x, q.gpu), ldx, dtype, q.c, _stream(stream)))
 
 
 def lora_mx_dequantize(q: Rows, y, ldy: int, dtype: int, stream=None) -> None:
     _on_gpu(q)
-    _check(_lib().lora_mx_dequantize(q.c, _addr(y), ldy, dtype, _stream(stream)))
+    _check(_lib().lora_mx_dequantize(q.c, _at("y", y, q.gpu), ldy, dtype, _stream(stream)))
 
 
 def lora_mx_workspace_bytes(x: Rows, w: Rows) -> int:
@@ -142,4 +158,4 @@ def lora_mx_workspace_bytes(x: Rows, w: Rows) -> int:
 
 def lora_mx_apply(x: Rows, w: Rows, y, ldy: int, dtype: int, ws, ws_bytes: int, stream=None) -> None:
     _on_gpu(x, w)
-    _check(_lib().lora_mx_apply(x.c, w.c, _addr(y), ldy, dtype, _space(ws, ws_bytes, x.device), ws_bytes, _stream(stream)))
+    _check(_lib().lora_mx_apply(x.c, w.c, _at("y", y, x.gpu), ldy, dtype, _space(ws, ws_bytes, x.device), ws_bytes, _stream(stream)))

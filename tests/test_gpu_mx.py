@@ -524,3 +524,18 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for (_, _, _, want, _), y in zip(jobs, ys):
         assert all(torch.equal(a, want) for a in y)
+
+
+def test_tensors_on_the_host_among_others_are_refused():
+    d, host = torch.zeros((2, 64), dtype=torch.float16, device=DEV), torch.zeros((2, 64), dtype=torch.float16)
+    q, w = MX.empty_rows(2, 64, R.E4M3, DEV), MX.empty_rows(8, 64, R.E2M1, DEV)
+    ws = torch.empty(MX.lora_mx_workspace_bytes(q, w), dtype=torch.uint8, device=DEV)
+    for i in range(5):
+        x, r, g, total, y = (host if j == i else torch.zeros_like(d) for j in range(5))
+        for rows in (q, None):
+            with pytest.raises(ValueError):
+                MX.lora_norm(x, 64, r, 64, g, 1e-5, 2, 64, R.F16, total, 64, y, 64, rows, stream())
+    for call in (lambda: MX.lora_mx_quantize(host, 64, R.F16, q, stream()), lambda: MX.lora_mx_dequantize(q, host, 64, R.F16, stream()),
+                 lambda: MX.lora_mx_apply(q, w, host, 64, R.F16, ws, ws.numel(), stream())):
+        with pytest.raises(ValueError):
+            call()

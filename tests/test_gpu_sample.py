@@ -262,3 +262,10 @@ def test_more_rows_than_a_launch_has():
         want, own, total = R.sample(zz[i], t[r], int(k[r]), p[r], m[r], u[r])
         assert tokens[r] == want, r
         assert abs(probs[r] - own / total) <= own / total * (2.0 ** -24 + 2.0 ** -50), r
+
+
+def test_logits_on_the_host_are_refused():
+    z, u = torch.zeros((2, 64)), torch.zeros(2, device=DEV)
+    tokens, ws = torch.zeros(2, dtype=torch.int32, device=DEV), torch.empty(64, dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError):
+        SA.lora_sample(z, 64, R.F32, 2, 64, None, u, tokens, None, ws, 64, stream())

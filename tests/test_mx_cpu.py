@@ -251,3 +251,12 @@ def test_tensors_on_the_host_are_refused():
         SA.lora_sample(y, 64, L.LORA_F16, 2, 64, None, f, i, None, ws, 16)
     with pytest.raises(ValueError):            # parameters of fewer rows
         SA.lora_sample(GB, 64, L.LORA_F16, 3, 64, SA.Params(f), 2 * GB, 3 * GB, 0, 4 * GB, 16)
+
+
+@pytest.mark.parametrize("which", ["x", "residual", "weight", "total", "y"])
+def test_a_norm_of_host_tensors_is_refused(which):
+    torch = pytest.importorskip("torch")
+    a = dict(x=GB, residual=2 * GB, weight=3 * GB, total=4 * GB, y=5 * GB)
+    a[which] = torch.zeros((2, 64), dtype=torch.float16)
+    with pytest.raises(ValueError):
+        MX.lora_norm(a["x"], 64, a["residual"], 64, a["weight"], 1e-5, 2, 64, L.LORA_F16, a["total"], 64, a["y"], 64)
