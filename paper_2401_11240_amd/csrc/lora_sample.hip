@@ -882,11 +882,11 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
 // slice); numbers in sh.seg_n[0 .. segs).  False if one did not fit or all do not.
 __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int segs, int& n) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
-    const uint32_t mine = t < segs ? sh.seg_n[t] : 0;
-    uint64_t all;
-    const uint32_t first = (uint32_t)scan(sh, mine, all);
+    const uint64_t mine = t < segs ? sh.seg_n[t] : 0;
+    uint64_t all;                          // (one that did not fit makes it too large)
+    const uint64_t first = scan(sh, mine > (uint64_t)kWaveList ? mine + kList : mine, all);
     n = (int)all;
-    if (__syncthreads_or(mine > (uint32_t)kWaveList) || all > (uint64_t)kList) return false;
+    if (all > (uint64_t)kList) return false;
     if (t < segs) sh.segs[t] = first;      // (for a moment)
     __syncthreads();
     if (segs == kWaves) {
@@ -900,20 +900,23 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
         for (int q = 0; q < kPer; ++q)
             if (l + 64 * q < of) sh.list[to + l + 64 * q] = r[q];
     } else {
-        // the first 64 of all of the wave's parts at once, more where there are
-        uint64_t r[kMaxSlices];
+        // the first 64 of eight of the wave's parts at once, more where there are
+        constexpr int kPer = 8;
+        for (int j0 = 0; j0 * kWaves < segs; j0 += kPer) {
+            uint64_t r[kPer];
 #pragma unroll
-        for (int j = 0; j < kMaxSlices; ++j) {
-            const int g = w + kWaves * j;
-            r[j] = g < segs && l < (int)sh.seg_n[g] ? from[(int64_t)g * kWaveList + l] : 0;
-        }
+            for (int j = 0; j < kPer; ++j) {
+                const int g = w + kWaves * (j0 + j);
+                r[j] = g < segs && l < (int)sh.seg_n[g] ? from[(int64_t)g * kWaveList + l] : 0;
+            }
 #pragma unroll
-        for (int j = 0; j < kMaxSlices; ++j) {
-            const int g = w + kWaves * j;
-            if (g >= segs) break;
-            const int of = (int)sh.seg_n[g], to = (int)sh.segs[g];
-            if (l < of) sh.list[to + l] = r[j];
-            for (int i = l + 64; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
+            for (int j = 0; j < kPer; ++j) {
+                const int g = w + kWaves * (j0 + j);
+                if (g >= segs) break;
+                const int of = (int)sh.seg_n[g], to = (int)sh.segs[g];
+                if (l < of) sh.list[to + l] = r[j];
+                for (int i = l + 64; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
+            }
         }
     }
     __syncthreads();
