@@ -393,13 +393,16 @@ __device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shar
 
 // f(logits, index of the first) for the logits of segment `seg`, by one wave, whose lanes hold kVec consecutive ones each,
 // lane by lane and step by step in the order of the indices.  NaN is as -infinity, and so is what lies past the
-// segment.  (16 bytes a lane and load, at whatever alignment the row has; two loads on their way together.)
+// segment, and all that lanes have whose `want` is false.  (16 bytes a lane and load, at whatever alignment the row has; U
+// loads on their way together.)
 template <int DT>
 struct Vec {
     static constexpr int kVec = DT == LORA_F32 ? 4 : 8;
     u32x4 w;
-    __device__ __forceinline__ void load(const Row& R, int i) {
-        __builtin_memcpy(&w, (const unsigned char*)R.z + (int64_t)i * (DT == LORA_F32 ? 4 : 2), 16);
+    __device__ __forceinline__ void load(const Row& R, int i, bool want) {
+        constexpr uint32_t kNone = DT == LORA_F32 ? 0xff800000u : DT == LORA_F16 ? 0xfc00fc00u : 0xff80ff80u;
+        w = u32x4{kNone, kNone, kNone, kNone};
+        if (want) __builtin_memcpy(&w, (const unsigned char*)R.z + (int64_t)i * (DT == LORA_F32 ? 4 : 2), 16);
     }
     __device__ __forceinline__ float get(int e) const {
         const uint32_t x = DT == LORA_F32 ? w[e & 3] : w[(e >> 1) & 3] >> (16 * (e & 1)) & 0xffffu;
@@ -407,18 +410,18 @@ struct Vec {
         return l == l ? l : -INFINITY;
     }
 };
-template <int DT, class F>
-__device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, int seg, const F& f) {
+template <int DT, int U = 2, class F>
+__device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, int seg, const F& f, bool want = true) {
     constexpr int kVec = Vec<DT>::kVec, kStep = 64 * kVec;
     const int l = threadIdx.x & 63, end = min(R.V, (seg + 1) * a.seg);
     int c = seg * a.seg;
     float v[kVec];
-    for (; c + 2 * kStep <= end; c += 2 * kStep) {
-        Vec<DT> x[2];
-        x[0].load(R, c + kVec * l);
-        x[1].load(R, c + kStep + kVec * l);
+    for (; c + U * kStep <= end; c += U * kStep) {
+        Vec<DT> x[U];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < U; ++q) x[q].load(R, c + kStep * q + kVec * l, want);
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[e] = x[q].get(e);
             f(v, c + kStep * q + kVec * l);
@@ -427,7 +430,7 @@ __device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, i
     for (; c < end; c += kStep) {
         if (c + kStep <= end) {
             Vec<DT> x;
-            x.load(R, c + kVec * l);
+            x.load(R, c + kVec * l, want);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[e] = x.get(e);
             f(v, c + kVec * l);
@@ -436,7 +439,7 @@ __device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, i
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
             const int i = c + kVec * l + e;
-            v[e] = i < end ? logit<DT>(R.z, i) : -INFINITY;
+            v[e] = want && i < end ? logit<DT>(R.z, i) : -INFINITY;
             v[e] = v[e] == v[e] ? v[e] : -INFINITY;
         }
         f(v, c + kVec * l);
@@ -583,8 +586,9 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
 
 // Step 3 for segment `seg`, by one wave: its logits of the cut's bins into `list` of kWaveList, in the order of their
 // indices, and, where lo is not 0, the sum of weights below it into `sum`.  Their number, which may be more than the room.
+// `most`: the thread's largest of the segment, where top_k is small; a thread without a listed one reads nothing.
 template <int DT>
-__device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, Shared& sh, int seg, uint64_t* list, uint64_t& sum) {
+__device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, Shared& sh, int seg, float most, uint64_t* list, uint64_t& sum) {
     const int lo = sh.cut.lo, hi = sh.cut.hi;
     constexpr int kVec = Vec<DT>::kVec;
     uint32_t n = 0;
@@ -603,12 +607,12 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
     };
     sum = 0;
     if (lo == 0) {
-        for_segment<DT>(a, R, seg, [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
+        for_segment<DT, 4>(a, R, seg, [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
             uint32_t in = 0;
 #pragma unroll
             for (int e = 0; e < kVec; ++e) in |= (uint32_t)(R.bin_of(v[e]) <= hi) << e;
             add(in, v, i);
-        });
+        }, !R.small_k() || R.bin_of(most) <= hi);
     } else {
         for_segment<DT>(a, R, seg, [&](const float (&v)[kVec], int i) __attribute__((always_inline)) {
             uint32_t in = 0;
@@ -985,7 +989,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleA
     bool fits = !sh.cut.slow;
     if (fits) {
         uint64_t sum;
-        const uint32_t of = collect<DT>(a, R, sh, w, sh.list + w * kWaveList, sum);
+        const uint32_t of = collect<DT>(a, R, sh, w, most, sh.list + w * kWaveList, sum);
         if ((t & 63) == 0) sh.seg_n[w] = of;
         __syncthreads();
         fits = gather(sh, sh.list, kWaves, n);
@@ -1042,7 +1046,9 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
     Row R(a, blockIdx.y, DT);
     const double f = fraction();
     // (of four slices at once, those past the last read as the last again and not counted)
+    float own = 0.f;
     if (R.small_k()) {
+        own = ws.most[blockIdx.x * kSampleThreads + t];
         float most[kMaxSlices] = {};
 #pragma unroll
         for (int j = 0; j < kMaxSlices; ++j)
@@ -1082,7 +1088,7 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
     if (blockIdx.x == 0 && t == 0) *ws.cut = sh.cut;
     if (sh.cut.slow) return;
     uint64_t sum;
-    const uint32_t n = collect<DT>(a, R, sh, seg, ws.list + (int64_t)seg * kWaveList, sum);
+    const uint32_t n = collect<DT>(a, R, sh, seg, own, ws.list + (int64_t)seg * kWaveList, sum);
     if ((t & 63) == 0) {
         ws.n[seg] = n;
         ws.segs[seg] = sum;
