@@ -20,11 +20,11 @@
 // Sums are whole numbers, so neither the order of atomic additions nor the division of a row over workgroups changes
 // a bit.
 //
-// What bounds it: a few rows, the four launches (3 to 10 us each in a trace; one row of 32000: 27 us, most of it the way of the first loads and of
-// barriers of sixteen waves); many rows with top_p and no small top_k, the weights of all logits, about 25 binary64
-// operations each, twice where the list does not hold all that is kept, and their atomic additions (64 rows of 128000 in
-// bfloat16: 67-70 us; with one of them done by slow_row 365); many rows with
-// a small top_k, two readings of the logits (256 x 50257 in float32: 29 us, 51 MB).
+// What bounds it: a few rows, the four launches (3 to 9 us each in a trace; one row of 32000: 22 us, most of it the way of the first loads, of
+// code that every workgroup runs through once, and of barriers of sixteen waves); many rows with top_p and no small top_k, the weights
+// of all logits, about 20 binary64 operations each, twice where the list does not hold all that is kept, and their atomic additions
+// (64 rows of 128000 in bfloat16: 49 us); many rows with a small top_k, the reading of the logits (256 x 50257 in float32: 21 us, 51 MB,
+// of which 8 are that reading, 3 the second, of the threads that have a listed logit, and 8 the way from there to the token).
 #include <cmath>
 
 #include <algorithm>
@@ -1137,11 +1137,15 @@ struct SamplePlan {
 };
 
 // One launch and a workgroup a row from 129 rows on, or where a row is short; slices of 4096 logits at least, as many as
-// give every compute unit a workgroup, otherwise.  Measured, one launch against 2, 4 and 8 slices: 256 rows of
-// 50257 with top_k 29 us against 44, 53, 67, with top_p alone 76 against 89, 101, 113; 64 rows of 128000, all kinds, 127
-// against 88, 64, 63; 16 rows of 32000 without filters 34 against 30, 25, 24; one row of 32000 33 against 32, 28, 27.
+// give every compute unit a workgroup, otherwise.  What a row costs depends on its parameters, which are on the device: with a
+// small top_k one workgroup is faster further up than with top_p alone.  Measured (us), one launch against 2, 4 and 8 slices:
+// 256 rows of 50257 with top_k 50 21 against 33, 39, 49, with top_p alone 57 against 68, 80, 92; 128 rows of 50257 18 against
+// 23, 26 and 55 against 50, 52, of 32000 14 against 21, 23 and 36 against 35, 42; 60 rows of 24000 12 against 19, 19 and 29
+// against 35, 29, of 50257 17 against 21, 20 and 54 against 49, 36; 64 rows of 128000, all kinds, 103 against 70, 49, 50; 16 rows
+// of 32000 without filters 28 against 26, 22, 22; one row of 20000 with top_p 22 against 25, 23, 22, of 32000 28 against 27, 23, 22.
 SamplePlan plan_sample(int n_rows, int n_vocab) {
-    int64_t slices = n_vocab <= 16384 ? 1 : std::min<int64_t>({kMaxSlices, (n_vocab + 4095) / 4096, 256 / std::max(1, n_rows)});
+    const bool one = n_vocab <= 24576 || (n_rows > 64 && n_vocab <= 49152);
+    int64_t slices = one ? 1 : std::min<int64_t>({kMaxSlices, (n_vocab + 4095) / 4096, 256 / std::max(1, n_rows)});
     slices = std::max<int64_t>(1, slices);
     SamplePlan p;
     p.seg = (int)((n_vocab + slices * kWaves * 256 - 1) / (slices * kWaves * 256)) * 256;
