@@ -13,9 +13,10 @@
 //      order of the indices again, the segment and in it the logit where the running sum passes the target.
 //
 // Where there are rows enough a workgroup takes a row all the way, otherwise a row is divided into slices, a workgroup
-// each, with a launch for each step.  A list holds kList logits.  Rows that need a longer one (a top_k of thousands,
-// thousands of equal logits at a threshold) are done by one workgroup, thresholds digit by digit of an ordered key
-// (slow_row).
+// each, with a launch for each step.  A list holds kList logits, a sixteenth for each wave of a workgroup; where a wave has more
+// (the likely logits are neighbours) the waves collect again, in any order, and the token's segment is read once more.  Rows that
+// need a longer list (a top_k of thousands,
+// thousands of equal logits at a threshold) are done by one workgroup, thresholds digit by digit of an ordered key (slow_row).
 //
 // Sums are whole numbers, so neither the order of atomic additions nor the division of a row over workgroups changes
 // a bit.
@@ -587,7 +588,8 @@ __device__ __forceinline__ void decide(const Row& R, Shared& sh) {
 // Step 3 for segment `seg`, by one wave: its logits of the cut's bins into `list` of kWaveList, in the order of their
 // indices, and, where lo is not 0, the sum of weights below it into `sum`.  Their number, which may be more than the room.
 // `most`: the thread's largest of the segment, where top_k is small; a thread without a listed one reads nothing.
-template <int DT>
+// ANY: into a list of kList that all waves share, in any order, sh.digit (0 before) counting.
+template <int DT, bool ANY>
 __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, Shared& sh, int seg, float most, uint64_t* list, uint64_t& sum) {
     const int lo = sh.cut.lo, hi = sh.cut.hi;
     constexpr int kVec = Vec<DT>::kVec;
@@ -596,11 +598,12 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
     auto add = [&](uint32_t in, const float (&v)[kVec], int i) __attribute__((always_inline)) {
         if (!__any(in)) return;
         const uint32_t own = __popc(in), sums = wave_sums(own);
+        if (ANY) n = (uint32_t)__builtin_amdgcn_readlane((int)((threadIdx.x & 63) == 63 ? atomicAdd(&sh.digit, sums) : 0u), 63);
         uint32_t at = n + sums - own;
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
             if (in >> e & 1) {
-                if (at < (uint32_t)kWaveList) list[at] = ranked(v[e], i + e);
+                if (at < (uint32_t)(ANY ? kList : kWaveList)) list[at] = ranked(v[e], i + e);
                 ++at;
             }
         n += at_lane(sums, 63);
@@ -761,12 +764,13 @@ __device__ __forceinline__ void sort_list(Shared& sh, int n) {
     __syncthreads();
 }
 
-// Step 4, from the list (n logits in the order of their indices) and the segments' sums in sh.
+// Step 4, from the list (n logits, `ordered` by their indices or not) and the segments' sums in sh.
 template <int DT>
-__device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& sh, int n) {
+__device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& sh, int n, bool ordered) {
     const int t = threadIdx.x;
     constexpr int kEach = kList / kSampleThreads;
     const Cut cut = sh.cut;
+    const bool direct = cut.lo == 0 && ordered;    // the token is found in the list itself
     auto weight_at = [&](uint64_t r) __attribute__((always_inline)) { return R.weight_of(logit_of((uint32_t)(r >> 32)), sh.frac); };
     const bool cuts = n > 0 && (cut.k_cuts || R.has_p);
     const int most = cut.k_cuts ? min(R.k, n) : n;
@@ -789,7 +793,7 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
                 in &= rank == 0 || (double)(cut.below + before) < (double)R.p * (double)all;
             }
             if (!in) w = 0;
-            if (cut.lo > 0) {              // (the segment's search asks for the last)
+            if (!direct) {                 // (the segment's search asks for the last)
                 if (t == 0) sh.digit = 0;
                 __syncthreads();
                 if (in) atomicMax(&sh.digit, (uint32_t)rank);
@@ -800,7 +804,7 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
             }
         }
         w = (t & 3) == 0 ? R.kept(w) : 0;
-        if (cut.lo == 0) {
+        if (direct) {
             const uint64_t run = scan(sh, w, all), target = R.target(all);
             if (w && run <= target && target < run + w) R.choose(a, index_of(mine), w, all);
             return;
@@ -844,7 +848,7 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
             v[j] = mine[j] && mine[j] >= last ? R.kept(weight_at(mine[j])) : 0;
             sum += v[j];
         }
-        if (cut.lo == 0) {
+        if (direct) {
             uint64_t run = scan(sh, sum, all);
             const uint64_t target = R.target(all);
 #pragma unroll
@@ -883,14 +887,17 @@ __device__ __forceinline__ void pick(const SampleArgs& a, const Row& R, Shared& 
 }
 
 // The waves' lists, from[kWaveList g ..] for wave g, one behind the other in sh.list (which `from` may be itself, of one
-// slice); numbers in sh.seg_n[0 .. segs).  False if one did not fit or all do not.
-__device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int segs, int& n) {
+// slice); numbers in sh.seg_n[0 .. segs).  kFull if all do not fit; kCrowded if one is longer than a wave's part: of one
+// slice it is not whole then and nothing is moved, of several the list is whole, but in any order.
+enum Gathered { kOrdered, kCrowded, kFull };
+__device__ __forceinline__ Gathered gather(Shared& sh, const uint64_t* from, int segs, int& n) {
     const int t = threadIdx.x, l = t & 63, w = t >> 6;
     const uint64_t mine = t < segs ? sh.seg_n[t] : 0;
-    uint64_t all;                          // (one that did not fit makes it too large)
-    const uint64_t first = scan(sh, mine > (uint64_t)kWaveList ? mine + kList : mine, all);
-    n = (int)all;
-    if (all > (uint64_t)kList) return false;
+    uint64_t all;                          // (in the upper half how many are longer)
+    const uint64_t first = scan(sh, mine > (uint64_t)kWaveList ? mine + (1ull << 32) : mine, all) & 0xffffffffu;
+    n = (int)(uint32_t)all;
+    const Gathered how = (uint32_t)all > (uint32_t)kList ? kFull : all >> 32 ? kCrowded : kOrdered;
+    if (how == kFull || (how == kCrowded && segs == kWaves)) return how;
     if (t < segs) sh.segs[t] = first;      // (for a moment)
     __syncthreads();
     if (segs == kWaves) {
@@ -919,12 +926,13 @@ __device__ __forceinline__ bool gather(Shared& sh, const uint64_t* from, int seg
                 if (g >= segs) break;
                 const int of = (int)sh.seg_n[g], to = (int)sh.segs[g];
                 if (l < of) sh.list[to + l] = r[j];
+#pragma unroll 4
                 for (int i = l + 64; i < of; i += 64) sh.list[to + i] = from[(int64_t)g * kWaveList + i];
             }
         }
     }
     __syncthreads();
-    return true;
+    return how;
 }
 
 // 2^(43 + i / 64), by the series of e^x: past x^20 nothing is left of it.
@@ -986,22 +994,27 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_row_kernel(SampleA
     fill_bins<DT>(a, R, sh, 0, most);
     decide(R, sh);
     int n = 0;
-    bool fits = !sh.cut.slow;
-    if (fits) {
+    Gathered how = sh.cut.slow ? kFull : kOrdered;
+    if (how != kFull) {
         uint64_t sum;
-        const uint32_t of = collect<DT>(a, R, sh, w, most, sh.list + w * kWaveList, sum);
+        const uint32_t of = collect<DT, false>(a, R, sh, w, most, sh.list + w * kWaveList, sum);
         if ((t & 63) == 0) sh.seg_n[w] = of;
         __syncthreads();
-        fits = gather(sh, sh.list, kWaves, n);
+        how = gather(sh, sh.list, kWaves, n);
         __syncthreads();
         if ((t & 63) == 0) sh.segs[w] = sum;
+        if (t == 0) sh.digit = 0;
         __syncthreads();
+        if (how == kCrowded) {
+            collect<DT, true>(a, R, sh, w, most, sh.list, sum);
+            __syncthreads();
+        }
     }
-    if (!fits) {
+    if (how == kFull) {
         slow_row<DT>(a, R, sh);
         return;
     }
-    pick<DT>(a, R, sh, n);
+    pick<DT>(a, R, sh, n, how == kOrdered);
 }
 
 // The row's best of its slices', which lanes hold.
@@ -1088,7 +1101,13 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_list_kernel(Sample
     if (blockIdx.x == 0 && t == 0) *ws.cut = sh.cut;
     if (sh.cut.slow) return;
     uint64_t sum;
-    const uint32_t n = collect<DT>(a, R, sh, seg, own, ws.list + (int64_t)seg * kWaveList, sum);
+    uint32_t n = collect<DT, false>(a, R, sh, seg, own, ws.list + (int64_t)seg * kWaveList, sum);
+    if (t == 0) sh.digit = 0;
+    if (__syncthreads_or(n > (uint32_t)kWaveList)) {   // the slice's waves share their parts, and the first has all
+        collect<DT, true>(a, R, sh, seg, own, ws.list + (int64_t)blockIdx.x * kList, sum);
+        __syncthreads();
+        n = t < 64 ? sh.digit : 0;
+    }
     if ((t & 63) == 0) {
         ws.n[seg] = n;
         ws.segs[seg] = sum;
@@ -1118,18 +1137,18 @@ __global__ void __launch_bounds__(kSampleThreads) lora_sample_pick_kernel(Sample
     }
     __syncthreads();
     int n = 0;
-    bool fits = !sh.cut.slow;
-    if (fits) {
-        fits = gather(sh, ws.list, segs, n);
+    Gathered how = sh.cut.slow ? kFull : kOrdered;
+    if (how != kFull) {
+        how = gather(sh, ws.list, segs, n);
         __syncthreads();
         if (t < segs) sh.segs[t] = sum;
         __syncthreads();
     }
-    if (!fits) {
+    if (how == kFull) {
         slow_row<DT>(a, R, sh);
         return;
     }
-    pick<DT>(a, R, sh, n);
+    pick<DT>(a, R, sh, n, how == kOrdered);
 }
 
 struct SamplePlan {

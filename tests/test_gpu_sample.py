@@ -127,6 +127,23 @@ def test_filters_that_end_among_many(v, scale, dtype):
 
 
 @dtypes
+@pytest.mark.parametrize("likely", [300, 1500, 2900])
+@pytest.mark.parametrize("v", [7000, 20000, 60000])
+def test_likely_logits_that_are_neighbours(v, likely, dtype):
+    """All that the filters leave lies in a short piece of the row, at its start, inside and at its end."""
+    rng = np.random.default_rng([5, v, likely, dtype])
+    z = rng.standard_normal((18, v)) * 0.5 - 20
+    for r in range(18):
+        first = (0, (v - likely) // 3, v - likely)[r % 3]
+        z[r, first:first + likely] += 20
+    z = torch.from_numpy(z).to(DEV).to(TYPE[dtype])
+    k = np.repeat(np.array([0, 280, 1000], np.int32), 6)
+    p = np.array([1, 1, 1, 0.9, 0.9, 0.4] * 3, np.float32)
+    m = np.where(np.arange(18) % 4 == 3, 0.2, 0).astype(np.float32)
+    check(z, np.ones(18, np.float32), k, p, m, rng.random(18).astype(np.float32), dtype)
+
+
+@dtypes
 @pytest.mark.parametrize("v", [9, 3000, 90000])
 def test_masked_infinite_and_nan_logits(v, dtype):
     rng = np.random.default_rng([4, v])
