@@ -148,9 +148,10 @@ def _addr(p) -> int:
 def _stream(s) -> int:
     if s is None:
         return 0
-    if hasattr(s, "cuda_stream"):
+    try:                                   # (a call of a few rows costs the host what this costs it)
         return int(s.cuda_stream)
-    return int(s)
+    except AttributeError:
+        return int(s)
 
 
 def _check(rc: int):

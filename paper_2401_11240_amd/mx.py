@@ -99,20 +99,29 @@ def _addr(p) -> int:
         return 0 if p is None else int(p)
 
 
-def _at(name: str, t, gpu: int) -> int:
-    """The address of a tensor on that GPU, or the address that is given."""
-    try:
-        p = t.data_ptr()
-    except AttributeError:
-        return 0 if t is None else int(t)
-    if gpu < 0 or t.get_device() != gpu:
-        raise ValueError(f"{name} is on {t.device}: a tensor on cuda:{max(gpu, 0)} is needed")
-    return p
+def _at(gpu: int, names: str, *tensors) -> list:
+    """The addresses of tensors on that GPU (or those that are given), in one call: each costs the host what a
+    launch of few rows is about to wait for."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        try:
+            p = t.data_ptr()
+        except AttributeError:
+            out.append(int(t))
+            continue
+        if t.get_device() != gpu or gpu < 0:
+            raise ValueError(f"{names.split()[len(out)]} is on {t.device}: a tensor on cuda:{max(gpu, 0)} is needed")
+        out.append(p)
+    return out
 
 
 def _on_gpu(*rows: Rows) -> None:
+    gpu = rows[0].gpu
     for r in rows:
-        if r.gpu != rows[0].gpu or r.gpu < 0:
+        if r.gpu != gpu or gpu < 0:
             raise ValueError(f"rows in blocks on {rows[0].device} and {r.device}: device tensors of one GPU are needed")
 
 
@@ -135,19 +144,19 @@ def lora_norm(x, ldx: int, residual, ldr: int, weight, eps: float, n_rows: int, 
     else:                                  # (outputs are never all missing: one of them says where)
         on = next((t for t in (y, total, x, weight, residual) if hasattr(t, "get_device")), None)
         gpu = -1 if on is None else on.get_device()
-    _check(_lib().lora_norm(_at("x", x, gpu), ldx, _at("residual", residual, gpu), ldr, _at("weight", weight, gpu), eps, n_rows,
-                            h, dtype, _at("total", total, gpu), ldt, _at("y", y, gpu), ldy, q.c if q is not None else None,
+    px, pr, pw, pt, py = _at(gpu, "x residual weight total y", x, residual, weight, total, y)
+    _check(_lib().lora_norm(px, ldx, pr, ldr, pw, eps, n_rows, h, dtype, pt, ldt, py, ldy, None if q is None else q.c,
                             _stream(stream)))
 
 
 def lora_mx_quantize(x, ldx: int, dtype: int, q: Rows, stream=None) -> None:
     _on_gpu(q)
-    _check(_lib().lora_mx_quantize(_at("x", x, q.gpu), ldx, dtype, q.c, _stream(stream)))
+    _check(_lib().lora_mx_quantize(_at(q.gpu, "x", x)[0], ldx, dtype, q.c, _stream(stream)))
 
 
 def lora_mx_dequantize(q: Rows, y, ldy: int, dtype: int, stream=None) -> None:
     _on_gpu(q)
-    _check(_lib().lora_mx_dequantize(q.c, _at("y", y, q.gpu), ldy, dtype, _stream(stream)))
+    _check(_lib().lora_mx_dequantize(q.c, _at(q.gpu, "y", y)[0], ldy, dtype, _stream(stream)))
 
 
 def lora_mx_workspace_bytes(x: Rows, w: Rows) -> int:
@@ -158,4 +167,4 @@ def lora_mx_workspace_bytes(x: Rows, w: Rows) -> int:
 
 def lora_mx_apply(x: Rows, w: Rows, y, ldy: int, dtype: int, ws, ws_bytes: int, stream=None) -> None:
     _on_gpu(x, w)
-    _check(_lib().lora_mx_apply(x.c, w.c, _at("y", y, x.gpu), ldy, dtype, _space(ws, ws_bytes, x.device), ws_bytes, _stream(stream)))
+    _check(_lib().lora_mx_apply(x.c, w.c, _at(x.gpu, "y", y)[0], ldy, dtype, _space(ws, ws_bytes, x.device), ws_bytes, _stream(stream)))

@@ -86,7 +86,7 @@ def lora_sample(logits, ld: int, dtype: int, n_rows: int, n_vocab: int, params, 
         raise ValueError(f"tensors on {on}: device tensors are needed")
     if params is not None and params.device is not None and (on or params.device) != params.device:
         raise ValueError(f"the parameters are on {params.device}, the rows on {on}")
-    _check(_lib().lora_sample(_at("logits", logits, -1 if on is None else on.index), ld, dtype, n_rows, n_vocab, params.c if params is not None else None,
+    _check(_lib().lora_sample(_at(-1 if on is None else on.index, "logits", logits)[0], ld, dtype, n_rows, n_vocab, params.c if params is not None else None,
                               _array("u", u, n_rows, "torch.float32", on), _array("tokens", tokens, n_rows, "torch.int32", on),
                               _array("probs", probs, n_rows, "torch.float32", on), _space(ws, ws_bytes, on), ws_bytes,
                               _stream(stream)))
