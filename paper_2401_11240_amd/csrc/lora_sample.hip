@@ -275,123 +275,6 @@ struct Row {
     }
 };
 
-// A threshold over the row in memory, by the whole workgroup: the lowest key whose larger ones sum to less than `limit`,
-// and in `above` what they sum to.  BY_WEIGHT: of weights, otherwise of ones.  With weights, keys below floor_key do not
-// count and those of floor_key weigh floor_sum together.
-template <int DT, bool BY_WEIGHT>
-__device__ __forceinline__ uint32_t threshold(const Row& R, Shared& sh, double limit, uint32_t floor_key, uint64_t floor_sum,
-                                              uint64_t& above) {
-    uint32_t prefix = 0;
-    above = 0;
-    for (int level = 0; level < 3; ++level) {
-        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-        __syncthreads();
-        for (int i = threadIdx.x; i < kDigits; i += kSampleThreads) sh.hist[i] = 0;
-        __syncthreads();
-        for (int i = threadIdx.x; i < R.V; i += kSampleThreads) {
-            const float l = logit<DT>(R.z, i);
-            const uint32_t key = key_of(l);
-            if (key <= kKeyNone || (level > 0 && (key >> (shift + bits)) != prefix)) continue;
-            uint64_t v = 1;
-            if (BY_WEIGHT) v = key > floor_key ? R.weight_of(l, sh.frac) : 0;
-            if (v) atomicAdd(&sh.hist[(key >> shift) & ((1u << bits) - 1)], (unsigned long long)v);
-        }
-        if (BY_WEIGHT && threadIdx.x == 0 && floor_sum && (level == 0 || (floor_key >> (shift + bits)) == prefix))
-            atomicAdd(&sh.hist[(floor_key >> shift) & ((1u << bits) - 1)], (unsigned long long)floor_sum);
-        __syncthreads();
-        find_digit(above, limit, sh);
-        prefix = prefix << bits | sh.digit;
-        above = sh.above;
-    }
-    return prefix;
-}
-
-// The row from memory by one workgroup, however it is.
-template <int DT>
-__device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shared& sh) {
-    const int t = threadIdx.x, l = t & 63, w = t >> 6, V = R.V;
-    auto weight_at = [&](uint32_t key) { return R.weight_of(logit_of(key), sh.frac); };
-    auto key_at = [&](int i) { return key_of(logit<DT>(R.z, i)); };
-    // kept are keys above tkey, and of those equal the first `share`
-    uint32_t tkey = kKeyNone, share = 0;
-    if (R.has_k) {
-        uint64_t above;
-        tkey = threshold<DT, false>(R, sh, (double)R.k, 0, 0, above);
-        share = (uint32_t)(R.k - above);   // (at least 1; more than there are if few logits are left)
-    }
-    if (R.has_p && !(R.p > 0.f)) {
-        tkey = key_of(R.lmax_f);
-        share = 1;
-    } else if (R.has_p) {
-        uint64_t sum = 0, ties = 0;        // over K
-        for (int i = t; i < V; i += kSampleThreads) {
-            const uint32_t key = key_at(i);
-            if (key <= kKeyNone) continue;
-            if (key > tkey) sum += weight_at(key);
-            else if (key == tkey) ++ties;
-        }
-        sum = block_sum(sum, sh);
-        ties = block_sum(ties, sh);
-        const uint64_t floor_sum = tkey > kKeyNone ? min((uint64_t)share, ties) * weight_at(tkey) : 0;
-        const double limit = (double)R.p * (double)(sum + floor_sum);
-        uint64_t above;
-        const uint32_t key = threshold<DT, true>(R, sh, limit, tkey, floor_sum, above);
-        const uint64_t each = weight_at(key);
-        // the first `few` of the equal ones begin below the limit
-        uint32_t few = 1, most = key == tkey ? share : (uint32_t)V;
-        while (few < most) {
-            const uint32_t mid = few + (most - few + 1) / 2;
-            if ((double)(above + (mid - 1) * each) < limit) few = mid;
-            else most = mid - 1;
-        }
-        tkey = key;
-        share = few;
-    }
-    const uint64_t tie_weight = tkey > kKeyNone ? R.kept(weight_at(tkey)) : 0;
-    // weights and ties of each wave's part of the row, in the order of the indices
-    const int per = ((V + kWaves - 1) / kWaves + 63) & ~63;
-    const int i0 = min(w * per, V), i1 = min(i0 + per, V);
-    uint64_t sum = 0, ties = 0;
-    for (int i = i0 + l; i < i1; i += 64) {
-        const uint32_t key = key_at(i);
-        if (key <= kKeyNone) continue;
-        if (key > tkey) sum += R.kept(weight_at(key));
-        else if (key == tkey) ++ties;
-    }
-    sum = wave_sum(sum);
-    ties = wave_sum(ties);
-    __syncthreads();
-    if (l == 0) {
-        sh.parts[w] = sum;
-        sh.ties[w] = ties;
-    }
-    __syncthreads();
-    uint64_t total = 0, at = 0, ties_before = 0, seen = 0;
-    for (int i = 0; i < kWaves; ++i) {
-        if (i == w) {
-            at = total;
-            ties_before = seen;
-        }
-        const uint64_t left = share > seen ? share - seen : 0;
-        total += sh.parts[i] + min(left, sh.ties[i]) * tie_weight;
-        seen += sh.ties[i];
-    }
-    const uint64_t target = R.target(total);
-    // the wave in whose part the target lies comes to it
-    for (int i = i0; i < i1; i += 64) {
-        const uint32_t key = i + l < i1 ? key_at(i + l) : 0;
-        const bool tie = key == tkey && key > kKeyNone;
-        const uint64_t ballot = __ballot(tie);
-        const uint64_t rank = ties_before + __popcll(ballot & ((1ull << l) - 1));
-        const uint64_t own = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
-        const uint64_t v = wave_sums(own);
-        if (own && at + v > target && at + v - own <= target) R.choose(a, i + l, own, total);
-        at += at_lane(v, 63);
-        ties_before += __popcll(ballot);
-        if (at > target) break;
-    }
-}
-
 // f(logits, index of the first) for the logits of segment `seg`, by one wave, whose lanes hold kVec consecutive ones each,
 // lane by lane and step by step in the order of the indices.  NaN is as -infinity, and so is what lies past the
 // segment, and all that lanes have whose `want` is false.  (16 bytes a lane and load, at whatever alignment the row has; U
@@ -444,6 +327,142 @@ __device__ __forceinline__ void for_segment(const SampleArgs& a, const Row& R, i
             v[e] = v[e] == v[e] ? v[e] : -INFINITY;
         }
         f(v, c + kVec * l);
+    }
+}
+
+// f(logit) for wave w's sixteenth of the row, which lies behind those of the waves before it.
+template <int DT, class F>
+__device__ __forceinline__ void for_part(const SampleArgs& a, const Row& R, const F& f) {
+    constexpr int kVec = Vec<DT>::kVec;
+    const int w = threadIdx.x >> 6;
+    for (int seg = w * a.slices; seg < (w + 1) * a.slices; ++seg)
+        for_segment<DT>(a, R, seg, [&](const float (&v)[kVec], int) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) f(v[e]);
+        });
+}
+
+// Running sum in front of x over the workgroup's threads; `all` gets the whole.
+__device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) {
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint64_t s = wave_sums(x);
+    __syncthreads();
+    if (l == 63) sh.parts[w] = s;
+    __syncthreads();
+    return in_front(sh.parts, all) + s - x;
+}
+
+// A threshold over the row in memory, by the whole workgroup: the lowest key whose larger ones sum to less than `limit`,
+// and in `above` what they sum to.  BY_WEIGHT: of weights, otherwise of ones.  With weights, keys below floor_key do not
+// count and those of floor_key weigh floor_sum together.
+template <int DT, bool BY_WEIGHT>
+__device__ __forceinline__ uint32_t threshold(const SampleArgs& a, const Row& R, Shared& sh, double limit, uint32_t floor_key, uint64_t floor_sum,
+                                              uint64_t& above) {
+    uint32_t prefix = 0;
+    above = 0;
+    for (int level = 0; level < 3; ++level) {
+        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+        __syncthreads();
+        for (int i = threadIdx.x; i < kDigits; i += kSampleThreads) sh.hist[i] = 0;
+        __syncthreads();
+        for_part<DT>(a, R, [&](float l) __attribute__((always_inline)) {
+            const uint32_t key = key_of(l);
+            if (key <= kKeyNone || (level > 0 && (key >> (shift + bits)) != prefix)) return;
+            uint64_t v = 1;
+            if (BY_WEIGHT) v = key > floor_key ? R.weight_of(l, sh.frac) : 0;
+            if (v) atomicAdd(&sh.hist[(key >> shift) & ((1u << bits) - 1)], (unsigned long long)v);
+        });
+        if (BY_WEIGHT && threadIdx.x == 0 && floor_sum && (level == 0 || (floor_key >> (shift + bits)) == prefix))
+            atomicAdd(&sh.hist[(floor_key >> shift) & ((1u << bits) - 1)], (unsigned long long)floor_sum);
+        __syncthreads();
+        find_digit(above, limit, sh);
+        prefix = prefix << bits | sh.digit;
+        above = sh.above;
+    }
+    return prefix;
+}
+
+// The row from memory by one workgroup, however it is.
+template <int DT>
+__device__ __forceinline__ void slow_row(const SampleArgs& a, const Row& R, Shared& sh) {
+    const int t = threadIdx.x, w = t >> 6, V = R.V;
+    auto weight_at = [&](uint32_t key) { return R.weight_of(logit_of(key), sh.frac); };
+    // kept are keys above tkey, and of those equal the first `share`
+    uint32_t tkey = kKeyNone, share = 0;
+    if (R.has_k) {
+        uint64_t above;
+        tkey = threshold<DT, false>(a, R, sh, (double)R.k, 0, 0, above);
+        share = (uint32_t)(R.k - above);   // (at least 1; more than there are if few logits are left)
+    }
+    if (R.has_p && !(R.p > 0.f)) {
+        tkey = key_of(R.lmax_f);
+        share = 1;
+    } else if (R.has_p) {
+        uint64_t sum = 0, ties = 0;        // over K
+        for_part<DT>(a, R, [&](float l) __attribute__((always_inline)) {
+            const uint32_t key = key_of(l);
+            if (key > kKeyNone && key > tkey) sum += weight_at(key);
+            ties += key > kKeyNone && key == tkey;
+        });
+        sum = block_sum(sum, sh);
+        ties = block_sum(ties, sh);
+        const uint64_t floor_sum = tkey > kKeyNone ? min((uint64_t)share, ties) * weight_at(tkey) : 0;
+        const double limit = (double)R.p * (double)(sum + floor_sum);
+        uint64_t above;
+        const uint32_t key = threshold<DT, true>(a, R, sh, limit, tkey, floor_sum, above);
+        const uint64_t each = weight_at(key);
+        // the first `few` of the equal ones begin below the limit
+        uint32_t few = 1, most = key == tkey ? share : (uint32_t)V;
+        while (few < most) {
+            const uint32_t mid = few + (most - few + 1) / 2;
+            if ((double)(above + (mid - 1) * each) < limit) few = mid;
+            else most = mid - 1;
+        }
+        tkey = key;
+        share = few;
+    }
+    const uint64_t tie_weight = tkey > kKeyNone ? R.kept(weight_at(tkey)) : 0;
+    // weights and ties of each wave's part of the row
+    uint64_t sum = 0, ties = 0;
+    for_part<DT>(a, R, [&](float l) __attribute__((always_inline)) {
+        const uint32_t key = key_of(l);
+        if (key > kKeyNone && key > tkey) sum += R.kept(weight_at(key));
+        ties += key > kKeyNone && key == tkey;
+    });
+    sum = wave_sum(sum);
+    ties = wave_sum(ties);
+    __syncthreads();
+    if ((t & 63) == 0) {
+        sh.part[w] = sum;
+        sh.ties[w] = ties;
+    }
+    __syncthreads();
+    auto part_of = [&](int i, uint64_t seen) { return sh.part[i] + min(share > seen ? share - seen : 0, sh.ties[i]) * tie_weight; };
+    uint64_t total = 0, seen = 0;
+    for (int i = 0; i < kWaves; ++i) {
+        total += part_of(i, seen);
+        seen += sh.ties[i];
+    }
+    const uint64_t target = R.target(total);
+    // the part in which the target lies, and in it the logit, by all
+    uint64_t at = 0;
+    int p = 0;
+    seen = 0;
+    for (; p < kWaves - 1 && target >= at + part_of(p, seen); ++p) {
+        at += part_of(p, seen);
+        seen += sh.ties[p];
+    }
+    const int first = p * a.slices * a.seg, end = min(V, first + a.slices * a.seg);
+    for (int i = first; i < end && at <= target; i += kSampleThreads) {
+        const uint32_t key = i + t < end ? key_of(logit<DT>(R.z, i + t)) : 0;
+        const bool tie = key == tkey && key > kKeyNone;
+        uint64_t here, all;
+        const uint64_t rank = seen + scan(sh, tie ? 1 : 0, here);
+        const uint64_t own = key > kKeyNone && key > tkey ? R.kept(weight_at(key)) : tie && rank < share ? tie_weight : 0;
+        const uint64_t before = at + scan(sh, own, all);
+        if (own && before <= target && target < before + own) R.choose(a, i + t, own, total);
+        at += all;
+        seen += here;
     }
 }
 
@@ -630,16 +649,6 @@ __device__ __forceinline__ uint32_t collect(const SampleArgs& a, const Row& R, S
         sum = wave_sum(sum);
     }
     return n;
-}
-
-// Running sum in front of x over the workgroup's threads; `all` gets the whole.
-__device__ __forceinline__ uint64_t scan(Shared& sh, uint64_t x, uint64_t& all) {
-    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const uint64_t s = wave_sums(x);
-    __syncthreads();
-    if (l == 63) sh.parts[w] = s;
-    __syncthreads();
-    return in_front(sh.parts, all) + s - x;
 }
 
 // How many of list[0 .. n) are larger than `mine`, and their weights' sum, by the quad that holds `mine` (0 for none).
