@@ -9,7 +9,8 @@
 //      least top_k logits are as large as the top_k-th of those, and not many more;
 //   3. the logits of bins lo .. hi in a list, in the order of their indices, and where lo is not 0 the
 //      weights below it, summed by segments of the row;
-//   4. one workgroup sorts the list, falling, and finds in its running sums the last logit that is kept; then, in the
+//   4. one workgroup finds the last logit of the list that is kept (by comparing all with all where they are few, else with a
+//      finer histogram, whose one bin at the border is compared, or is sorted with the list where it is large); then, in the
 //      order of the indices again, the segment and in it the logit where the running sum passes the target.
 //
 // Where there are rows enough a workgroup takes a row all the way, otherwise a row is divided into slices, a workgroup
