@@ -286,3 +286,47 @@ def test_logits_on_the_host_are_refused():
     tokens, ws = torch.zeros(2, dtype=torch.int32, device=DEV), torch.empty(64, dtype=torch.uint8, device=DEV)
     with pytest.raises(ValueError):
         SA.lora_sample(z, 64, R.F32, 2, 64, None, u, tokens, None, ws, 64, stream())
+
+
+@pytest.mark.parametrize("rows,v", [(3, 24576), (3, 24577), (64, 24577), (65, 24577), (65, 49152), (65, 49153), (128, 49153), (129, 49153)])
+def test_sizes_at_the_borders_between_one_launch_and_several(rows, v):
+    rng = np.random.default_rng([10, rows, v])
+    z = logits(rng, rows, v, R.BF16, pad=1)
+    check(z, *mixed(rng, rows, v), rng.random(rows).astype(np.float32), R.BF16)
+
+
+def test_two_recordings_of_several_launches_share_a_workspace():
+    """Rows of slices and rows of one workgroup, replayed in turn with other inputs and eager calls between."""
+    rng = np.random.default_rng(11)
+    st = torch.cuda.Stream()
+    st.wait_stream(stream())
+    shapes = ((6, 50000), (9, 30000))
+    n = max(SA.lora_sample_workspace_bytes(rows, v, R.F32) for rows, v in shapes)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    made = []
+    for rows, v in shapes:
+        z, u = logits(rng, rows, v, R.F32), device(rng.random(rows), np.float32)
+        arrays = [device(a, d) for a, d in zip(mixed(rng, rows, v), (np.float32, np.int32, np.float32, np.float32))]
+        params, tokens = SA.Params(*arrays), torch.empty(rows, dtype=torch.int32, device=DEV)
+        probs = torch.empty(rows, device=DEV)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            SA.lora_sample(z, v, R.F32, rows, v, params, u, tokens, probs, ws, n, st)
+        made.append((rows, v, z, u, arrays, params, tokens, probs, g))
+    for i in range(6):
+        rows, v, z, u, arrays, params, tokens, probs, g = made[i % 2]
+        z.copy_(logits(rng, rows, v, R.F32, scale=(2.0, 0.02, 0.5)[i // 2]))
+        new = mixed(rng, rows, v)
+        for dst, a, d in zip(arrays, new, (np.float32, np.int32, np.float32, np.float32)):
+            dst.copy_(device(a, d))
+        uu = rng.random(rows).astype(np.float32)
+        u.copy_(device(uu, np.float32))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            g.replay()
+        torch.cuda.synchronize()
+        got, own = tokens.cpu().numpy(), probs.cpu().numpy()
+        eager = choose(z, params, uu, R.F32)
+        assert np.array_equal(got, eager[0]) and np.array_equal(own, eager[1])
+        assert np.array_equal(got, check(z, *new, uu, R.F32))
