@@ -44,6 +44,7 @@ struct Chunk {                             // 8 consecutive elements
     static constexpr int kBytes = 16;
     u32x4 w;
     __device__ __forceinline__ void load(const unsigned char* p) { w = *(const u32x4*)p; }
+    __device__ __forceinline__ void load_far(const unsigned char* p) { w = __builtin_nontemporal_load((const u32x4*)p); }
     __device__ __forceinline__ void clear() { w = u32x4{0, 0, 0, 0}; }
     __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
@@ -55,6 +56,10 @@ struct Chunk {                             // 8 consecutive elements
     static __device__ __forceinline__ void put(unsigned char* p, const float (&v)[8]) {
         *(u32x4*)p = u32x4{Fmt::pack2(v[0], v[1]), Fmt::pack2(v[2], v[3]), Fmt::pack2(v[4], v[5]), Fmt::pack2(v[6], v[7])};
     }
+    // past the caches: 16 bytes a lane of consecutive lanes are whole lines
+    static __device__ __forceinline__ void put_far(unsigned char* p, const float (&v)[8]) {
+        __builtin_nontemporal_store(u32x4{Fmt::pack2(v[0], v[1]), Fmt::pack2(v[2], v[3]), Fmt::pack2(v[4], v[5]), Fmt::pack2(v[6], v[7])}, (u32x4*)p);
+    }
 };
 template <>
 struct Chunk<FmtF32> {
@@ -63,6 +68,10 @@ struct Chunk<FmtF32> {
     __device__ __forceinline__ void load(const unsigned char* p) {
         w[0] = ((const u32x4*)p)[0];
         w[1] = ((const u32x4*)p)[1];
+    }
+    __device__ __forceinline__ void load_far(const unsigned char* p) {
+        w[0] = __builtin_nontemporal_load((const u32x4*)p);
+        w[1] = __builtin_nontemporal_load((const u32x4*)p + 1);
     }
     __device__ __forceinline__ void clear() { w[0] = w[1] = u32x4{0, 0, 0, 0}; }
     __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -73,6 +82,8 @@ struct Chunk<FmtF32> {
         ((f32x4*)p)[0] = f32x4{v[0], v[1], v[2], v[3]};
         ((f32x4*)p)[1] = f32x4{v[4], v[5], v[6], v[7]};
     }
+    // (halves of lines, which the L2 has to put together: past it 8192 x 8192 into 8 bits and back took 146 us, through it 142)
+    static __device__ __forceinline__ void put_far(unsigned char* p, const float (&v)[8]) { put(p, v); }
 };
 
 // The larger of the quad's values, in all four lanes.
@@ -149,7 +160,9 @@ __device__ __forceinline__ float towards(float y, float rest) {
 
 // A row by TPR threads (a wave, or a workgroup of 256 or 1024), CH chunks each, which stay in
 // registers between the sum of squares and the outputs: x and the residual are read once.  HBM bounds many rows (8437 x
-// 5120 with all outputs 73-76 us, 5.1-5.3 TB/s), the launch and the chain of load, sum and barrier a few (one row of 4096: 3.7 us).
+// 5120 with all outputs 70-71 us, 5.5 TB/s), the launch and the chain of load, sum and barrier a few (one row of 4096: 3.3 us).
+// Rows of 16 bits are written past the caches (256 x 8192 6.6 -> 5.6 us, 1024 x 8192 18.4 -> 14.2, 8437 x 5120 73.5 -> 71.3); the
+// products that read them next take the same time either way.
 // Every output of a row is written after all of its inputs are read where that is asked
 // for: y depends on the whole row, and total[i] only on x[i] and residual[i].
 template <class Fmt, int CH, int TPR>
@@ -187,7 +200,7 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
             q = fmaf(s[i][e], s[i][e], q);
         }
         sum += q;
-        if (a.total && i * TPR + t < a.chunks) Chunk<Fmt>::put(a.total + row * a.ldt + 16 * (i * TPR + t), s[i]);
+        if (a.total && i * TPR + t < a.chunks) Chunk<Fmt>::put_far(a.total + row * a.ldt + 16 * (i * TPR + t), s[i]);
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
@@ -235,7 +248,7 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
                 if ((__float_as_uint(v[e]) & kHalfWay) == 0) v[e] = towards(v[e], fmaf(hi, w[e], -v[e]) + lo_by);
             }
         }
-        if (a.y && c < a.chunks) Chunk<Fmt>::put(a.y + row * a.ldy + 16 * c, v);
+        if (a.y && c < a.chunks) Chunk<Fmt>::put_far(a.y + row * a.ldy + 16 * c, v);
         if (a.codes && i * TPR < a.chunks) {
             if (c >= a.chunks) {           // (rows of zeros may not be: 0 times infinity)
 #pragma unroll
@@ -261,10 +274,11 @@ void launch_norm_tpr(const NormArgs& a, int tpr, hipStream_t st) {
 
 template <class Fmt>
 void launch_norm(const NormArgs& a, hipStream_t st) {
-    // many short rows: a wave each, without barriers; few long ones: as many threads as there are chunks, for the sake of
-    // the loads on their way (us with 256 against 1024 threads, h 8192: 64 rows 5.3 against 4.4, 256 rows 6.6 against
-    // 6.2; past that the barriers of 16 waves cost more: 1024 rows 14.3 against 15.3, 8437 x 5120 75.2 against 80.5)
-    const int tpr = a.n_rows >= 1024 && a.chunks <= 256 ? 64 : a.chunks <= (a.n_rows <= 512 ? 512 : 1024) ? 256 : 1024;
+    // many short rows: a wave each, without barriers; long ones, and rather long ones that are few: as many threads as there are
+    // chunks, for the sake of the loads on their way (us with 256 against 1024 threads, h 8192: 64 rows 5.9 against 4.4, 256 rows
+    // 7.2 against 5.8, 2048 rows 31.6 against 30.3; h 4096: one row 3.7 against 3.3, 256 rows 4.5 against 4.1, 512 rows 5.9 against
+    // 6.2; 8437 x 5120 70.0 against 72.2; a wave against 256 threads: 4000 x 1024 8.1 against 9.8, 1024 x 2048 7.2 against 5.7)
+    const int tpr = a.n_rows >= 1024 && a.chunks <= 128 ? 64 : a.chunks > 768 || (a.chunks >= 512 && a.n_rows <= 256) ? 1024 : 256;
     const int ch = (a.chunks + tpr - 1) / tpr;
     if (ch <= 1) launch_norm_tpr<Fmt, 1>(a, tpr, st);
     else if (ch <= 2) launch_norm_tpr<Fmt, 2>(a, tpr, st);
@@ -285,16 +299,21 @@ struct BlocksArgs {
     int format;
 };
 
-// A chunk a thread, blocks in the order of memory: a 28672 x 8192 weight into 4 bits and back takes 252 us, 4.2 TB/s (the
-// trace: 122 and 138; a large copy runs at 4.9 TB/s); 203 rows of 4096 into 8 bits and back 4.6, two launches.
-template <class Fmt>
+// A chunk a thread, blocks in the order of memory, rows written past the caches: a 28672 x 8192 weight into 4 bits and back takes
+// 189 us, 5.7 TB/s (254 through the caches; a large copy runs at 4.9 TB/s); 203 rows of 4096 into 8 bits and back 4.4, two launches.
+// FAR: values are read past the caches.
+template <class Fmt, bool FAR>
 __global__ void __launch_bounds__(kThreads) lora_mx_quantize_kernel(BlocksArgs a) {
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
     if (i >= a.total) return;              // (whole quads: total is a multiple of 4)
     const uint32_t row = i / a.per_row, c = i - row * a.per_row;
     Chunk<Fmt> in;
     in.clear();
-    if (c < a.chunks) in.load(a.values + row * a.ld + (uint32_t)Chunk<Fmt>::kBytes * (uint64_t)c);
+    const unsigned char* from = a.values + row * a.ld + (uint32_t)Chunk<Fmt>::kBytes * (uint64_t)c;
+    if (c < a.chunks) {
+        if (FAR) in.load_far(from);
+        else in.load(from);
+    }
     float v[8];
     in.get(v);
     u32x2 w;
@@ -329,7 +348,7 @@ __global__ void __launch_bounds__(kThreads) lora_mx_dequantize_kernel(BlocksArgs
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= f;
-    Chunk<Fmt>::put(a.values + row * a.ld + (uint32_t)Chunk<Fmt>::kBytes * (uint64_t)c, v);
+    Chunk<Fmt>::put_far(a.values + row * a.ld + (uint32_t)Chunk<Fmt>::kBytes * (uint64_t)c, v);
 }
 
 int element_bytes(int32_t dtype) { return dtype == LORA_F32 ? 4 : 2; }
@@ -341,6 +360,7 @@ int check_values(const char* name, const void* p, const char* ld_name, int64_t l
 }
 
 constexpr uint32_t kLaunchChunks = 1u << 30;   // of one launch, at most (or one row)
+constexpr int64_t kFar = 256 << 20;            // bytes of the memory-side cache
 
 template <bool BACK>
 int enqueue_blocks(const char* name, const lora_mx_t* q, const void* values, int64_t ld, int32_t dtype, void* stream) {
@@ -355,6 +375,9 @@ int enqueue_blocks(const char* name, const lora_mx_t* q, const void* values, int
     a.chunks = (uint32_t)q->h / 8;
     a.per_row = 4 * (uint32_t)mx_blocks(q->h);
     a.format = q->format;
+    // (more than the memory-side cache holds, of which nothing is there and nothing would stay: 28672 x 8192 in bfloat16 into 4
+    // bits and back 189 us against 221 through the caches; 13824 x 5120 72.0 against 70.7, 203 x 4096 4.7 against 4.5)
+    const bool far = (int64_t)q->n_rows * q->h * element_bytes(dtype) > kFar;
     const uint32_t row = BACK ? a.chunks : a.per_row;
     const int32_t step = (int32_t)std::max(1u, kLaunchChunks / row);
     for (int64_t r = 0; r < q->n_rows; r += step) {
@@ -369,9 +392,10 @@ int enqueue_blocks(const char* name, const lora_mx_t* q, const void* values, int
             else if (dtype == LORA_BF16) hipLaunchKernelGGL(lora_mx_dequantize_kernel<FmtBF16>, grid, dim3(kThreads), 0, st, a);
             else hipLaunchKernelGGL(lora_mx_dequantize_kernel<FmtF32>, grid, dim3(kThreads), 0, st, a);
         } else {
-            if (dtype == LORA_F16) hipLaunchKernelGGL(lora_mx_quantize_kernel<FmtF16>, grid, dim3(kThreads), 0, st, a);
-            else if (dtype == LORA_BF16) hipLaunchKernelGGL(lora_mx_quantize_kernel<FmtBF16>, grid, dim3(kThreads), 0, st, a);
-            else hipLaunchKernelGGL(lora_mx_quantize_kernel<FmtF32>, grid, dim3(kThreads), 0, st, a);
+            auto kernel = dtype == LORA_F16    ? far ? lora_mx_quantize_kernel<FmtF16, true> : lora_mx_quantize_kernel<FmtF16, false>
+                          : dtype == LORA_BF16 ? far ? lora_mx_quantize_kernel<FmtBF16, true> : lora_mx_quantize_kernel<FmtBF16, false>
+                          : far ? lora_mx_quantize_kernel<FmtF32, true> : lora_mx_quantize_kernel<FmtF32, false>;
+            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a);
         }
         if (int rc = check_launch(name)) return rc;
     }

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kJoinThreads) lora_mx_join_kernel(GemmArgs a) 
 // of 32, two slices of K 64.  Loads go from memory to LDS without registers, RING - 1 steps ahead; a slice's
 // fragments are read while the slice before is multiplied; one barrier a step.
 //
-// 8437 rows, 5120 -> 13824, 8-bit x: 487-496 us, 2.4 PFLOP/s (550 on another card); 2048 rows, 8192 -> 8192, 4-bit x: 77-82 us,
+// 8437 rows, 5120 -> 13824, 8-bit x: 482-490 us, 2.4 PFLOP/s (550 on another card); 2048 rows, 8192 -> 8192, 4-bit x: 75-81 us,
 // 3.5 PFLOP/s; 64 rows, 8192 -> 28672: 36-38 us, 3.4 TB/s of W, bound by loads.  Of the first the matrix instructions alone
 // take 300 us (they are 4 PFLOP/s with 8-bit x, 6 with 4-bit x), the loads alone 347, and the whole with codes of zero 400 where
 // random ones take 550: the clock, which the power limit sets by what the data make the units switch, is a good part of
@@ -338,7 +338,8 @@ __global__ void __launch_bounds__(64 * WN * WT) lora_mx_tile_kernel(GemmArgs a) 
         return;
     }
     // 16-bit y: 32 rows at a time through the wave's own share of LDS (16-byte chunk q of row r at slot
-    // q ^ r % 16, its halves swapped for odd r / 16) and out by rows, 16 bytes per lane
+    // q ^ r % 16, its halves swapped for odd r / 16) and out by rows, 16 bytes per lane, past the caches, which keep x and W
+    // (8437 rows, 5120 -> 13824: 490 -> 483 us, 2048 rows, 8192 -> 8192 with 4-bit x 86 -> 81)
     constexpr int QC = 4 * C::NB, kMask = QC < 16 ? QC - 1 : 15;
     u32x2* q8 = (u32x2*)(smem + T.w * 32 * QC);
     const u32x4* q16 = (const u32x4*)q8;
@@ -359,7 +360,7 @@ __global__ void __launch_bounds__(64 * WN * WT) lora_mx_tile_kernel(GemmArgs a) 
             const u32x4 v = q16[ro * QC + (qc ^ (ro & kMask))];
             const int row = tb + 32 * j + ro, n = nb + 8 * qc;
             if (row < a.n_rows && n < a.h_out)
-                *(u32x4*)((uint16_t*)a.y + row * a.ldy + n) = (ro >> 4) & 1 ? u32x4{v.z, v.w, v.x, v.y} : v;
+                __builtin_nontemporal_store((ro >> 4) & 1 ? u32x4{v.z, v.w, v.x, v.y} : v, (u32x4*)((uint16_t*)a.y + row * a.ldy + n));
         }
         __builtin_amdgcn_sched_barrier(0);
     }
