@@ -129,7 +129,9 @@ class Step:
             self.v = torch.empty_like(self.k)
             self.a = torch.empty_like(self.q)
             self._make_blocks(seg_lens)
-        self._plans, self._plan_of = [], {}              # plans with what they serve; a table's plan, or that of three
+        # plans with what they serve; the plan of a table behind weights of one kind (the same adapters may be behind
+        # weights of both), or of three tables behind weights in blocks
+        self._plans, self._plan_of = [], {}
         try:
             for layer in self.layers:
                 one = self._plan_for_three(layer, stream)
@@ -189,8 +191,8 @@ class Step:
             raise ValueError(f"{what}: a norm's weight is {self.q.dtype} [{self.hidden}] on {self.q.device}, contiguous")
 
     def _plan_for(self, p: Projection, stream):
-        """One plan serves all tables of a shape whose adapters agree in rank."""
-        if p.table in self._plan_of:
+        """One plan serves all tables of a shape and kind of weight whose adapters agree in rank."""
+        if (p.table, p.in_blocks) in self._plan_of:
             return
         for kind, plan in self._plans:
             if kind == (p.shape, p.in_blocks) and self._fits(plan, p):
@@ -198,7 +200,7 @@ class Step:
         else:
             plan = (L.lora_plan_create if p.in_blocks else L.lora_base_plan_create)(p.table, self.batch, stream)
             self._plans.append(((p.shape, p.in_blocks), plan))
-        self._plan_of[p.table] = plan
+        self._plan_of[p.table, p.in_blocks] = plan
 
     def _plan_for_three(self, layer: Layer, stream) -> bool:
         """One plan, and one launch, for the deltas of q, k and v behind weights in blocks (a token of 24 sequences, 4
@@ -250,7 +252,7 @@ class Step:
 
     def _apply(self, p: Projection, x, y, stream, rows=None, delta=True):
         """``rows``: x in blocks, for a weight in blocks; ``delta``: with the adapters' (there)."""
-        plan = self._plan_of.get(p.table)
+        plan = self._plan_of.get((p.table, p.in_blocks))
         if p.in_blocks:
             MX.lora_mx_apply(rows, p.wt, y, y.stride(0), self.code, self.ws, self.ws_bytes, stream)
             if self.n_rows and delta:                  # (without rows x and y have no memory, which the call refuses)
@@ -282,9 +284,11 @@ class Step:
                          self.code, self.total, self.hidden, self.h, self.hidden, rows, stream)
             x = self.h
         done = {self.hidden} if self.normed else set()   # widths of x that are in blocks already
-        tables = tuple(p.table for p in (w.q, w.k, w.v))
-        together = self._plan_of.get(tables)             # the plan of the three deltas in one launch
-        for p, y in ((w.q, self.q), (w.k, self.k), (w.v, self.v)):
+        three = (w.q, w.k, w.v)
+        tables = tuple(p.table for p in three)
+        # the plan of the three deltas in one launch (a 16-bit weight's own launch adds its delta)
+        together = self._plan_of.get(tables) if all(p.in_blocks for p in three) else None
+        for p, y in zip(three, (self.q, self.k, self.v)):
             rows = self._rows.get(("hq", p.shape[0])) if p.in_blocks else None
             if rows is not None and p.shape[0] not in done:
                 MX.lora_mx_quantize(x, x.stride(0), self.code, rows, stream)
