@@ -192,11 +192,14 @@ int lora_base_apply(lora_table_t t, const lora_batch_t* b, const void* x, int64_
  * dtype and referenced ranks match the plan's (NULL: the plan's own table),
  * with the operand rules of lora_base_apply.  Launches on one plan use the
  * plan's memory: order them on one stream.  lora_base_plan_destroy frees it.
+ * lora_base_plan_fits says whether lora_base_plan_apply takes table t, on the host
+ * only: LORA_OK, or the code that the apply would return for the table.
  */
 typedef struct lora_base_plan_s* lora_base_plan_t;
 int lora_base_plan_create(lora_base_plan_t* out, lora_table_t t, const lora_batch_t* b, void* stream);
 int lora_base_plan_apply(lora_base_plan_t p, lora_table_t t, const void* x, int64_t ldx, const void* wt, int64_t ldw,
                          void* y, int64_t ldy, void* stream);
+int lora_base_plan_fits(lora_base_plan_t p, lora_table_t t);
 int lora_base_plan_destroy(lora_base_plan_t p);
 
 /*
@@ -250,6 +253,9 @@ int lora_apply_fused_static(lora_table_t t, const lora_batch_t* b, const void* x
  * adapters holds them in its arguments; others may read them from the table's
  * device copy when they run).  A mismatch returns
  * LORA_E_SHAPE / LORA_E_RANK / LORA_E_INDEX and enqueues nothing.
+ * lora_plan_fits asks the same of the n tables that a launch of the plan would be given
+ * (n = 1; of lora_plan_create_multi, below, the plan's n; LORA_E_ARG for another n), on the
+ * host only: LORA_OK, or the code that the launch would return for the tables.
  *
  * lora_plan_shrink and lora_plan_expand are the two halves as separate
  * launches, for callers that schedule or time them apart: the shrink (a
@@ -260,6 +266,7 @@ int lora_apply_fused_static(lora_table_t t, const lora_batch_t* b, const void* x
  * stream): they share its workspace.
  */
 int lora_plan_create(lora_plan_t* out, lora_table_t t, const lora_batch_t* b, void* stream);
+int lora_plan_fits(lora_plan_t p, int32_t n, const lora_table_t* tables);
 
 /*
  * Re-planning for continuous batching (Section 2.2: the batch changes every

@@ -213,7 +213,7 @@ class Step:
             return True
         kind = tuple(p.shape for p in three)
         for k, plan in self._plans:
-            if k == kind and self._three_fit(plan, three):
+            if k == kind and L.lora_plan_fits(plan, tables):
                 break
         else:
             try:
@@ -227,28 +227,8 @@ class Step:
         return True
 
     @staticmethod
-    def _three_fit(plan: int, three) -> bool:
-        # (as below: the last y is missing, so nothing can be enqueued, and the call comes to say so only if all tables fit)
-        (h, n0), n1, n2 = three[0].shape, three[1].shape[1], three[2].shape[1]
-        try:
-            L.lora_plan_apply_multi(plan, [p.table for p in three], 1 << 40, h, [1 << 41, 1 << 42, None], [n0, n1, n2])
-        except L.LoraError as e:
-            return e.code == L.LORA_E_ARG
-        return False
-
-    @staticmethod
     def _fits(plan: int, p: Projection) -> bool:
-        # (a call without operands enqueues nothing: it is refused for the table where that does not
-        # fit the plan, for the missing x where it does; a plan of no rows takes it.  The delta's plan looks for
-        # missing operands first: there it is an x that no call may have)
-        try:
-            if p.in_blocks:
-                L.lora_plan_apply(plan, p.table, 1, p.shape[0], 1, p.shape[1])
-            else:
-                L.lora_base_plan_apply(plan, p.table, None, p.shape[0], None, p.shape[0], None, p.shape[1])
-        except L.LoraError as e:
-            return e.code == (L.LORA_E_ALIGN if p.in_blocks else L.LORA_E_ARG)
-        return True
+        return L.lora_plan_fits(plan, (p.table,)) if p.in_blocks else L.lora_base_plan_fits(plan, p.table)
 
     def _apply(self, p: Projection, x, y, stream, rows=None, delta=True):
         """``rows``: x in blocks, for a weight in blocks; ``delta``: with the adapters' (there)."""

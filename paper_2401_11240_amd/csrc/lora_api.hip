@@ -1547,15 +1547,21 @@ int lora_base_plan_create(lora_base_plan_t* out, lora_table_t t, const lora_batc
 
 int lora_base_plan_apply(lora_base_plan_t pl, lora_table_t t, const void* x, int64_t ldx, const void* wt, int64_t ldw,
                          void* y, int64_t ldy, void* stream) {
-    if (!pl || !pl->dmem) return fail(LORA_E_ARG, "plan is NULL");
+    if (int rc = lora_base_plan_fits(pl, t)) return rc;
     const lora_table_s* tt = t ? t : pl->table;
-    if (int rc = check_compatible(pl->L.p, tt)) return rc;
-    if (tt->device != pl->device) return fail(LORA_E_ARG, "table is on another device than the plan");
     if (pl->n_rows == 0) return LORA_OK;
     uint64_t w_span = 0;
     if (int rc = check_base_operands(tt, pl->n_rows, x, ldx, wt, ldw, y, ldy, &w_span)) return rc;
     DeviceGuard dg(tt->device);
     return base_run(tt, pl->L, pl->n_rows, pl->dmem, x, ldx, wt, ldw, w_span, y, ldy, (hipStream_t)stream);
+}
+
+int lora_base_plan_fits(lora_base_plan_t pl, lora_table_t t) {
+    if (!pl || !pl->dmem) return fail(LORA_E_ARG, "plan is NULL");
+    const lora_table_s* tt = t ? t : pl->table;
+    if (int rc = check_compatible(pl->L.p, tt)) return rc;
+    if (tt->device != pl->device) return fail(LORA_E_ARG, "table is on another device than the plan");
+    return LORA_OK;
 }
 
 int lora_base_plan_destroy(lora_base_plan_t pl) {
@@ -1708,6 +1714,19 @@ int lora_plan_apply_multi(lora_plan_t pl, const lora_table_t* tables, const void
         a.ph_out[i] = tt->h_out;
     }
     LORA_HIP_TRY(launch_step(a, (const uint32_t*)pl->dmem, t0->dtype, (hipStream_t)stream));
+    return LORA_OK;
+}
+
+int lora_plan_fits(lora_plan_t pl, int32_t n, const lora_table_t* tables) {
+    if (!pl || !pl->dmem) return fail(LORA_E_ARG, "plan is NULL");
+    if (!tables) return fail(LORA_E_ARG, "tables is NULL");
+    if (n != pl->plan.n_proj) return fail(LORA_E_ARG, "the plan has " + std::to_string(pl->plan.n_proj) + " projections");
+    for (int i = 0; i < n; ++i) {
+        const lora_table_s* tt = tables[i] ? tables[i] : (i == 0 ? pl->table : nullptr);
+        if (!tt) return fail(LORA_E_ARG, "table " + std::to_string(i) + " is NULL");
+        if (int rc = check_compatible_proj(pl->plan, tt, i)) return rc;
+        if (tt->device != pl->device) return fail(LORA_E_ARG, "table is on another device than the plan");
+    }
     return LORA_OK;
 }
 

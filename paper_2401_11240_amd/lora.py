@@ -42,7 +42,7 @@ EXPORTS = (
     "lora_plan_bytes", "lora_plan_create_reserved", "lora_plan_update", "lora_apply_fused_static",
     "lora_plan_create_multi", "lora_plan_apply_multi",
     "lora_base_workspace_bytes", "lora_base_apply", "lora_base_plan_create", "lora_base_plan_apply",
-    "lora_base_plan_destroy",
+    "lora_base_plan_destroy", "lora_plan_fits", "lora_base_plan_fits",
     "lora_group_rows", "lora_plan_inspect", "lora_base_inspect", "lora_last_error", "lora_abi_version",
 )
 
@@ -110,6 +110,7 @@ def load():
         "lora_base_plan_create": [C.POINTER(vp), vp, C.POINTER(_Batch), vp],
         "lora_base_plan_apply": [vp, vp, vp, i64, vp, i64, vp, i64, vp],
         "lora_base_plan_destroy": [vp],
+        "lora_base_plan_fits": [vp, vp],
         "lora_plan_create": [C.POINTER(vp), vp, C.POINTER(_Batch), vp],
         "lora_plan_bytes": [vp, C.POINTER(_Batch), C.POINTER(sz)],
         "lora_plan_create_reserved": [C.POINTER(vp), vp, C.POINTER(_Batch), sz, vp],
@@ -117,6 +118,7 @@ def load():
         "lora_plan_apply": [vp, vp, vp, i64, vp, i64, vp],
         "lora_plan_create_multi": [C.POINTER(vp), i32, C.POINTER(vp), C.POINTER(_Batch), vp],
         "lora_plan_apply_multi": [vp, C.POINTER(vp), vp, i64, C.POINTER(vp), C.POINTER(i64), vp],
+        "lora_plan_fits": [vp, i32, C.POINTER(vp)],
         "lora_plan_destroy": [vp],
         "lora_plan_shrink": [vp, vp, vp, i64, vp],
         "lora_plan_expand": [vp, vp, vp, i64, vp],
@@ -239,6 +241,18 @@ def lora_base_plan_apply(plan: int, table, x, ldx: int, wt, ldw: int, y, ldy: in
                                        _stream(stream)))
 
 
+def _fits(rc: int) -> bool:
+    if rc in (LORA_E_SHAPE, LORA_E_RANK, LORA_E_INDEX):
+        return False
+    _check(rc)
+    return True
+
+
+def lora_base_plan_fits(plan: int, table: int) -> bool:
+    """Whether the plan runs on this table."""
+    return _fits(load().lora_base_plan_fits(plan, table or None))
+
+
 def lora_base_plan_destroy(plan: int) -> None:
     _check(load().lora_base_plan_destroy(plan))
 
@@ -287,6 +301,11 @@ def lora_plan_apply_multi(plan: int, tables, x, ldx: int, ys, ldys, stream=None)
     Y = (C.c_void_p * max(1, n))(*[_addr(y) for y in ys])
     LD = (C.c_int64 * max(1, n))(*[int(v) for v in ldys])
     _check(load().lora_plan_apply_multi(plan, T, _addr(x), ldx, Y, LD, _stream(stream)))
+
+
+def lora_plan_fits(plan: int, tables) -> bool:
+    """Whether the plan runs on these tables (as many as its projections)."""
+    return _fits(load().lora_plan_fits(plan, len(tables), (C.c_void_p * max(1, len(tables)))(*[int(t or 0) for t in tables])))
 
 
 def lora_plan_shrink(plan: int, table, x, ldx: int, stream=None) -> None:

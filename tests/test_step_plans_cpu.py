@@ -123,3 +123,33 @@ def test_a_layer_partly_in_blocks_behind_one_that_is_wholly(library):
     step.project(1, x)
     assert library.ran == [("product", whole.q.wt), ("delta", 11), ("base", 12), ("product", whole.v.wt), ("delta", 13)]
     step.release()
+
+
+def test_a_step_asks_for_plans_and_runs_nothing(library, monkeypatch):
+    """Layers of one shape share plans, which the library is asked about: nothing that could enqueue is called before
+    the step runs."""
+    asked = []
+
+    def runs(*a, **k):
+        raise AssertionError("a step that is being made runs something")
+
+    def fits(plan, tables):
+        asked.append((plan, tables))
+        return True
+
+    for name in ("lora_plan_apply", "lora_plan_apply_multi", "lora_base_plan_apply", "lora_plan_shrink", "lora_plan_expand"):
+        monkeypatch.setattr(L, name, runs)
+    monkeypatch.setattr(L, "lora_plan_fits", fits)
+    monkeypatch.setattr(L, "lora_base_plan_fits", lambda plan, table: fits(plan, (table,)))
+    step = step_of([layer((1, 2, 3, 4), True), layer((5, 6, 7, 8), True), layer((9, 10, 11, 12), False)])
+    three, o = (THREE, (1, 2, 3)), (DELTA, 4)
+    assert asked == [(three, (5, 6, 7)), (o, (8,)), ((BASE, 9), (10,)), ((BASE, 9), (11,)), ((BASE, 9), (12,))]
+    assert [plan for _, plan in step._plans] == [three, o, (BASE, 9)]
+    step.release()
+
+
+def test_questions_about_no_plan():
+    for call in (lambda: L.lora_plan_fits(None, (None,)), lambda: L.lora_plan_fits(None, ()), lambda: L.lora_base_plan_fits(None, None)):
+        with pytest.raises(L.LoraError) as e:
+            call()
+        assert e.value.code == L.LORA_E_ARG
