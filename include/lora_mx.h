@@ -40,7 +40,8 @@
  *     leading dimensions too);
  *   - codes 16-byte aligned, ld_codes a multiple of 16 and at least a row's bytes;
  *     scales 4-byte aligned, ld_scales a multiple of 4 and at least a row's blocks;
- *   - codes and scales of the product's x and w: 256 leading dimensions within 0x7fff0000 bytes;
+ *   - codes and scales of the product's x and w: 256 leading dimensions within 0x7fff0000 bytes; rows of x
+ *     times rows of w at most 2^42;
  *   - element types LORA_F16, LORA_BF16, and LORA_F32 where it is named;
  *   - outputs do not overlap inputs or each other, but where it is said.
  *

@@ -28,7 +28,8 @@ typedef __attribute__((address_space(3))) unsigned char lds_u8;
 
 constexpr int kUnits = 256, kXcds = 8;     // compute units and XCDs of the card
 constexpr int64_t kJoinMost = 1 << 30;     // elements of y that may be joined from split K
-constexpr int64_t kMostTiles = 1 << 22;    // of a launch
+constexpr int64_t kMostTiles = 1 << 22;    // of a launch; a product of more goes to several
+constexpr int64_t kMostY = 1ll << 42;      // elements of y
 constexpr int kTileSpan = 256;             // rows that one buffer resource covers, at most
 
 struct GemmArgs {
@@ -565,9 +566,10 @@ Plan plan_product(int n_rows, int h_out, int blocks, int format) {
     for (const auto& t : kTiles)
         for (int want = 1; want <= 8; want *= 2) {
             const int range = 16 * ceil_div(sixteens, want), splits = ceil_div(blocks, range);
-            if (want > 1 && (splits <= want / 2 || (int64_t)n_rows * h_out > kJoinMost)) break;
+            const int64_t each_range = (int64_t)ceil_div(h_out, t[0]) * ceil_div(n_rows, t[1]);
+            if (want > 1 && (splits <= want / 2 || (int64_t)n_rows * h_out > kJoinMost || each_range > kMostTiles)) break;
             const double bytes = (double)std::min(range, blocks) * (t[0] * 16 + t[1] * (format == LORA_E4M3 ? 32 : 16)) * 1e-3;
-            const int64_t groups = (int64_t)ceil_div(h_out, t[0]) * ceil_div(n_rows, t[1]) * splits;
+            const int64_t groups = each_range * splits;
             const int64_t each = (groups + kUnits - 1) / kUnits, rest = each % t[2];    // of the unit with most
             const double unit = (double)(each - rest) * bytes / (t[2] > 1 ? 60 : 34) + (double)rest * bytes / (rest > 1 ? 60 : 34);
             double us = 4 + std::max(unit, (double)groups * bytes / 11800 + weight / 1e7);
@@ -589,6 +591,7 @@ int check_product(const lora_mx_t* x, const lora_mx_t* w) {
     if (w->format != LORA_E2M1) return set_error(LORA_E_ARG, "w: format must be LORA_E2M1");
     if (x->h != w->h) return set_error(LORA_E_SHAPE, "x and w differ in h");
     if (w->n_rows < 8 || w->n_rows % 8) return set_error(LORA_E_SHAPE, "w: n_rows must be a positive multiple of 8");
+    if ((int64_t)x->n_rows * w->n_rows > kMostY) return set_error(LORA_E_SHAPE, "y has more than 2^42 elements");
     for (const lora_mx_t* q : {x, w})
         if (std::max(q->ld_codes, q->ld_scales) * kTileSpan > (int64_t)kMaxSpan)
             return set_error(LORA_E_SHAPE, "256 rows of x or w span more than 0x7fff0000 bytes");
@@ -666,8 +669,6 @@ int lora_mx_apply(const lora_mx_t* x, const lora_mx_t* w, void* y, int64_t ldy, 
             if (o.meets(i)) return set_error(LORA_E_OVERLAP, "y or ws overlaps x or w");
     if (out[0].meets(out[1])) return set_error(LORA_E_OVERLAP, "y and ws overlap");
     if (x->n_rows == 0) return LORA_OK;
-    if ((int64_t)ceil_div(x->n_rows, 64) * ceil_div(w->n_rows, 64) > kMostTiles)
-        return set_error(LORA_E_SHAPE, "lora_mx_apply: too many rows times h_out");
     hipStream_t st = (hipStream_t)stream;
     StreamDevice g(st);
     if (!g.ok) return set_error(LORA_E_HIP, "lora_mx_apply: no device for the stream");
@@ -676,7 +677,7 @@ int lora_mx_apply(const lora_mx_t* x, const lora_mx_t* w, void* y, int64_t ldy, 
     a.xs = (const unsigned char*)x->scales;
     a.w = (const unsigned char*)w->codes;
     a.ws = (const unsigned char*)w->scales;
-    a.y = y;
+    a.y = y;                               // (of several launches, each has its own)
     a.part = (float*)ws;
     a.ldx = x->ld_codes;
     a.ldxs = x->ld_scales;
@@ -690,9 +691,23 @@ int lora_mx_apply(const lora_mx_t* x, const lora_mx_t* w, void* y, int64_t ldy, 
     const Plan p = plan_product(a.n_rows, a.h_out, a.blocks, x->format);
     a.splits = p.splits;
     a.split_blocks = p.split_blocks;
-    if (x->format == LORA_E4M3) launch_product<LORA_E4M3>(a, p, st);
-    else launch_product<LORA_E2M1>(a, p, st);
-    if (int rc = check_launch("lora_mx_apply")) return rc;
+    // rows and columns of a launch: whole tiles, at most kMostTiles
+    const int cols = p.tiles ? (int)std::min<int64_t>(a.h_out, kMostTiles * p.tn) : a.h_out;
+    const int rows = p.tiles ? (int)std::min<int64_t>(a.n_rows, kMostTiles / ceil_div(cols, p.tn) * p.tt) : a.n_rows;
+    for (int64_t n = 0; n < w->n_rows; n += cols)
+        for (int64_t t = 0; t < x->n_rows; t += rows) {
+            GemmArgs b = a;
+            b.x += t * a.ldx;
+            b.xs += t * a.ldxs;
+            b.w += n * a.ldw;
+            b.ws += n * a.ldws;
+            b.y = (char*)y + (t * ldy + n) * e;
+            b.n_rows = (int)std::min<int64_t>(rows, a.n_rows - t);
+            b.h_out = (int)std::min<int64_t>(cols, a.h_out - n);
+            if (x->format == LORA_E4M3) launch_product<LORA_E4M3>(b, p, st);
+            else launch_product<LORA_E2M1>(b, p, st);
+            if (int rc = check_launch("lora_mx_apply")) return rc;
+        }
     if (p.splits == 1) return LORA_OK;
     hipLaunchKernelGGL(lora_mx_join_kernel, dim3(ceil_div((int64_t)a.n_rows * (a.h_out / 4), kJoinThreads)), dim3(kJoinThreads), 0,
                        st, a);
