@@ -81,10 +81,10 @@ def lora_sample(logits, ld: int, dtype: int, n_rows: int, n_vocab: int, params, 
                 stream=None) -> None:
     if params is not None and params.n_rows is not None and params.n_rows < n_rows:
         raise ValueError(f"params: {params.n_rows} rows of {n_rows}")
-    on = next((t.device for t in (tokens, u, logits, probs) if hasattr(t, "device")), None)
+    on = next((t.device for t in (tokens, u, logits, probs, ws, params) if getattr(t, "device", None) is not None), None)
     if on is not None and on.type != "cuda":
         raise ValueError(f"tensors on {on}: device tensors are needed")
-    if params is not None and params.device is not None and (on or params.device) != params.device:
+    if params is not None and params.device is not None and on != params.device:
         raise ValueError(f"the parameters are on {params.device}, the rows on {on}")
     _check(_lib().lora_sample(_at(-1 if on is None else on.index, "logits", logits)[0], ld, dtype, n_rows, n_vocab, params.c if params is not None else None,
                               _array("u", u, n_rows, "torch.float32", on), _array("tokens", tokens, n_rows, "torch.int32", on),
