@@ -43,7 +43,8 @@
  *   - codes and scales of the product's x and w: 256 leading dimensions within 0x7fff0000 bytes; rows of x
  *     times rows of w at most 2^42;
  *   - element types LORA_F16, LORA_BF16, and LORA_F32 where it is named;
- *   - outputs do not overlap inputs or each other, but where it is said.
+ *   - outputs do not overlap inputs or each other, but where it is said.  Matrices whose rows are equally far
+ *     apart may be columns of one buffer; of others the memory from the first byte to the last counts.
  *
  * Asynchrony, errors and thread safety are lora.h's: calls are enqueued on the caller's
  * stream, allocate nothing, copy nothing to the host and never wait.  All may be recorded

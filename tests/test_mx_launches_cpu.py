@@ -35,3 +35,49 @@ def test_products_of_more_tiles_than_a_launch_has(calls, rows, h, h_out, fmt):
 def test_products_of_more_than_2_to_42_elements_are_refused(calls, rows, h, h_out):
     with pytest.raises(ValueError, match="2\\^42"):
         calls.product(rows, h, h_out, MX.LORA_E4M3, L.LORA_F16)
+
+
+COLUMNS = 1 << 48          # a buffer of 5 rows, 4096 bytes apart
+
+
+def mx_rows(codes, scales, ld, n=5, h=256, fmt=MX.LORA_E4M3):
+    return MX._Rows(COLUMNS + codes, COLUMNS + scales, ld, ld, n, h, fmt)
+
+
+@pytest.mark.parametrize("codes,scales,meet", [(0, 256, False), (16, 272, False), (256, 248, False), (0, 252, True), (0, 4088, False),
+                                               (0, 4092, True), (0, -8, False), (0, -4, True), (3840, 4096 - 256 - 8, False), (3856, 0, True),
+                                               (4096, 256, False), (4096, 256 + 2 * 4096, False), (4096, 252 + 2 * 4096, True), (0, 0, True)])
+def test_codes_and_scales_in_columns_of_one_buffer(calls, codes, scales, meet):
+    """256 bytes of codes and 8 of scales a row: refused only where a row's bytes are another's."""
+    q = mx_rows(codes + 4096, scales + 4096, 4096)
+
+    def call():
+        return calls._launched(calls.lib.lora_mx_quantize(9 << 48, 256, L.LORA_F16, q, None))
+    if meet:
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    else:
+        assert len(call()) == 1
+
+
+@pytest.mark.parametrize("rows,ldy,y,meet", [(5, 2048, 512, False), (5, 2048, 496, True), (5, 2048, 4096 - 512, False), (5, 2048, 4096 - 496, True),
+                                             (5, 2048, 16384 + 512, False), (5, 2056, 512, True), (5, 256, 5 * 4096, False), (1, 256, 512, False),
+                                             (1, 2048, 496, True), (1, 8, 512, False)])
+def test_a_norm_beside_its_rows(calls, rows, ldy, y, meet):
+    """Rows of 256 16-bit elements, 2048 apart: y in other columns, in rows of another distance, one row."""
+    def call():
+        return calls._launched(calls.lib.lora_norm(COLUMNS, 2048, None, 0, None, 1e-5, rows, 256, L.LORA_F16, None, 0, COLUMNS + y, max(ldy, 256), None, None))
+    if meet:
+        with pytest.raises(ValueError, match="overlap"):
+            call()
+    else:
+        assert len(call()) == 1
+
+
+def test_one_row_between_others(calls):
+    """u, tokens and probs between two rows of logits."""
+    launched = calls._launched(calls.lib.lora_sample(COLUMNS, 2048, L.LORA_F16, 5, 256, None, COLUMNS + 512, COLUMNS + 532, COLUMNS + 4096 - 20, 9 << 48, 16, None))
+    assert len(launched) == 1
+    for tokens, probs in ((COLUMNS + 508, COLUMNS + 600), (COLUMNS + 600, COLUMNS + 4096 - 16), (COLUMNS + 528, COLUMNS + 600), (COLUMNS + 600, COLUMNS + 612)):
+        with pytest.raises(ValueError, match="overlap"):
+            calls._launched(calls.lib.lora_sample(COLUMNS, 2048, L.LORA_F16, 5, 256, None, COLUMNS + 512, tokens, probs, 9 << 48, 16, None))
