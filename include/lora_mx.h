@@ -40,6 +40,8 @@
  *     leading dimensions too);
  *   - codes 16-byte aligned, ld_codes a multiple of 16 and at least a row's bytes;
  *     scales 4-byte aligned, ld_scales a multiple of 4 and at least a row's blocks;
+ *     (the product reads scales in whole 4-byte words, behind the last row's last block up to 3 bytes more, which
+ *     may hold anything but have to be readable);
  *   - codes and scales of the product's x and w: 256 leading dimensions within 0x7fff0000 bytes; rows of x
  *     times rows of w at most 2^42;
  *   - element types LORA_F16, LORA_BF16, and LORA_F32 where it is named;

@@ -36,7 +36,8 @@ def scale_bytes(h: int) -> int:
 class Rows:
     """Rows of h elements in blocks: uint8 device tensors codes [n_rows, at least
     ``code_bytes``] and scales [n_rows, at least a byte for each block], dense in the last
-    dimension."""
+    dimension.  (The product reads the last row's scales to the end of a 4-byte word: torch's own
+    allocations have it, memory of another origin must.)"""
 
     def __init__(self, codes, scales, fmt: int, h: int):
         for name, t in (("codes", codes), ("scales", scales)):

@@ -66,3 +66,21 @@ def test_a_norm_beside_its_rows(rows, h, dtype):
     MX.lora_norm(x, ld, r, ld, None, 1e-5, rows, h, dtype, t, ld, y, ld, None, stream())
     MX.lora_norm(xs, h, rs, h, None, 1e-5, rows, h, dtype, ts, h, ys, h, None, stream())
     assert torch.equal(t, ts) and torch.equal(y, ys) and torch.equal(x, xs) and torch.equal(r, rs) and (buf[:, 4 * h:] == 7).all()
+
+
+@formats
+@pytest.mark.parametrize("rows,h", [(1, 8), (3, 40), (1, 4104), (70, 264), (260, 1064)])
+def test_bytes_behind_the_last_scale_count_for_nothing(rows, h, fmt):
+    """Scales that end with their last block: the rest of the word may hold anything."""
+    rng = np.random.default_rng([42, rows, h, fmt])
+    n, ld = R.blocks(h), MX.scale_bytes(h)
+    x, w = random_rows(rng, rows, h, fmt), random_rows(rng, 264, h, R.E2M1)
+    want = apply(x, w, R.F32)
+
+    def ending(q, fill):
+        flat = torch.full((q.n_rows * ld + 64,), fill, dtype=torch.uint8, device=DEV)
+        s = flat.as_strided((q.n_rows, n), (ld, 1))
+        s.copy_(q.scales[:, :n])
+        return MX.Rows(q.codes, s, q.fmt, h)
+    for fill in (0, 1, 127, 255):
+        assert torch.equal(apply(ending(x, fill), ending(w, fill), R.F32), want)
