@@ -262,14 +262,19 @@ __global__ void __launch_bounds__(TPR < kThreads ? kThreads : TPR) lora_norm_ker
     }
 }
 
-template <class Fmt, int CH>
-void launch_norm_tpr(const NormArgs& a, int tpr, hipStream_t st) {
-    if (tpr == 64)
-        hipLaunchKernelGGL((lora_norm_kernel<Fmt, CH, 64>), dim3((a.n_rows + 3) / 4), dim3(kThreads), 0, st, a);
-    else if (tpr == 256)
-        hipLaunchKernelGGL((lora_norm_kernel<Fmt, CH, 256>), dim3(a.n_rows), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((lora_norm_kernel<Fmt, CH, 1024>), dim3(a.n_rows), dim3(1024), 0, st, a);
+template <class Fmt, int CH, int TPR>
+void launch_norm_form(const NormArgs& a, hipStream_t st) {
+    constexpr int kRows = TPR < kThreads ? kThreads / TPR : 1;
+    hipLaunchKernelGGL((lora_norm_kernel<Fmt, CH, TPR>), dim3((a.n_rows + kRows - 1) / kRows), dim3(TPR * kRows), 0, st, a);
+}
+// MOST: the most chunks a thread that TPR threads are given
+template <class Fmt, int TPR, int MOST>
+void launch_norm_tpr(const NormArgs& a, hipStream_t st) {
+    const int ch = (a.chunks + TPR - 1) / TPR;
+    if (ch <= 1) launch_norm_form<Fmt, 1, TPR>(a, st);
+    else if (ch <= 2) launch_norm_form<Fmt, 2, TPR>(a, st);
+    else if (ch <= 4) launch_norm_form<Fmt, std::min(MOST, 4), TPR>(a, st);
+    else launch_norm_form<Fmt, MOST, TPR>(a, st);
 }
 
 template <class Fmt>
@@ -279,11 +284,9 @@ void launch_norm(const NormArgs& a, hipStream_t st) {
     // 7.2 against 5.8, 2048 rows 31.6 against 30.3; h 4096: one row 3.7 against 3.3, 256 rows 4.5 against 4.1, 512 rows 5.9 against
     // 6.2; 8437 x 5120 70.0 against 72.2; a wave against 256 threads: 4000 x 1024 8.1 against 9.8, 1024 x 2048 7.2 against 5.7)
     const int tpr = a.n_rows >= 1024 && a.chunks <= 128 ? 64 : a.chunks > 768 || (a.chunks >= 512 && a.n_rows <= 256) ? 1024 : 256;
-    const int ch = (a.chunks + tpr - 1) / tpr;
-    if (ch <= 1) launch_norm_tpr<Fmt, 1>(a, tpr, st);
-    else if (ch <= 2) launch_norm_tpr<Fmt, 2>(a, tpr, st);
-    else if (ch <= 4) launch_norm_tpr<Fmt, 4>(a, tpr, st);
-    else launch_norm_tpr<Fmt, 8>(a, tpr, st);
+    if (tpr == 64) launch_norm_tpr<Fmt, 64, 2>(a, st);
+    else if (tpr == 256) launch_norm_tpr<Fmt, 256, 4>(a, st);
+    else launch_norm_tpr<Fmt, 1024, kNormMax / 8 / 1024>(a, st);
 }
 
 // ---------------------------------------------------------------------------

@@ -81,3 +81,30 @@ def test_one_row_between_others(calls):
     for tokens, probs in ((COLUMNS + 508, COLUMNS + 600), (COLUMNS + 600, COLUMNS + 4096 - 16), (COLUMNS + 528, COLUMNS + 600), (COLUMNS + 600, COLUMNS + 612)):
         with pytest.raises(ValueError, match="overlap"):
             calls._launched(calls.lib.lora_sample(COLUMNS, 2048, L.LORA_F16, 5, 256, None, COLUMNS + 512, tokens, probs, 9 << 48, 16, None))
+
+
+def test_every_kernel_is_reached(calls):
+    """No form of the norm, the blocks, the product or the sampling kernels is compiled that no call launches."""
+    reached = set()
+
+    def take(launched):
+        reached.update(ln.kernel for ln in launched)
+    for dtype in (L.LORA_F16, L.LORA_BF16, MX.LORA_F32):
+        for fmt in (MX.LORA_E4M3, MX.LORA_E2M1):
+            for rows in (1, 1 << 18):
+                q = calls._rows(0, rows, 1024, fmt)
+                take(calls._launched(calls.lib.lora_mx_quantize(9 << 48, 1024, dtype, q, None)))
+                take(calls._launched(calls.lib.lora_mx_dequantize(q, 9 << 48, 1024, dtype, None)))
+            for rows in (1, 4, 5, 16, 17, 32, 33, 64, 128, 256, 512, 2048, 8437):
+                for h in (64, 512, 4096, 8192):
+                    for h_out in (64, 1024, 4104, 8192, 28672):
+                        take(calls.product(rows, h, h_out, fmt, dtype)[0])
+        if dtype != MX.LORA_F32:
+            for rows in (1, 1023, 1024):
+                for chunks in [2 ** i + d for i in range(14) for d in (0, 1)] + [767, 768, 769, 3 * 256, 8192]:
+                    if chunks <= 8192:
+                        take(calls.norm(rows, 8 * chunks, dtype))
+        for rows, vocab in ((1, 100), (64, 128000)):
+            take(calls._launched(calls.lib.lora_sample(1 << 48, vocab, dtype, rows, vocab, None, 2 << 48, 3 << 48, None, 4 << 48, 1 << 40, None)))
+    mine = {k for k in calls.kernels() if k.startswith(("lora_norm", "lora_mx", "lora_sample"))}
+    assert reached == mine, sorted(mine - reached)
