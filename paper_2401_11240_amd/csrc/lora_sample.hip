@@ -23,10 +23,14 @@
 // a bit.
 //
 // What bounds it: a few rows, the four launches (3 to 9 us each in a trace; one row of 32000: 22 us, most of it the way of the first loads, of
-// code that every workgroup runs through once, and of barriers of sixteen waves); many rows with top_p and no small top_k, the weights
-// of all logits, about 20 binary64 operations each, twice where the list does not hold all that is kept, and their atomic additions
-// (64 rows of 128000 in bfloat16: 49 us); many rows with a small top_k, the reading of the logits (256 x 50257 in float32: 21 us, 51 MB,
-// of which 8 are that reading, 3 the second, of the threads that have a listed logit, and 8 the way from there to the token).
+// code that every workgroup runs through once, and of barriers of sixteen waves); many rows with top_p and no small top_k (64 rows of
+// 128000 in bfloat16: 49 us), that a compute unit has one workgroup: its 1024 threads take 72 to 98 registers each in the launches
+// that weigh 16-bit logits, of 64 that two workgroups would leave them, so nothing runs beside what it waits for (first loads, atomic
+// additions, barriers).  The weights by themselves, about 20 binary64 instructions of 4 cycles, are 4 us of the 32000 logits of a
+// workgroup, twice that where the list does not hold all that is kept or where nothing but min_p filters; and in a batch of
+// all kinds the workgroups of the rows with a small top_k have none of that work.  Many rows with a small top_k: the reading of the logits
+// (256 x 50257 in float32: 21 us, 51 MB, of which 8 are that reading, 3 the second, of the threads that have a listed logit, and 8 the
+// way from there to the token, through some twenty barriers of sixteen waves).
 #include <cmath>
 
 #include <algorithm>
@@ -279,7 +283,9 @@ struct Row {
 // f(logits, index of the first) for the logits of segment `seg`, by one wave, whose lanes hold kVec consecutive ones each,
 // lane by lane and step by step in the order of the indices.  NaN is as -infinity, and so is what lies past the
 // segment, and all that lanes have whose `want` is false.  (16 bytes a lane and load, at whatever alignment the row has; U
-// loads on their way together.)
+// loads on their way together.  A segment is a multiple of 256 logits and a step of a 16-bit row 512: where the multiple is odd the
+// last half step is read logit by logit, and so is all of segments of 256, which rows of up to 4096 logits have, and
+// few rows of up to 65536.)
 template <int DT>
 struct Vec {
     static constexpr int kVec = DT == LORA_F32 ? 4 : 8;
@@ -1168,7 +1174,10 @@ struct SamplePlan {
 // One launch and a workgroup a row from 129 rows on, or where a row is short; slices of 4096 logits at least, as many as
 // give every compute unit a workgroup, otherwise.  What a row costs depends on its parameters, which are on the device: with a
 // small top_k one workgroup is faster further up than with top_p alone.  Measured (us), one launch against 2, 4 and 8 slices:
-// 256 rows of 50257 with top_k 50 21 against 33, 39, 49, with top_p alone 57 against 68, 80, 92; 128 rows of 50257 18 against
+// 256 rows of 50257 with top_k 50 21 against 33, 39, 49, with top_p alone 57 against 68, 80, 92; of 128000 in bfloat16, one launch
+// against 2, 3 and 4 slices, all kinds, top_p 0.95 and top_k 50: 86 rows 100 against 70, 64, 56, 103 against 73, 82, 80 and 27 against 27, 37, 33;
+// 129 rows 103 against 74, 75, 70, 107 against 106, 109, 96 and 28 against 40, 39, 42; 200 rows 104 against 87, 106, 91, 107 against 123,
+// 146, 127 and 29 against 42, 54, 53; 300 rows 140 against 125, 131, 120, 200 against 181, 197, 176 and 53 against 62, 73, 70; 128 rows of 50257 18 against
 // 23, 26 and 55 against 50, 52, of 32000 14 against 21, 23 and 36 against 35, 42; 60 rows of 24000 12 against 19, 19 and 29
 // against 35, 29, of 50257 17 against 21, 20 and 54 against 49, 36; 64 rows of 128000, all kinds, 103 against 70, 49, 50; 16 rows
 // of 32000 without filters 28 against 26, 22, 22; one row of 20000 with top_p 22 against 25, 23, 22, of 32000 28 against 27, 23, 22.
